@@ -16,6 +16,11 @@
  *                               query embeddings and every context embedding, highest scores
  *                               selected, neighbourhood kept contiguous (Sec. 3.3, App. C.6).
  *
+ * Around them stand the calls that a model's serving needs next to these: rotary positions
+ * (reform_rotary_embed), whole prompts packed into one batch (reform_prompt_attend), and generation
+ * from a batch of caches, by single tokens or by trees of drafted ones (reform_tree_attend,
+ * reform_tree_accept).
+ *
  * Conventions common to all calls
  *   - Every data pointer is a DEVICE pointer (HIP global memory) owned by the caller.  The
  *     library never allocates, frees or keeps a pointer; scratch comes in through `workspace`,
@@ -366,6 +371,187 @@ typedef struct {
 reform_status reform_gather_rows(const reform_rows_desc *desc, const void *table,
                                  const int32_t *idx, const int32_t *count, void *out,
                                  int32_t *err, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------- */
+/* reform_rotary_embed -- queries and keys to their positions, keys and values into the caches
+ *
+ * For token i at position pos[i] and pair c in [0, rotary_dim/2) with frequency f_c:
+ *     a       = pos[i] * f_c                     (inverse = 1: -pos[i] * f_c)
+ *     y[x]    = magnitude * (x cos a - x' sin a)     of every query and key head, where (x, x') are the
+ *     y[x']   = magnitude * (x' cos a + x sin a)     elements of the pair: c and c + rotary_dim/2
+ *               (REFORM_PAIRS_HALVES) or 2c and 2c + 1 (REFORM_PAIRS_ADJACENT)
+ * Elements [rotary_dim, head_dim) and values are copied.  inverse = 1 is the transposed map: with the
+ * same magnitude it takes the gradient of the rotated states to that of the unrotated ones; with
+ * 1 / magnitude it takes the rotation back.
+ *     f_c = theta^(-2c/rotary_dim)                                          REFORM_ROPE_PLAIN
+ *         = theta^(-2c/rotary_dim) / factor                                 REFORM_ROPE_LINEAR
+ *         = theta'^(-2c/rotary_dim), theta' = theta * factor^(rotary_dim/(rotary_dim-2))  REFORM_ROPE_BASE
+ *         = f (1 - r_c) + f / factor * r_c, f = theta^(-2c/rotary_dim):     REFORM_ROPE_PARTS: r_c rises from 0
+ *               at pair floor(p(turns_high)) to 1 at pair ceil(p(turns_low)), both kept within [0, rotary_dim-1],
+ *               p(t) = rotary_dim ln(original_len / (2 pi t)) / (2 ln theta): the pair that turns t times
+ *               within original_len
+ *                                                                           REFORM_ROPE_BANDS: r_c falls from 1
+ *               at turns_low to 0 at turns_high turns within original_len, linearly in the turns
+ * Frequencies and angles are formed in fp64 and reduced to a fraction of a turn before the fp32
+ * sine and cosine; products and sums in fp32, rounded once.
+ *
+ *     q, q_out    [n_q_heads][n_tokens][head_dim] by strides; NULL iff n_q_heads = 0
+ *     k, v        [n_kv_heads][n_tokens][head_dim] by strides; k NULL iff n_kv_heads = 0, v may be NULL
+ *                 (no values); input strides of 0 (one head or row for all) are allowed
+ *     k_out,v_out slot == NULL: as k, row i for token i, strides kv_out_*.  Otherwise caches in n_blocks
+ *                 blocks of block_len rows, block_stride elements apart: token i goes to row
+ *                 slot[i] % block_len of block slot[i] / block_len, head h kv_out_head_stride elements
+ *                 behind head h-1; a token whose slot is outside [0, n_blocks*block_len) is not stored
+ *                 (padding).  Slots should differ: of two tokens with one slot the row holds either or a
+ *                 mixture.  v_out may be NULL iff v is.
+ *     pos         [n_tokens] int32, any sign
+ *     slot        [n_tokens] int32 or NULL
+ * q_out may be q, and without slots k_out may be k and v_out v, with the same strides (then rotated in
+ * place); other overlaps of outputs with inputs or each other are not allowed.
+ * Supported: head_dim <= 512 and a multiple of 16 bytes; rotary_dim even, at most head_dim, a multiple of 16
+ * bytes (REFORM_PAIRS_ADJACENT) or of 32 (REFORM_PAIRS_HALVES); strides multiples of 16 bytes, pointers
+ * 16-byte aligned; n_tokens = 0 does nothing.
+ */
+typedef enum { REFORM_PAIRS_HALVES = 0, REFORM_PAIRS_ADJACENT = 1 } reform_rope_pairs;
+typedef enum {
+    REFORM_ROPE_PLAIN = 0, REFORM_ROPE_LINEAR = 1, REFORM_ROPE_BASE = 2, REFORM_ROPE_PARTS = 3, REFORM_ROPE_BANDS = 4
+} reform_rope_scaling;
+
+typedef struct {
+    uint32_t struct_size;
+    int32_t  dtype;
+    int32_t  n_tokens, n_q_heads, n_kv_heads, head_dim;
+    int32_t  rotary_dim;
+    int32_t  pairs;                          /* reform_rope_pairs                              */
+    int32_t  inverse;                        /* 0 or 1                                         */
+    int32_t  scaling;                        /* reform_rope_scaling                            */
+    double   theta;                          /* > 1, finite                                    */
+    double   factor;                         /* >= 1, finite; not read for REFORM_ROPE_PLAIN   */
+    double   turns_high, turns_low;          /* 0 < turns_low < turns_high, finite, and ...    */
+    int32_t  original_len;                   /* ... >= 1: read for PARTS and BANDS only        */
+    float    magnitude;                      /* > 0, finite; 1 unless the model asks for another */
+    int32_t  block_len, n_blocks;            /* read iff slot != NULL; block_len*n_blocks < 2^31 */
+    int64_t  block_stride;                   /* all strides in elements                        */
+    int64_t  q_head_stride, q_row_stride, k_head_stride, k_row_stride, v_head_stride, v_row_stride;
+    int64_t  q_out_head_stride, q_out_row_stride, kv_out_head_stride, kv_out_row_stride;
+} reform_rotary_desc;
+
+reform_status reform_rotary_embed(const reform_rotary_desc *desc, const void *q, const void *k, const void *v,
+                                  const int32_t *pos, const int32_t *slot,
+                                  void *q_out, void *k_out, void *v_out, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------- */
+/* reform_prompt_attend -- causal attention over whole prompts of different lengths, packed
+ *
+ * Sequence s has query rows [cu_q[s], cu_q[s+1]) and key rows [cu_k[s], cu_k[s+1]) of packed tensors;
+ * its last query row sees all of its keys and each row before it one key less:
+ *     s_ij   = scale * <q_hi, k_gj>,  j in [0, nk - nq + i],  nq and nk the sequence's rows, g = h / G
+ *     out_hi = sum_j softmax_j(s_ij) v_gj,      lse_hi = log sum_j exp(s_ij)
+ * (with nk = nq plain causal attention, with nk > nq a prompt behind nk - nq cached rows).  A row that
+ * sees no key (nk < nq) gets out = 0 and lse = -inf.  Rows of q that belong to no sequence keep what out and
+ * lse held.
+ *     q, out   [n_q_heads][n_q_rows][head_dim], k, v [n_kv_heads][n_k_rows][head_dim]: by strides, elements
+ *              of a row contiguous (token-major tensors are addressed in place)
+ *     cu_q     [n_seq + 1] int32 in device memory, ascending, 0 <= cu_q[s] <= n_q_rows
+ *     cu_k     the same for the keys, or NULL for cu_q
+ *     lse      [n_q_heads][n_q_rows] fp32, may be NULL
+ * The lengths are read on the device, so a captured call follows them.  Boundaries outside [0, n_q_rows]
+ * or [0, n_k_rows] are moved into it and a descending pair counts as an empty sequence, so that nothing
+ * outside the tensors is read or written; sequences must not overlap in q.
+ * Arithmetic as in reform_chunk_attend_score, bitwise reproducible.
+ * Supported: REFORM_BF16 with head_dim 64 or 128; REFORM_F32 with head_dim % 4 == 0, <= 256; at most 65536
+ * sequences; n_q_heads * n_q_rows and n_kv_heads * n_k_rows below 2^30; row strides of k and v below 2^24.
+ * n_q_rows = 0 does nothing.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t  dtype;
+    int32_t  n_q_heads, n_kv_heads, head_dim;
+    int32_t  n_seq, n_q_rows, n_k_rows;
+    float    scale;                          /* > 0, finite                                    */
+    int32_t  reserved;                       /* 0                                              */
+    int64_t  q_head_stride, q_row_stride, k_head_stride, k_row_stride;   /* elements, multiples */
+    int64_t  v_head_stride, v_row_stride, o_head_stride, o_row_stride;   /* of 16 bytes         */
+} reform_prompt_desc;
+
+size_t reform_prompt_attend_workspace(const reform_prompt_desc *desc);
+
+reform_status reform_prompt_attend(const reform_prompt_desc *desc, const void *q, const void *k, const void *v,
+                                   const int32_t *cu_q, const int32_t *cu_k, void *out, float *lse,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------- */
+/* reform_tree_attend -- drafted tokens over a batch of caches
+ *
+ * Every sequence b of a batch has cached rows [0, L), L = cache_len[b], and behind them the rows of
+ * its n = node_count[b] <= n_nodes drafted tokens (the caller writes them there, see reform_rotary_embed).
+ * Node i sees all cached rows, itself and its ancestors:
+ *     s_ij   = scale * <q_bhi, k_bgj>,  j in [0, L) or j - L in { i, parent[i], parent[parent[i]], ... }
+ *     out, lse as in reform_chunk_attend_score
+ *     q, out     [n_seq][n_q_heads][n_nodes][head_dim] by strides
+ *     k, v       [n_seq][n_kv_heads][capacity][head_dim], rows contiguous, seq and head strides given
+ *     cache_len  [n_seq] int32 in device memory; values outside [0, max_cache_len] are moved into it
+ *     parent     [n_seq][n_nodes] int32 in device memory: a node before the node itself, or -1 (also for
+ *                anything else) for one without a parent; NULL: each node's parent is the one before it, so
+ *                that n_nodes = 1 is a generated token and NULL a short piece of text
+ *     node_count [n_seq] int32 in device memory or NULL (all have n_nodes); values outside [0, n_nodes] are
+ *                moved into it.  Rows of out and lse from node_count[b] on keep what they held.
+ *     lse        [n_seq][n_q_heads][n_nodes] fp32, may be NULL
+ * Supported: n_nodes in [1, 64]; types and head_dim as reform_prompt_attend; max_cache_len + n_nodes <=
+ * capacity; with B = ceil(n_nodes * G / 16), n_seq * n_kv_heads * B * ((max_cache_len + n_nodes) / 16 + 64) below 2^31.
+ * n_seq = 0 does nothing.
+ * The workspace takes partial results where long caches are shared out over workgroups.  Without it, or
+ * with less than the query asks for, the call returns REFORM_ERR_WORKSPACE.  Results depend on the batch
+ * that a sequence is computed in by rounding only (fp32 sums of the same terms in another order) and are
+ * bitwise reproducible for the same arguments.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t  dtype;
+    int32_t  n_seq, n_q_heads, n_kv_heads, head_dim;
+    int32_t  n_nodes, max_cache_len, capacity;
+    float    scale;                          /* > 0, finite                                    */
+    int64_t  q_seq_stride, q_head_stride, q_row_stride, o_seq_stride, o_head_stride, o_row_stride;
+    int64_t  kv_seq_stride, kv_head_stride;  /* elements, multiples of 16 bytes, as all strides */
+} reform_tree_desc;
+
+size_t reform_tree_attend_workspace(const reform_tree_desc *desc);
+
+reform_status reform_tree_attend(const reform_tree_desc *desc, const void *q, const void *k, const void *v,
+                                 const int32_t *cache_len, const int32_t *parent, const int32_t *node_count,
+                                 void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* reform_tree_accept -- the drafted tokens that the model agrees with stay in the caches
+ *
+ * Node 0 is the last token that is certain already.  From it the path goes down as long as a child's drafted
+ * token is the one the model chose after its parent (of several such children the first):
+ *     path_0 = 0,   path_{m+1} = min { c > path_m : parent[c] = path_m, drafted[c] = target[path_m] }
+ * Then row L + m of every cache becomes old row L + path_m, L = cache_len[b], m below the path's length, in
+ * place; rows behind keep their content.
+ *     parent, drafted, target  [n_seq][n_nodes] int32 in device memory; target[i]: the token the model chose
+ *                  after node i.  parent NULL: a chain
+ *     cache_len, node_count    as in reform_tree_attend; a sequence without nodes, or whose cache_len is
+ *                  outside [0, capacity - nodes], is left alone (accepted 0, next_token -1)
+ *     k, v         [n_layers] such caches, kv_layer_stride elements apart; both NULL: nothing moves
+ *     path         [n_seq][n_nodes] int32 out, -1 behind the path, may be NULL
+ *     accepted     [n_seq] int32 out: nodes on the path, may be NULL
+ *     next_token   [n_seq] int32 out: target of the path's last node, may be NULL
+ *     new_len      [n_seq] int32 out: cache_len + accepted, may be NULL; must not be cache_len itself
+ * Supported: n_nodes in [1, 64]; head_dim * sizeof(element) a multiple of 16, at most 4096 bytes;
+ * n_layers * n_seq * n_kv_heads below 2^30.  n_seq = 0 does nothing.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t  dtype;
+    int32_t  n_seq, n_kv_heads, head_dim;
+    int32_t  n_nodes, capacity, n_layers;
+    int64_t  kv_seq_stride, kv_head_stride, kv_layer_stride;   /* elements                     */
+} reform_accept_desc;
+
+reform_status reform_tree_accept(const reform_accept_desc *desc, const int32_t *parent, const int32_t *drafted,
+                                 const int32_t *target, const int32_t *cache_len, const int32_t *node_count,
+                                 void *k, void *v, int32_t *path, int32_t *accepted, int32_t *next_token,
+                                 int32_t *new_len, void *hip_stream);
 
 /* ------------------------------------------------------------------------------------------- */
 /* Measurement aids (no step of the method): what this machine sustains on the resources the

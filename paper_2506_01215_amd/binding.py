@@ -24,7 +24,10 @@ EXPORTED = [
     "reform_evict_topk_compact_static", "reform_debug_set_move_spin_limit",
     "reform_gather_topk_workspace", "reform_gather_topk", "reform_gather_similarity",
     "reform_gather_pooled_workspace", "reform_gather_pooled", "reform_embed_save_selected",
-    "reform_rerotate_keys", "reform_gather_rows", "reform_probe_mfma_bf16", "reform_probe_stream",
+    "reform_rerotate_keys", "reform_gather_rows", "reform_rotary_embed",
+    "reform_prompt_attend_workspace", "reform_prompt_attend",
+    "reform_tree_attend_workspace", "reform_tree_attend", "reform_tree_accept",
+    "reform_probe_mfma_bf16", "reform_probe_stream",
     "reform_status_string", "reform_version",
 ]
 
@@ -91,6 +94,46 @@ class RopeDesc(ctypes.Structure):
                 ("rotary_dim", ctypes.c_int32), ("theta", ctypes.c_float)]
 
 
+class RotaryDesc(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32),
+                 ("n_tokens", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                 ("rotary_dim", ctypes.c_int32), ("pairs", ctypes.c_int32),
+                 ("inverse", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                 ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                 ("turns_high", ctypes.c_double), ("turns_low", ctypes.c_double),
+                 ("original_len", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                 ("block_len", ctypes.c_int32), ("n_blocks", ctypes.c_int32),
+                 ("block_stride", ctypes.c_int64)]
+                + [(f"{t}_{u}_stride", ctypes.c_int64) for t in ("q", "k", "v", "q_out", "kv_out")
+                   for u in ("head", "row")])
+
+
+class PromptDesc(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32),
+                 ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                 ("n_seq", ctypes.c_int32), ("n_q_rows", ctypes.c_int32), ("n_k_rows", ctypes.c_int32),
+                 ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+                + [(f"{t}_{u}_stride", ctypes.c_int64) for t in "qkvo" for u in ("head", "row")])
+
+
+class TreeDesc(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("n_seq", ctypes.c_int32),
+                 ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                 ("n_nodes", ctypes.c_int32), ("max_cache_len", ctypes.c_int32), ("capacity", ctypes.c_int32),
+                 ("scale", ctypes.c_float)]
+                + [(f"{t}_{u}_stride", ctypes.c_int64) for t in "qo" for u in ("seq", "head", "row")]
+                + [("kv_seq_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64)])
+
+
+class AcceptDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("n_seq", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("n_nodes", ctypes.c_int32),
+                ("capacity", ctypes.c_int32), ("n_layers", ctypes.c_int32),
+                ("kv_seq_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64),
+                ("kv_layer_stride", ctypes.c_int64)]
+
+
 def library_path():
     return _LIB_PATH
 
@@ -133,6 +176,18 @@ def load_library():
     lib.reform_rerotate_keys.argtypes = [ctypes.POINTER(RopeDesc), vp, vp, vp]
     lib.reform_gather_rows.restype = ctypes.c_int
     lib.reform_gather_rows.argtypes = [ctypes.POINTER(RowsDesc), vp, vp, vp, vp, vp, vp]
+    lib.reform_rotary_embed.restype = ctypes.c_int
+    lib.reform_rotary_embed.argtypes = [ctypes.POINTER(RotaryDesc)] + [vp] * 9
+    lib.reform_prompt_attend_workspace.restype = sz
+    lib.reform_prompt_attend_workspace.argtypes = [ctypes.POINTER(PromptDesc)]
+    lib.reform_prompt_attend.restype = ctypes.c_int
+    lib.reform_prompt_attend.argtypes = [ctypes.POINTER(PromptDesc)] + [vp] * 8 + [sz, vp]
+    lib.reform_tree_attend_workspace.restype = sz
+    lib.reform_tree_attend_workspace.argtypes = [ctypes.POINTER(TreeDesc)]
+    lib.reform_tree_attend.restype = ctypes.c_int
+    lib.reform_tree_attend.argtypes = [ctypes.POINTER(TreeDesc)] + [vp] * 9 + [sz, vp]
+    lib.reform_tree_accept.restype = ctypes.c_int
+    lib.reform_tree_accept.argtypes = [ctypes.POINTER(AcceptDesc)] + [vp] * 12
     lib.reform_probe_mfma_bf16.restype = ctypes.c_int
     lib.reform_probe_mfma_bf16.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int32, vp]
     lib.reform_probe_stream.restype = ctypes.c_int
@@ -368,6 +423,177 @@ def reform_gather_rows(table, idx, count=None, out=None, err=None, stream=None):
                                 _ptr(err), _stream(stream))
     _check(rc, "reform_gather_rows")
     return out
+
+
+def _on_current_device(first, *others):
+    """The serving calls launch on the current device: every tensor has to be there (a host tensor's address would be
+    read by the GPU)."""
+    dev = first.get_device()
+    if dev < 0 or dev != torch.cuda.current_device() or any(t is not None and t.get_device() != dev for t in others):
+        raise ValueError("all tensors have to be on the current GPU")
+
+
+ROPE_SCALING = {None: 0, "none": 0, "linear": 1, "base": 2, "parts": 3, "bands": 4}
+
+
+def _i32(t, shape, what):
+    """The address of an int32 tensor of this shape; a missing one gives None."""
+    if t is None:
+        return None
+    assert t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == tuple(shape), what
+    return t.data_ptr()
+
+
+def reform_rotary_embed(q, k, v, pos, theta=10000.0, rotary_dim=None, interleaved=False, inverse=False,
+                        scaling=None, factor=1.0, original_len=0, turns_high=32.0, turns_low=1.0,
+                        magnitude=1.0, slot=None, q_out=None, k_out=None, v_out=None, stream=None):
+    """q [Hq, n, d], k, v [Hkv, n, d] (any strides with contiguous elements; q, or k and v, or v may be None),
+    pos [n] i32.  Queries and keys are rotated to their positions, values copied.  slot None: into q_out, k_out, v_out
+    like the inputs (made where missing; the inputs themselves rotate in place).  slot [n] i32: keys and values go to
+    caches k_out, v_out [Hkv, cap, d] or [blocks, Hkv, cap, d], row slot % cap of block slot // cap.
+    Returns (q_out, k_out, v_out)."""
+    lib = load_library()
+    if scaling not in ROPE_SCALING:
+        raise ValueError(f"scaling {scaling!r}: one of {list(ROPE_SCALING)}")
+    first = q if q is not None else k
+    assert first is not None and (v is None or k is not None)
+    n, d = first.shape[1:]
+    for t in (q, k, v):
+        assert t is None or (t.dim() == 3 and t.shape[1:] == (n, d) and t.stride(2) == 1 and t.dtype == first.dtype)
+    assert v is None or v.shape == k.shape
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if slot is None:
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        if v is not None and v_out is None:
+            v_out = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+    for t, o in ((q, q_out), (k, k_out), (v, v_out)):
+        assert (t is None) == (o is None), "an output without its input, or caches missing"
+        assert o is None or (o.dtype == first.dtype and o.stride(-1) == 1)
+        assert t is None or (o.shape == t.shape if slot is None or t is q else True)
+    block_len = n_blocks = block_stride = 0
+    kv_out = (0, 0)
+    if k is not None:
+        if slot is not None:
+            assert k_out.dim() in (3, 4) and k_out.shape[-3] == k.shape[0] and k_out.shape[-1] == d
+            block_len = k_out.shape[-2]
+            n_blocks, block_stride = (k_out.shape[0], k_out.stride(0)) if k_out.dim() == 4 else (1, 0)
+        assert v is None or (v_out.shape == k_out.shape and v_out.stride() == k_out.stride())
+        kv_out = k_out.stride()[-3:-1]
+    strides = []
+    for t in (q, k, v):
+        strides += (0, 0) if t is None else t.stride()[:2]
+    strides += (0, 0) if q is None else q_out.stride()[:2]
+    _on_current_device(first, q, k, v, pos, slot, q_out, k_out, v_out)
+    desc = RotaryDesc(ctypes.sizeof(RotaryDesc), _dtype_code(first), n, 0 if q is None else q.shape[0],
+                      0 if k is None else k.shape[0], d, d if rotary_dim is None else int(rotary_dim),
+                      int(bool(interleaved)), int(bool(inverse)), ROPE_SCALING[scaling], float(theta), float(factor),
+                      float(turns_high), float(turns_low), int(original_len), float(magnitude), block_len, n_blocks,
+                      block_stride, *strides, *kv_out)
+    rc = lib.reform_rotary_embed(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _i32(pos, (n,), "pos"),
+                                 _i32(slot, (n,), "slot"), _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(stream))
+    _check(rc, "reform_rotary_embed")
+    return q_out, k_out, v_out
+
+
+def prompt_desc(q, k, v, out, cu_q, scale):
+    Hq, nq, d = q.shape
+    Hkv, nk, d2 = k.shape
+    assert d2 == d and v.shape == k.shape and out.shape == q.shape
+    assert q.dtype == k.dtype == v.dtype == out.dtype
+    assert q.stride(2) == k.stride(2) == v.stride(2) == out.stride(2) == 1
+    return PromptDesc(ctypes.sizeof(PromptDesc), _dtype_code(q), Hq, Hkv, d, cu_q.shape[0] - 1, nq, nk, float(scale), 0,
+                      q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1),
+                      out.stride(0), out.stride(1))
+
+
+def reform_prompt_attend(q, k, v, cu_q, scale, cu_k=None, out=None, lse=None, workspace=None, stream=None):
+    """q [Hq, nq, d], k, v [Hkv, nk, d] packed sequences (any strides with contiguous elements), cu_q [n_seq + 1] i32
+    their boundaries, cu_k those of the keys (None: cu_q).  Causal attention inside every sequence, its last row seeing all of its
+    keys.  Returns (out, lse [Hq, nq])."""
+    lib = load_library()
+    if out is None:
+        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
+    assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2]
+    _on_current_device(q, k, v, cu_q, cu_k, out, lse, workspace)
+    desc = prompt_desc(q, k, v, out, cu_q, scale)
+    assert cu_k is not None or k.shape[1] == q.shape[1], "cu_k is needed where there are more or fewer key rows"
+    ws, ws_bytes = _workspace(lib.reform_prompt_attend_workspace, ctypes.byref(desc), q.device, workspace, stream)
+    rc = lib.reform_prompt_attend(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _i32(cu_q, cu_q.shape, "cu_q"),
+                                  _i32(cu_k, cu_q.shape, "cu_k"), _ptr(out), _ptr(lse), ws, ws_bytes, _stream(stream))
+    _check(rc, "reform_prompt_attend")
+    return out, lse
+
+
+def tree_desc(q, k, v, out, scale, max_cache_len=None):
+    S, Hq, T, d = q.shape
+    S2, Hkv, cap, d2 = k.shape
+    assert S2 == S and d2 == d and v.shape == k.shape and v.stride() == k.stride() and out.shape == q.shape
+    assert q.dtype == k.dtype == v.dtype == out.dtype
+    assert q.stride(3) == out.stride(3) == k.stride(3) == 1 and (cap == 1 or k.stride(2) == d)
+    return TreeDesc(ctypes.sizeof(TreeDesc), _dtype_code(q), S, Hq, Hkv, d, T,
+                    cap - T if max_cache_len is None else int(max_cache_len), cap, float(scale),
+                    *q.stride()[:3], *out.stride()[:3], *k.stride()[:2])
+
+
+def reform_tree_attend(q, k, v, cache_len, scale, parent=None, node_count=None, max_cache_len=None, out=None, lse=None,
+                       workspace=None, stream=None):
+    """q [S, Hq, T, d]: T drafted tokens of each of S sequences; k, v [S, Hkv, cap, d]: their caches, rows
+    [0, cache_len[b]) cached, the drafted tokens' rows behind them.  parent [S, T] i32 (None: a chain), node_count [S] i32
+    (None: T each).  max_cache_len bounds cache_len (None: cap - T).  Returns (out, lse [S, Hq, T])."""
+    lib = load_library()
+    S, Hq, T, d = q.shape
+    if out is None:
+        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.zeros(q.shape[:3], dtype=torch.float32, device=q.device)
+    assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:3]
+    _on_current_device(q, k, v, cache_len, parent, node_count, out, lse, workspace)
+    desc = tree_desc(q, k, v, out, scale, max_cache_len)
+    ws, ws_bytes = _workspace(lib.reform_tree_attend_workspace, ctypes.byref(desc), q.device, workspace, stream)
+    rc = lib.reform_tree_attend(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _i32(cache_len, (S,), "cache_len"),
+                                _i32(parent, (S, T), "parent"), _i32(node_count, (S,), "node_count"), _ptr(out), _ptr(lse),
+                                ws, ws_bytes, _stream(stream))
+    _check(rc, "reform_tree_attend")
+    return out, lse
+
+
+def reform_tree_accept(parent, drafted, target, cache_len, k=None, v=None, node_count=None, path=None, accepted=None,
+                       next_token=None, new_len=None, stream=None):
+    """parent (None: a chain), drafted, target [S, T] i32; k, v [S, Hkv, cap, d] or [layers, S, Hkv, cap, d] caches whose accepted
+    rows move together in place, or None.  Returns (path [S, T] i32, accepted [S], next_token [S], new_len [S])."""
+    lib = load_library()
+    S, T = drafted.shape
+    i32 = dict(dtype=torch.int32, device=drafted.device)
+    path = torch.empty((S, T), **i32) if path is None else path
+    accepted, next_token, new_len = (torch.empty((S,), **i32) if t is None else t for t in (accepted, next_token, new_len))
+    dtype, Hkv, cap, d, layers, strides = REFORM_F32, 1, (1 << 31) - 1, 4, 1, (0, 0, 0)
+    if k is not None:
+        assert k.dim() in (4, 5) and v.shape == k.shape and v.stride() == k.stride() and v.dtype == k.dtype
+        Hkv, cap, d = k.shape[-3:]
+        assert k.shape[-4] == S and k.stride(-1) == 1 and (cap == 1 or k.stride(-2) == d)
+        dtype, layers = _dtype_code(k), k.shape[0] if k.dim() == 5 else 1
+        strides = (k.stride(-4), k.stride(-3), k.stride(0) if k.dim() == 5 else 0)
+    _on_current_device(drafted, parent, target, cache_len, node_count, k, v, path, accepted, next_token, new_len)
+    desc = AcceptDesc(ctypes.sizeof(AcceptDesc), dtype, S, Hkv, d, T, cap, layers, *strides)
+    rc = lib.reform_tree_accept(ctypes.byref(desc), _i32(parent, (S, T), "parent"), _i32(drafted, (S, T), "drafted"),
+                                _i32(target, (S, T), "target"), _i32(cache_len, (S,), "cache_len"),
+                                _i32(node_count, (S,), "node_count"), _ptr(k), _ptr(v), _i32(path, (S, T), "path"),
+                                _i32(accepted, (S,), "accepted"), _i32(next_token, (S,), "next_token"),
+                                _i32(new_len, (S,), "new_len"), _stream(stream))
+    _check(rc, "reform_tree_accept")
+    return path, accepted, next_token, new_len
+
+
+def prompt_workspace_bytes(desc):
+    return load_library().reform_prompt_attend_workspace(ctypes.byref(desc))
+
+
+def tree_workspace_bytes(desc):
+    return load_library().reform_tree_attend_workspace(ctypes.byref(desc))
 
 
 def pooled_desc(emb, qry, budget, pool_window=129, n_head_keep=0, n_tail_keep=0, eps=1e-8):

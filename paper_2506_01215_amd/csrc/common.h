@@ -120,6 +120,64 @@ struct RopeParams {
     double neg2_log2_theta_over_rot;   // -2 log2(theta) / rot
 };
 
+constexpr int kRotaryMaxDim = 512;
+
+struct RotaryParams {
+    const void *src[3];      // q, k, v (v may be null)
+    void *dst[3];
+    const int32_t *pos, *slot;
+    long src_hs[3], src_rs[3], dst_hs[3], dst_rs[3];   // bytes
+    long block_bytes;        // slots: bytes between the blocks of k_out and v_out
+    int block_len;
+    unsigned n_slots;        // 0: no slots
+    int n, heads[3];         // tokens; heads of each part
+    int skip_rest[3];        // in place: what is not rotated is there already
+    int rot, elts;           // rotated elements, elements of a row
+    int inverse;
+    double neg2_log2_theta_over_rot;
+    double scale;            // REFORM_ROPE_LINEAR: 1 / factor, else 1
+    int ramp;                // 0 none, 1 over the pairs, 2 over the turns
+    double ramp_at, ramp_inv, ramp_low;   // r = clamp((x - ramp_at) * ramp_inv), f (1 - r (1 - ramp_low))
+    double turns;            // ramp 2: x = turns * quarters
+    float magnitude;
+};
+
+struct AcceptParams {
+    const int32_t *parent, *drafted, *target, *cache_len, *node_count;   // parent, node_count nullable
+    void *k, *v;
+    int32_t *path, *accepted, *next_token, *new_len;                     // nullable
+    int n_seq, n_kv, n_nodes, n_layers, capacity;
+    int row_bytes;
+    long seq_bytes, head_bytes, layer_bytes;
+};
+
+struct TreeParams {
+    const void *q, *k, *v;
+    void *out;
+    float *lse;              // nullable
+    const int32_t *cache_len, *parent, *node_count;      // the last two nullable
+    int n_seq, Hq, Hkv, G, D, T, max_len;
+    long q_ss, q_hs, q_rs, o_ss, o_hs, o_rs, kv_ss, kv_hs;   // elements
+    float scale;
+    int shares;              // workgroups over the list of all sequences' key tiles; 0: one per sequence, head and row block
+    int least;               // tiles that a share has at least, where there are fewer sequences and heads than shares
+    int row_blocks;          // of T * G rows
+    int part_rows;           // rows of one partial result
+    float *part_o;           // [2 * shares][part_rows][D] unnormalised outputs
+    float2 *part_ml;         // [2 * shares][part_rows] reference maximum (log2 units) and sum
+};
+
+struct PromptParams {
+    const void *q, *k, *v;
+    void *out;
+    float *lse;              // nullable
+    const int32_t *cu_q, *cu_k;
+    int Hq, Hkv, G, D, n_seq, n_q, n_k;
+    long q_hs, q_rs, k_hs, k_rs, v_hs, v_rs, o_hs, o_rs;     // elements
+    float scale;
+    int by_head;             // as in AttnParams
+};
+
 struct EmbedParams {
     const void *src;     // first token's head vector
     void *emb;           // embedding row of the first token

@@ -212,7 +212,7 @@ const char *reform_status_string(reform_status s)
     return "unknown status";
 }
 
-int32_t reform_version(void) { return 100; }
+int32_t reform_version(void) { return 200; }
 
 // ---------------------------------------------------------------------------------------
 static AttnParams attn_sizes(const reform_attn_desc *d)

@@ -1,0 +1,169 @@
+"""GPU: reform_prompt_attend against the 64-bit definition: packed sequences of any lengths, one token to long ones,
+keys before the first query row, rows that see nothing, odd heads, strides, values far apart."""
+import math
+import random
+
+import pytest
+import torch
+
+import serving_reference as ref
+from paper_2506_01215_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+KEPT = 5.0           # what rows of no sequence hold before and after
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def starts(lens):
+    got = [0]
+    for n in lens:
+        got.append(got[-1] + n)
+    return got
+
+
+def run_case(hq, hkv, d, q_lens, k_lens, dtype, seed, spare=0, layout="heads", sharp=1.0):
+    g = torch.Generator().manual_seed(seed)
+    nq, nk = sum(q_lens) + spare, sum(k_lens) + spare
+    q, k, v = ref.randn(g, hq, nq, d), ref.randn(g, hkv, nk, d), ref.randn(g, hkv, nk, d)
+    q, k, v = (q * sharp).to(dtype), k.to(dtype), v.to(dtype)
+    scale = d ** -0.5
+    print(f"[prompt] {hq}/{hkv} d={d} {dtype} q={q_lens[:8]} k={k_lens[:8]} spare={spare} {layout}", flush=True)
+    if layout == "tokens":       # token-major, as a projection leaves them, with room between the rows
+        put = lambda x: torch.cat([x, x], -1).transpose(0, 1).contiguous().to(DEV)[..., :d].transpose(0, 1)  # noqa: E731
+    else:
+        put = lambda x: x.to(DEV)  # noqa: E731
+    qd, kd, vd = put(q), put(k), put(v)
+    out = torch.full((nq, hq, d), KEPT, dtype=dtype, device=DEV).transpose(0, 1) if layout == "tokens" \
+        else torch.full((hq, nq, d), KEPT, dtype=dtype, device=DEV)
+    lse = torch.full((hq, nq), KEPT, device=DEV)
+    same = list(q_lens) == list(k_lens)
+    got, got_lse = binding.reform_prompt_attend(qd, kd, vd, i32(starts(q_lens)), scale, cu_k=None if same else i32(starts(k_lens)),
+                                                out=out, lse=lse)
+    want, want_lse, a, err = ref.prompt_attend(q, k, v, q_lens, k_lens, scale)
+    rows = sum(q_lens)
+    ref.check_attention(got[:, :rows], got_lse[:, :rows], want[:, :rows], want_lse[:, :rows], a[:, :rows], err[:, :rows],
+                        max(k_lens), dtype, "prompt")
+    if spare:
+        assert bool((got[:, rows:] == KEPT).all()) and bool((got_lse[:, rows:] == KEPT).all())
+    return got, got_lse
+
+
+BF, F = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("hq,hkv,d,q_lens,dtype", [
+    (1, 1, 64, [1], BF), (4, 4, 128, [1, 1, 1], BF), (8, 2, 64, [0, 5, 0, 1, 64, 0], BF),
+    (8, 2, 128, [33, 31, 32, 64, 65, 63, 7], BF), (32, 8, 128, [130], BF), (14, 2, 64, [257, 3, 100], BF),
+    (3, 1, 128, [300, 1, 77], BF), (24, 8, 64, [129, 64, 200], BF), (5, 5, 128, [500], BF), (16, 1, 64, [90, 91], BF),
+    (1, 1, 64, [1], F), (4, 4, 64, [128, 301, 256], F), (6, 2, 128, [17, 0, 90], F), (2, 1, 256, [40, 3], F), (8, 2, 36, [50, 16], F),
+    (3, 3, 100, [33], F), (4, 1, 4, [20], F), (2, 2, 200, [65], F),
+])
+def test_prompts(hq, hkv, d, q_lens, dtype):
+    run_case(hq, hkv, d, q_lens, q_lens, dtype, seed=sum(q_lens) + d)
+
+
+@pytest.mark.parametrize("hq,hkv,d,q_lens,k_lens,dtype", [
+    (8, 2, 128, [1, 40, 64, 7], [300, 41, 64, 500], BF),
+    (4, 2, 64, [100, 3], [164, 1000], BF),
+    (8, 2, 128, [20, 70, 5, 30], [0, 30, 5, 1], BF),         # fewer keys than rows: the first rows see nothing
+    (8, 4, 64, [300], [200], BF),
+    (4, 2, 64, [20, 70, 5], [0, 30, 50], F),
+    (2, 1, 96, [9, 1], [300, 77], F),
+])
+def test_keys_before_and_rows_without_keys(hq, hkv, d, q_lens, k_lens, dtype):
+    run_case(hq, hkv, d, q_lens, k_lens, dtype, seed=d, spare=11)
+
+
+@pytest.mark.parametrize("rows", ["short", "narrow", "wide"])
+@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 128), (6, 2, 64), (7, 1, 128), (2, 2, 64)])
+def test_every_form(rows, hq, hkv, d):
+    """Batches large enough for the blocks of 128 and 256 rows, ragged ends of all kinds; few heads, so that the
+    reference stays quick.  The form follows the number of rows: many short sequences take the last one."""
+    unit = {"short": 900, "narrow": 9000, "wide": 36000}[rows] // hq
+    lens, left, rnd = [], unit, random.Random(unit + d)
+    while left > 0:
+        n = min(left, rnd.choice([1, 7, 64, 65, 128, 257, 600, 777]))
+        lens.append(n)
+        left -= n
+    run_case(hq, hkv, d, lens, lens, BF, seed=unit, spare=3)
+    if rows != "short":
+        run_case(hq, hkv, d, [unit // 8, 1], [unit // 8 + 130, 70], BF, seed=unit)
+
+
+def test_token_major_strides():
+    run_case(8, 2, 128, [65, 3, 200], [65, 3, 200], BF, seed=1, layout="tokens")
+    run_case(4, 1, 64, [1300, 1200], [1300, 1200], BF, seed=1, layout="tokens", spare=2)
+    run_case(4, 2, 64, [65, 3], [65, 30], F, seed=2, layout="tokens", spare=5)
+
+
+def test_sharp_logits_rescale():
+    """Logits of some hundred: the reference maximum is outgrown again and again."""
+    run_case(4, 2, 128, [400, 90], [400, 90], BF, seed=3, sharp=12.0)
+    run_case(2, 1, 64, [3000], [3000], BF, seed=3, sharp=20.0)
+    run_case(2, 1, 64, [300], [300], F, seed=3, sharp=12.0)
+
+
+def test_more_sequences_than_a_wave_has_lanes():
+    lens = [(i * 7) % 23 for i in range(150)]
+    run_case(4, 2, 64, lens, lens, BF, seed=6)
+    run_case(2, 1, 64, lens[:70], [n + 5 for n in lens[:70]], F, seed=6)
+
+
+def test_boundaries_outside_are_moved_in():
+    """Device-side boundaries that point outside the tensors, descend or overlap in the keys: nothing outside is
+    touched, and what they mean after being moved in is computed."""
+    g = torch.Generator().manual_seed(4)
+    q, k, v = (ref.randn(g, 2, 100, 64, dtype=BF) for _ in range(3))
+    cu = [-7, 30, 30, 20, 60, 1 << 30]
+    out, lse = binding.reform_prompt_attend(q.to(DEV), k.to(DEV), v.to(DEV), i32(cu), 0.125, out=torch.full((2, 100, 64), KEPT, dtype=BF, device=DEV))
+    # the sequences that remain: [0, 30), [20, 60), [60, 100); rows 20..30 belong to two of them, either result stands
+    for lo, hi, own in ((0, 30, slice(0, 20)), (20, 60, slice(10, 40)), (60, 100, slice(0, 40))):
+        want, wl, a, err = ref.prompt_attend(q[:, lo:hi], k[:, lo:hi], v[:, lo:hi], [hi - lo], [hi - lo], 0.125)
+        ref.check_attention(out[:, lo:hi][:, own], lse[:, lo:hi][:, own], want[:, own], wl[:, own], a[:, own], err[:, own], 64, BF, f"{lo}")
+
+
+def test_infinite_and_nan_keys_stay_in_their_sequence():
+    """A sequence with broken values leaves its neighbours' results as they are, and so do rows of no sequence."""
+    g = torch.Generator().manual_seed(12)
+    lens = [40, 50, 64, 33]
+    n = sum(lens) + 20
+    for dtype in (BF, F):
+        q, k, v = (ref.randn(g, 4, n, 64, dtype=dtype).to(DEV) for _ in range(3))
+        cu = i32(starts(lens))
+        clean = binding.reform_prompt_attend(q, k, v, cu, 0.125)
+        k[:, 60], v[:, 61], q[:, 62] = math.nan, math.inf, math.nan
+        k[:, sum(lens):], v[:, sum(lens):] = math.nan, math.nan
+        dirty = binding.reform_prompt_attend(q, k, v, cu, 0.125)
+        for x, y in zip(clean, dirty):
+            assert torch.equal(x[:, :40], y[:, :40]) and torch.equal(x[:, 90:sum(lens)], y[:, 90:sum(lens)])
+        assert bool(torch.isnan(dirty[0][:, 62]).all())
+
+
+def test_same_results_as_the_single_sequence_call():
+    """One sequence without a cache is what reform_chunk_attend_score computes; both round within the same bounds."""
+    g = torch.Generator().manual_seed(2)
+    q, k, v = ref.randn(g, 8, 700, 128, dtype=BF).to(DEV), ref.randn(g, 2, 700, 128, dtype=BF).to(DEV), ref.randn(g, 2, 700, 128, dtype=BF).to(DEV)
+    out, lse = binding.reform_prompt_attend(q, k, v, i32([0, 700]), 128 ** -0.5)
+    other, other_lse, _ = binding.reform_chunk_attend_score(q, k, v, 0, 128 ** -0.5, want_score=False)
+    want, wl, a, err = ref.prompt_attend(q.cpu(), k.cpu(), v.cpu(), [700], [700], 128 ** -0.5)
+    for o, e in ((out, lse), (other, other_lse)):
+        ref.check_attention(o, e, want, wl, a, err, 700, BF)
+
+
+def test_runs_are_bitwise_alike_and_lse_may_be_missing():
+    import ctypes
+    g = torch.Generator().manual_seed(21)
+    q, k, v = ref.randn(g, 8, 3000, 64, dtype=BF).to(DEV), ref.randn(g, 2, 3000, 64, dtype=BF).to(DEV), ref.randn(g, 2, 3000, 64, dtype=BF).to(DEV)
+    cu = i32([0, 1000, 1001, 2900])
+    first = binding.reform_prompt_attend(q, k, v, cu, 0.125)
+    again = binding.reform_prompt_attend(q, k, v, cu, 0.125)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    out = torch.zeros_like(q)
+    desc = binding.prompt_desc(q, k, v, out, cu, 0.125)
+    rc = binding.load_library().reform_prompt_attend(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), cu.data_ptr(), None,
+                                                     out.data_ptr(), None, None, 0, torch.cuda.current_stream().cuda_stream)
+    assert rc == 0 and torch.equal(out, first[0])
