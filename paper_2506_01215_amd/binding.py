@@ -5,7 +5,9 @@ every step of the path runs in the library's kernels.  There is no fallback: if 
 library is missing or a call returns a non-OK status, a ReformError is raised.
 """
 import ctypes
+import functools
 import os
+import struct
 
 import torch
 
@@ -177,17 +179,17 @@ def load_library():
     lib.reform_gather_rows.restype = ctypes.c_int
     lib.reform_gather_rows.argtypes = [ctypes.POINTER(RowsDesc), vp, vp, vp, vp, vp, vp]
     lib.reform_rotary_embed.restype = ctypes.c_int
-    lib.reform_rotary_embed.argtypes = [ctypes.POINTER(RotaryDesc)] + [vp] * 9
+    lib.reform_rotary_embed.argtypes = [vp] * 10        # descriptors packed or as structures
     lib.reform_prompt_attend_workspace.restype = sz
-    lib.reform_prompt_attend_workspace.argtypes = [ctypes.POINTER(PromptDesc)]
+    lib.reform_prompt_attend_workspace.argtypes = [vp]
     lib.reform_prompt_attend.restype = ctypes.c_int
-    lib.reform_prompt_attend.argtypes = [ctypes.POINTER(PromptDesc)] + [vp] * 8 + [sz, vp]
+    lib.reform_prompt_attend.argtypes = [vp] * 9 + [sz, vp]
     lib.reform_tree_attend_workspace.restype = sz
-    lib.reform_tree_attend_workspace.argtypes = [ctypes.POINTER(TreeDesc)]
+    lib.reform_tree_attend_workspace.argtypes = [vp]
     lib.reform_tree_attend.restype = ctypes.c_int
-    lib.reform_tree_attend.argtypes = [ctypes.POINTER(TreeDesc)] + [vp] * 9 + [sz, vp]
+    lib.reform_tree_attend.argtypes = [vp] * 10 + [sz, vp]
     lib.reform_tree_accept.restype = ctypes.c_int
-    lib.reform_tree_accept.argtypes = [ctypes.POINTER(AcceptDesc)] + [vp] * 12
+    lib.reform_tree_accept.argtypes = [vp] * 13
     lib.reform_probe_mfma_bf16.restype = ctypes.c_int
     lib.reform_probe_mfma_bf16.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int32, vp]
     lib.reform_probe_stream.restype = ctypes.c_int
@@ -425,23 +427,54 @@ def reform_gather_rows(table, idx, count=None, out=None, err=None, stream=None):
     return out
 
 
-def _on_current_device(first, *others):
-    """The serving calls launch on the current device: every tensor has to be there (a host tensor's address would be
-    read by the GPU)."""
-    dev = first.get_device()
-    if dev < 0 or dev != torch.cuda.current_device() or any(t is not None and t.get_device() != dev for t in others):
+# The serving calls are made once per layer and generated token, so their descriptors are packed by `struct` (a ctypes
+# structure takes 2 us to fill), in the layout that the classes above declare, and tensors are checked with as few calls as will do.
+_CODES = {ctypes.c_uint32: "I", ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_float: "f", ctypes.c_double: "d"}
+
+
+def _packer(cls):
+    packer = struct.Struct("@" + "".join(_CODES[t] for _, t in cls._fields_))
+    assert packer.size == ctypes.sizeof(cls)
+    return functools.partial(packer.pack, ctypes.sizeof(cls))
+
+
+_pack_rotary, _pack_prompt, _pack_tree, _pack_accept = map(_packer, (RotaryDesc, PromptDesc, TreeDesc, AcceptDesc))
+_DTYPES = {torch.float32: REFORM_F32, torch.bfloat16: REFORM_BF16}
+_I32 = torch.int32
+
+
+def _gpu(t):
+    """The current device's index if t is there: calls launch on it, and a host tensor's address would be read by the GPU."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError("all tensors have to be on the current GPU")
+    return dev
+
+
+def _at(t, dev):
+    """Address of a tensor that has to be on the device `dev`, or None."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise ValueError("all tensors have to be on the current GPU")
+    return t.data_ptr()
+
+
+def _i32(t, n, dev, what):
+    """Address of n contiguous int32 on the device, or None."""
+    if t is None:
+        return None
+    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous int32 expected")
+    return _at(t, dev)
+
+
+def _require(ok, what):
+    if not ok:
+        raise ValueError(what)
 
 
 ROPE_SCALING = {None: 0, "none": 0, "linear": 1, "base": 2, "parts": 3, "bands": 4}
-
-
-def _i32(t, shape, what):
-    """The address of an int32 tensor of this shape; a missing one gives None."""
-    if t is None:
-        return None
-    assert t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == tuple(shape), what
-    return t.data_ptr()
 
 
 def reform_rotary_embed(q, k, v, pos, theta=10000.0, rotary_dim=None, interleaved=False, inverse=False,
@@ -453,59 +486,70 @@ def reform_rotary_embed(q, k, v, pos, theta=10000.0, rotary_dim=None, interleave
     caches k_out, v_out [Hkv, cap, d] or [blocks, Hkv, cap, d], row slot % cap of block slot // cap.
     Returns (q_out, k_out, v_out)."""
     lib = load_library()
-    if scaling not in ROPE_SCALING:
-        raise ValueError(f"scaling {scaling!r}: one of {list(ROPE_SCALING)}")
-    first = q if q is not None else k
-    assert first is not None and (v is None or k is not None)
-    n, d = first.shape[1:]
-    for t in (q, k, v):
-        assert t is None or (t.dim() == 3 and t.shape[1:] == (n, d) and t.stride(2) == 1 and t.dtype == first.dtype)
-    assert v is None or v.shape == k.shape
-    if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if slot is None:
-        if k is not None and k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        if v is not None and v_out is None:
-            v_out = torch.empty(v.shape, dtype=v.dtype, device=v.device)
-    for t, o in ((q, q_out), (k, k_out), (v, v_out)):
-        assert (t is None) == (o is None), "an output without its input, or caches missing"
-        assert o is None or (o.dtype == first.dtype and o.stride(-1) == 1)
-        assert t is None or (o.shape == t.shape if slot is None or t is q else True)
-    block_len = n_blocks = block_stride = 0
-    kv_out = (0, 0)
+    mode = ROPE_SCALING.get(scaling)
+    _require(mode is not None, f"scaling {scaling!r}: one of {list(ROPE_SCALING)}")
+    first = k if q is None else q
+    _require(first is not None and (v is None or k is not None), "queries, or keys with or without values")
+    dtype = first.dtype
+    _, n, d = first.shape
+    hq = hkv = block_len = n_blocks = block_stride = 0
+    qs = ks = vs = qos = kvos = (0, 0, 1)
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        hq = q.shape[0]
+        qs, qos = q.stride(), q_out.stride()
+        _require(q_out.shape == q.shape and q_out.dtype is dtype and qs[2] == qos[2] == 1, "q_out: like q, elements of a row contiguous")
+    else:
+        _require(q_out is None, "q_out without q")
     if k is not None:
-        if slot is not None:
-            assert k_out.dim() in (3, 4) and k_out.shape[-3] == k.shape[0] and k_out.shape[-1] == d
-            block_len = k_out.shape[-2]
-            n_blocks, block_stride = (k_out.shape[0], k_out.stride(0)) if k_out.dim() == 4 else (1, 0)
-        assert v is None or (v_out.shape == k_out.shape and v_out.stride() == k_out.stride())
-        kv_out = k_out.stride()[-3:-1]
-    strides = []
-    for t in (q, k, v):
-        strides += (0, 0) if t is None else t.stride()[:2]
-    strides += (0, 0) if q is None else q_out.stride()[:2]
-    _on_current_device(first, q, k, v, pos, slot, q_out, k_out, v_out)
-    desc = RotaryDesc(ctypes.sizeof(RotaryDesc), _dtype_code(first), n, 0 if q is None else q.shape[0],
-                      0 if k is None else k.shape[0], d, d if rotary_dim is None else int(rotary_dim),
-                      int(bool(interleaved)), int(bool(inverse)), ROPE_SCALING[scaling], float(theta), float(factor),
-                      float(turns_high), float(turns_low), int(original_len), float(magnitude), block_len, n_blocks,
-                      block_stride, *strides, *kv_out)
-    rc = lib.reform_rotary_embed(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _i32(pos, (n,), "pos"),
-                                 _i32(slot, (n,), "slot"), _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(stream))
+        hkv, nk, dk = k.shape
+        _require(nk == n and dk == d and k.dtype is dtype, "k: as many rows and elements as q, same type")
+        if slot is None:
+            if k_out is None:
+                k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
+            if v_out is None and v is not None:
+                v_out = torch.empty(v.shape, dtype=dtype, device=v.device)
+            _require(k_out.shape == k.shape, "k_out: like k")
+        else:
+            _require(k_out is not None and k_out.dim() in (3, 4), "slots need caches [heads, rows, d] or [blocks, heads, rows, d]")
+            shape = k_out.shape
+            _require(shape[-3] == hkv and shape[-1] == d, "caches with other heads or elements than k")
+            block_len = shape[-2]
+            n_blocks, block_stride = (shape[0], k_out.stride(0)) if len(shape) == 4 else (1, 0)
+        ks, kvos = k.stride(), k_out.stride()[-3:]
+        _require(k_out.dtype is dtype and ks[2] == kvos[2] == 1, "k_out: k's type, elements of a row contiguous")
+    else:
+        _require(k_out is None, "k_out without k")
+    if v is not None:
+        vs = v.stride()
+        _require(v.shape == k.shape and v.dtype is dtype and vs[2] == 1 and v_out is not None, "v: like k, and a v_out")
+        _require(v_out.shape == k_out.shape and v_out.stride() == k_out.stride() and v_out.dtype is dtype, "v_out: like k_out")
+    else:
+        _require(v_out is None, "v_out without v")
+    desc = _pack_rotary(_DTYPES[dtype], n, hq, hkv, d, d if rotary_dim is None else rotary_dim, 1 if interleaved else 0,
+                        1 if inverse else 0, mode, theta, factor, turns_high, turns_low, original_len, magnitude, block_len,
+                        n_blocks, block_stride, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], qos[0], qos[1], kvos[0], kvos[1])
+    dev = _gpu(first)
+    rc = lib.reform_rotary_embed(desc, _at(q, dev), _at(k, dev), _at(v, dev), _i32(pos, n, dev, "pos"), _i32(slot, n, dev, "slot"),
+                                 _at(q_out, dev), _at(k_out, dev), _at(v_out, dev), _stream(stream))
     _check(rc, "reform_rotary_embed")
     return q_out, k_out, v_out
 
 
-def prompt_desc(q, k, v, out, cu_q, scale):
+def _prompt_fields(q, k, v, out, n_seq, scale):
     Hq, nq, d = q.shape
-    Hkv, nk, d2 = k.shape
-    assert d2 == d and v.shape == k.shape and out.shape == q.shape
-    assert q.dtype == k.dtype == v.dtype == out.dtype
-    assert q.stride(2) == k.stride(2) == v.stride(2) == out.stride(2) == 1
-    return PromptDesc(ctypes.sizeof(PromptDesc), _dtype_code(q), Hq, Hkv, d, cu_q.shape[0] - 1, nq, nk, float(scale), 0,
-                      q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1),
-                      out.stride(0), out.stride(1))
+    Hkv, nk, dk = k.shape
+    dtype = q.dtype
+    qs, ks, vs, os = q.stride(), k.stride(), v.stride(), out.stride()
+    _require(dk == d and v.shape == k.shape and out.shape == q.shape, "shapes of q, k, v and out")
+    _require(k.dtype is dtype and v.dtype is dtype and out.dtype is dtype, "types of q, k, v and out")
+    _require(qs[2] == ks[2] == vs[2] == os[2] == 1, "elements of a row have to be contiguous")
+    return (_DTYPES[dtype], Hq, Hkv, d, n_seq, nq, nk, scale, 0, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os[0], os[1])
+
+
+def prompt_desc(q, k, v, out, cu_q, scale):
+    return PromptDesc(ctypes.sizeof(PromptDesc), *_prompt_fields(q, k, v, out, cu_q.shape[0] - 1, scale))
 
 
 def reform_prompt_attend(q, k, v, cu_q, scale, cu_k=None, out=None, lse=None, workspace=None, stream=None):
@@ -517,26 +561,33 @@ def reform_prompt_attend(q, k, v, cu_q, scale, cu_k=None, out=None, lse=None, wo
         out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
     if lse is None:
         lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
-    assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2]
-    _on_current_device(q, k, v, cu_q, cu_k, out, lse, workspace)
-    desc = prompt_desc(q, k, v, out, cu_q, scale)
-    assert cu_k is not None or k.shape[1] == q.shape[1], "cu_k is needed where there are more or fewer key rows"
-    ws, ws_bytes = _workspace(lib.reform_prompt_attend_workspace, ctypes.byref(desc), q.device, workspace, stream)
-    rc = lib.reform_prompt_attend(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _i32(cu_q, cu_q.shape, "cu_q"),
-                                  _i32(cu_k, cu_q.shape, "cu_k"), _ptr(out), _ptr(lse), ws, ws_bytes, _stream(stream))
+    n = cu_q.numel()
+    fields = _prompt_fields(q, k, v, out, n - 1, scale)
+    _require(n >= 1 and (cu_k is not None or fields[6] == fields[5]), "cu_k is needed where there are more or fewer key rows")
+    _require(lse.dtype is torch.float32 and lse.is_contiguous() and lse.numel() == fields[1] * fields[5], "lse: [heads, rows] fp32")
+    dev = _gpu(q)
+    desc = _pack_prompt(*fields)
+    ws, ws_bytes = _workspace(lib.reform_prompt_attend_workspace, desc, q.device, workspace, stream)
+    rc = lib.reform_prompt_attend(desc, q.data_ptr(), _at(k, dev), _at(v, dev), _i32(cu_q, n, dev, "cu_q"),
+                                  _i32(cu_k, n, dev, "cu_k"), _at(out, dev), _at(lse, dev), ws, ws_bytes, _stream(stream))
     _check(rc, "reform_prompt_attend")
     return out, lse
 
 
-def tree_desc(q, k, v, out, scale, max_cache_len=None):
+def _tree_fields(q, k, v, out, scale, max_cache_len):
     S, Hq, T, d = q.shape
-    S2, Hkv, cap, d2 = k.shape
-    assert S2 == S and d2 == d and v.shape == k.shape and v.stride() == k.stride() and out.shape == q.shape
-    assert q.dtype == k.dtype == v.dtype == out.dtype
-    assert q.stride(3) == out.stride(3) == k.stride(3) == 1 and (cap == 1 or k.stride(2) == d)
-    return TreeDesc(ctypes.sizeof(TreeDesc), _dtype_code(q), S, Hq, Hkv, d, T,
-                    cap - T if max_cache_len is None else int(max_cache_len), cap, float(scale),
-                    *q.stride()[:3], *out.stride()[:3], *k.stride()[:2])
+    Sk, Hkv, cap, dk = k.shape
+    dtype = q.dtype
+    qs, ks, os = q.stride(), k.stride(), out.stride()
+    _require(Sk == S and dk == d and v.shape == k.shape and v.stride() == ks and out.shape == q.shape, "shapes of q, k, v and out")
+    _require(k.dtype is dtype and v.dtype is dtype and out.dtype is dtype, "types of q, k, v and out")
+    _require(qs[3] == os[3] == ks[3] == 1 and (ks[2] == d or cap == 1), "contiguous elements, and rows of the caches")
+    return (_DTYPES[dtype], S, Hq, Hkv, d, T, cap - T if max_cache_len is None else max_cache_len, cap, scale,
+            qs[0], qs[1], qs[2], os[0], os[1], os[2], ks[0], ks[1])
+
+
+def tree_desc(q, k, v, out, scale, max_cache_len=None):
+    return TreeDesc(ctypes.sizeof(TreeDesc), *_tree_fields(q, k, v, out, scale, max_cache_len))
 
 
 def reform_tree_attend(q, k, v, cache_len, scale, parent=None, node_count=None, max_cache_len=None, out=None, lse=None,
@@ -545,18 +596,19 @@ def reform_tree_attend(q, k, v, cache_len, scale, parent=None, node_count=None, 
     [0, cache_len[b]) cached, the drafted tokens' rows behind them.  parent [S, T] i32 (None: a chain), node_count [S] i32
     (None: T each).  max_cache_len bounds cache_len (None: cap - T).  Returns (out, lse [S, Hq, T])."""
     lib = load_library()
-    S, Hq, T, d = q.shape
     if out is None:
         out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
     if lse is None:
         lse = torch.zeros(q.shape[:3], dtype=torch.float32, device=q.device)
-    assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:3]
-    _on_current_device(q, k, v, cache_len, parent, node_count, out, lse, workspace)
-    desc = tree_desc(q, k, v, out, scale, max_cache_len)
-    ws, ws_bytes = _workspace(lib.reform_tree_attend_workspace, ctypes.byref(desc), q.device, workspace, stream)
-    rc = lib.reform_tree_attend(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _i32(cache_len, (S,), "cache_len"),
-                                _i32(parent, (S, T), "parent"), _i32(node_count, (S,), "node_count"), _ptr(out), _ptr(lse),
-                                ws, ws_bytes, _stream(stream))
+    fields = _tree_fields(q, k, v, out, scale, max_cache_len)
+    S, T = fields[1], fields[5]
+    _require(lse.dtype is torch.float32 and lse.is_contiguous() and lse.numel() == S * fields[2] * T, "lse: [sequences, heads, nodes] fp32")
+    dev = _gpu(q)
+    desc = _pack_tree(*fields)
+    ws, ws_bytes = _workspace(lib.reform_tree_attend_workspace, desc, q.device, workspace, stream)
+    rc = lib.reform_tree_attend(desc, q.data_ptr(), _at(k, dev), _at(v, dev), _i32(cache_len, S, dev, "cache_len"),
+                                _i32(parent, S * T, dev, "parent"), _i32(node_count, S, dev, "node_count"), _at(out, dev),
+                                _at(lse, dev), ws, ws_bytes, _stream(stream))
     _check(rc, "reform_tree_attend")
     return out, lse
 
@@ -567,23 +619,27 @@ def reform_tree_accept(parent, drafted, target, cache_len, k=None, v=None, node_
     rows move together in place, or None.  Returns (path [S, T] i32, accepted [S], next_token [S], new_len [S])."""
     lib = load_library()
     S, T = drafted.shape
-    i32 = dict(dtype=torch.int32, device=drafted.device)
-    path = torch.empty((S, T), **i32) if path is None else path
-    accepted, next_token, new_len = (torch.empty((S,), **i32) if t is None else t for t in (accepted, next_token, new_len))
+    if path is None or accepted is None or next_token is None or new_len is None:
+        i32 = dict(dtype=_I32, device=drafted.device)
+        path = torch.empty((S, T), **i32) if path is None else path
+        accepted, next_token, new_len = (torch.empty((S,), **i32) if t is None else t for t in (accepted, next_token, new_len))
     dtype, Hkv, cap, d, layers, strides = REFORM_F32, 1, (1 << 31) - 1, 4, 1, (0, 0, 0)
     if k is not None:
-        assert k.dim() in (4, 5) and v.shape == k.shape and v.stride() == k.stride() and v.dtype == k.dtype
-        Hkv, cap, d = k.shape[-3:]
-        assert k.shape[-4] == S and k.stride(-1) == 1 and (cap == 1 or k.stride(-2) == d)
-        dtype, layers = _dtype_code(k), k.shape[0] if k.dim() == 5 else 1
-        strides = (k.stride(-4), k.stride(-3), k.stride(0) if k.dim() == 5 else 0)
-    _on_current_device(drafted, parent, target, cache_len, node_count, k, v, path, accepted, next_token, new_len)
-    desc = AcceptDesc(ctypes.sizeof(AcceptDesc), dtype, S, Hkv, d, T, cap, layers, *strides)
-    rc = lib.reform_tree_accept(ctypes.byref(desc), _i32(parent, (S, T), "parent"), _i32(drafted, (S, T), "drafted"),
-                                _i32(target, (S, T), "target"), _i32(cache_len, (S,), "cache_len"),
-                                _i32(node_count, (S,), "node_count"), _ptr(k), _ptr(v), _i32(path, (S, T), "path"),
-                                _i32(accepted, (S,), "accepted"), _i32(next_token, (S,), "next_token"),
-                                _i32(new_len, (S,), "new_len"), _stream(stream))
+        shape, ks = k.shape, k.stride()
+        _require(len(shape) in (4, 5) and v is not None and v.shape == shape and v.stride() == ks and v.dtype is k.dtype, "k and v: alike, 4 or 5 dimensions")
+        Hkv, cap, d = shape[-3:]
+        _require(shape[-4] == S and ks[-1] == 1 and (ks[-2] == d or cap == 1), "caches of other sequences, or rows not contiguous")
+        dtype = _DTYPES[k.dtype]
+        layers, strides = (shape[0], (ks[1], ks[2], ks[0])) if len(shape) == 5 else (1, (ks[0], ks[1], 0))
+    else:
+        _require(v is None, "v without k")
+    dev = _gpu(drafted)
+    n = S * T
+    rc = lib.reform_tree_accept(_pack_accept(dtype, S, Hkv, d, T, cap, layers, *strides), _i32(parent, n, dev, "parent"),
+                                _i32(drafted, n, dev, "drafted"), _i32(target, n, dev, "target"), _i32(cache_len, S, dev, "cache_len"),
+                                _i32(node_count, S, dev, "node_count"), _at(k, dev), _at(v, dev), _i32(path, n, dev, "path"),
+                                _i32(accepted, S, dev, "accepted"), _i32(next_token, S, dev, "next_token"),
+                                _i32(new_len, S, dev, "new_len"), _stream(stream))
     _check(rc, "reform_tree_accept")
     return path, accepted, next_token, new_len
 

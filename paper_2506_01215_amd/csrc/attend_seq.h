@@ -67,40 +67,38 @@ __device__ __forceinline__ unsigned long long tree_line(const int *parent, int n
     return ((unsigned long long)hi << 32) | lo;
 }
 
-constexpr int kSeqWaves = 8;
-
-// RG waves side by side take RG * 16 NB rows; the KG = 8 / RG groups of them divide the key tiles of TK
-// keys.  RG = 1: a wave's tiles are its own, no barrier in the loop.
-template <int D, int NB, int RG>
+// NW waves of 16 NB rows, all the same ones; each takes every NW-th tile of 32 keys, through LDS of its own, without a
+// barrier before the sums meet.
+template <int D, int NB, int NW>
 struct SeqShape {
-    static constexpr int KG = kSeqWaves / RG, R = 16 * NB * RG, TK = RG == 8 ? 64 : 32, SUB = TK / 32;
-    static constexpr int C8 = D / 8, ROW = D + 16, TILE = TK * ROW, GT = 64 * RG;
-    static constexpr int PIECES = TK * C8 / GT, BUFS = RG == 1 ? 1 : 2;
-    static constexpr int SL = KG > 1 ? KG / 2 : 1, OROW = D + 4;
-    static constexpr size_t stage_bytes = sizeof(u16) * (size_t)BUFS * KG * 2 * TILE;
+    static constexpr int R = 16 * NB, TK = 32;
+    static constexpr int C8 = D / 8, ROW = D + 16, TILE = TK * ROW;
+    static constexpr int PIECES = TK * C8 / 64;
+    static constexpr int SL = NW / 2, OROW = D + 4;
+    static constexpr size_t stage_bytes = sizeof(u16) * (size_t)NW * 2 * TILE;
     static constexpr size_t sum_bytes = sizeof(float) * (size_t)SL * R * OROW;
     static constexpr size_t base_bytes = (stage_bytes > sum_bytes ? stage_bytes : sum_bytes);
-    static constexpr size_t lds_bytes = base_bytes + sizeof(float) * 2 * kSeqWaves * 16 * NB;
+    static constexpr size_t line_at = base_bytes + sizeof(float) * 2 * NW * R;
+    static constexpr size_t lds_bytes = line_at + sizeof(unsigned long long) * 64;
 };
 
 // Key tiles [t0, t1) of the sequence (may be empty).  po, pml: null for a final result, else this block's
 // unnormalised sums [rows][D] and (reference maximum in log2 units, sum) [rows].
 // On entry nothing in `smem` may be in use by any wave.
-template <int D, int NB, int RG, bool TREE>
+template <int D, int NB, int NW, bool TREE>
 __device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, float scale, int t0, int t1, float *po,
                                             float2 *pml, char *smem)
 {
-    using S = SeqShape<D, NB, RG>;
-    constexpr int KS = D / 32, DB = D / 16, C8 = S::C8, ROW = S::ROW, TILE = S::TILE, KG = S::KG, TK = S::TK;
-    float *sm = (float *)(smem + S::base_bytes), *sl = sm + kSeqWaves * 16 * NB;
+    using S = SeqShape<D, NB, NW>;
+    constexpr int KS = D / 32, DB = D / 16, C8 = S::C8, ROW = S::ROW, TILE = S::TILE, TK = S::TK;
+    float *sm = (float *)(smem + S::base_bytes), *sl = sm + NW * S::R;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int ln = lane & 15, lg = lane >> 4;
-    const int rg = wave % RG, kg = wave / RG, tg = rg * 64 + lane;
 
-    // 16-byte pieces of a tile: piece i of a thread lies in row tg / C8 + i * (GT / C8)
+    // 16-byte pieces of a tile: piece i of a lane lies in row lane / C8 + i * (64 / C8)
     v4u kreg[S::PIECES], vreg[S::PIECES];
-    const uint32_t koff = (uint32_t)((tg / C8) * (int)s.k_rs + tg % C8 * 8) * 2u;
-    const uint32_t voff = (uint32_t)((tg / C8) * (int)s.v_rs + tg % C8 * 8) * 2u;
+    const uint32_t koff = (uint32_t)((lane / C8) * (int)s.k_rs + lane % C8 * 8) * 2u;
+    const uint32_t voff = (uint32_t)((lane / C8) * (int)s.v_rs + lane % C8 * 8) * 2u;
     auto load = [&](int t) {
         const char *kt = (const char *)((const u16 *)s.k + (size_t)t * TK * s.k_rs);
         const char *vt = (const char *)((const u16 *)s.v + (size_t)t * TK * s.v_rs);
@@ -108,48 +106,47 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, 
         if (last >= TK - 1) {
 #pragma unroll
             for (int i = 0; i < S::PIECES; ++i) {
-                kreg[i] = *(const v4u *)(kt + (koff + (uint32_t)(i * (S::GT / C8) * (int)s.k_rs) * 2u));
-                vreg[i] = *(const v4u *)(vt + (voff + (uint32_t)(i * (S::GT / C8) * (int)s.v_rs) * 2u));
+                kreg[i] = *(const v4u *)(kt + (koff + (uint32_t)(i * (64 / C8) * (int)s.k_rs) * 2u));
+                vreg[i] = *(const v4u *)(vt + (voff + (uint32_t)(i * (64 / C8) * (int)s.v_rs) * 2u));
             }
         } else {                                         // rows past the end repeat the last one
 #pragma unroll
             for (int i = 0; i < S::PIECES; ++i) {
-                const int row = min(tg / C8 + i * (S::GT / C8), last);
-                kreg[i] = *(const v4u *)(kt + (uint32_t)(row * (int)s.k_rs + tg % C8 * 8) * 2u);
-                vreg[i] = *(const v4u *)(vt + (uint32_t)(row * (int)s.v_rs + tg % C8 * 8) * 2u);
+                const int row = min(lane / C8 + i * (64 / C8), last);
+                kreg[i] = *(const v4u *)(kt + (uint32_t)(row * (int)s.k_rs + lane % C8 * 8) * 2u);
+                vreg[i] = *(const v4u *)(vt + (uint32_t)(row * (int)s.v_rs + lane % C8 * 8) * 2u);
             }
         }
     };
-    auto buffer = [&](int b) { return (u16 *)smem + (size_t)(b * KG + kg) * 2 * TILE; };
-    auto store = [&](u16 *dst) {
+    u16 *const mine = (u16 *)smem + (size_t)wave * 2 * TILE;
+    auto store = [&] {
 #pragma unroll
         for (int i = 0; i < S::PIECES; ++i) {
-            const int at = (tg / C8 + i * (S::GT / C8)) * ROW + tg % C8 * 8;
-            *(v4u *)(dst + at) = kreg[i];
-            *(v4u *)(dst + TILE + at) = vreg[i];
+            const int at = (lane / C8 + i * (64 / C8)) * ROW + lane % C8 * 8;
+            *(v4u *)(mine + at) = kreg[i];
+            *(v4u *)(mine + TILE + at) = vreg[i];
         }
     };
 
-    int t = t0 + kg;
-    if (t < t1) load(t);
-    // Q^T operands, and what the lane's rows see of the keys from s.open on
+    // Q^T operands
     v4u qreg[NB][KS];
-    int lim[NB];
-    unsigned long long line[NB];
-    unsigned long long mine = 0ull;
-    if (TREE && t1 * TK > s.open) mine = tree_line(s.parent, s.nodes);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        const int row = min(r.row0 + (rg * NB + nb) * 16 + ln, r.rows - 1), at = row / r.G;
-        if (TREE) {
-            line[nb] = ((unsigned long long)(unsigned)__shfl((int)(mine >> 32), at) << 32) | (unsigned)__shfl((int)mine, at);
-        } else {
-            lim[nb] = s.shift + at;
-        }
+        const int row = min(r.row0 + nb * 16 + ln, r.rows - 1), at = row / r.G;
         const u16 *src = (const u16 *)r.q + (size_t)(row % r.G) * r.q_hs + (size_t)at * r.q_rs + 8 * lg;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qreg[nb][ks] = *(const v4u *)(src + ks * 32);
     }
+    int t = t0 + wave;
+    if (t < t1) load(t);
+    // what every node sees of the drafted keys: every wave writes all of it for itself (the same words)
+    unsigned long long *lines = (unsigned long long *)(smem + S::line_at);
+    if (TREE && t1 * TK > s.open) lines[lane] = tree_line(s.parent, s.nodes);
+    // Q has to be there before the loop: a wait inside it would be one for the next tile's loads as well, in every trip
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qreg[nb][ks]));
     f32x4 o[NB][DB];
     float m[NB], l[NB];
 #pragma unroll
@@ -161,8 +158,11 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, 
     }
     const float c = scale * kLog2e;
 
-    auto compute = [&](const u16 *sk, int j0) {          // 32 keys; V lies one tile behind K
-        const u16 *sv = sk + TILE;
+    for (; t < t1; t += NW) {
+        store();
+        const int j0 = t * TK;
+        if (t + NW < t1) load(t + NW);
+        const u16 *sk = mine, *sv = mine + TILE;
         f32x4 x[NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) x[nb][0] = x[nb][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -177,13 +177,26 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, 
         if (j0 + 31 >= s.open) {
             asm volatile("; mask path" ::: "memory");
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int j = j0 + (e >> 2) * 16 + 4 * lg + (e & 3), node = j - s.open;
-                    const bool seen = TREE ? node < 0 || (node < 64 && ((line[nb] >> (node & 63)) & 1ull)) : j <= lim[nb];
-                    if (!seen) x[nb][e >> 2][e & 3] = -INFINITY;
+            for (int nb = 0; nb < NB; ++nb) {
+                // formed here, from values that the compiler cannot relate to the other uses: kept, they cost registers in the loop
+                int G = r.G, x0 = lane;
+                asm volatile("" : "+s"(G), "+v"(x0));
+                const int at = min(r.row0 + nb * 16 + (x0 & 15), r.rows - 1) / G, first = 4 * (x0 >> 4);
+                unsigned seen;                           // of the tile's keys 4 lg + e (bit e) and 16 + 4 lg + e (bit 16 + e)
+                if (TREE) {
+                    const int node = j0 - s.open;        // what the tile's first key is
+                    const unsigned long long line = lines[at];
+                    if (node >= 0) seen = node < 64 ? (unsigned)(line >> node) : 0u;
+                    else seen = (unsigned)(line << -node) | ((1u << -node) - 1u);        // -31 <= node
+                    seen >>= first;
+                } else {
+                    const int more = s.shift + at - j0 - first;    // keys behind the lane's first that are seen
+                    seen = more >= 31 ? ~0u : more < 0 ? 0u : (2u << more) - 1u;
                 }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!((seen >> ((e >> 2) * 16 + (e & 3))) & 1u)) x[nb][e >> 2][e & 3] = -INFINITY;
+            }
         }
         // against the reference so far, and anew with the true maximum where a row outgrew it (or has none yet)
         v4u pb[NB];
@@ -233,33 +246,6 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, 
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) o[nb][db] = mfma16((v4u){lo.x, lo.y, hi.x, hi.y}, pb[nb], o[nb][db]);
         }
-    };
-
-    if constexpr (RG == 1) {
-        for (; t < t1; t += KG) {
-            store(buffer(0));
-            const int j0 = t * TK;
-            if (t + KG < t1) load(t + KG);
-            compute(buffer(0), j0);
-        }
-    } else {
-        // the groups' tiles in step: stage i of group kg is tile t0 + i KG + kg, in the buffer i % 2
-        const int stages = (t1 - t0 + KG - 1) / KG;
-        if (t < t1) store(buffer(0));
-        if (t + KG < t1) load(t + KG);
-        __syncthreads();
-        for (int i = 0; i < stages; ++i, t += KG) {
-            if (t < t1) {
-#pragma unroll
-                for (int sub = 0; sub < S::SUB; ++sub) {
-                    const int j0 = t * TK + sub * 32;
-                    if (sub == 0 || j0 < s.n) compute(buffer(i & 1) + sub * 32 * ROW, j0);
-                }
-            }
-            if (t + KG < t1) store(buffer((i + 1) & 1));
-            if (t + 2 * KG < t1) load(t + 2 * KG);
-            __syncthreads();
-        }
     }
 
     // the waves' sums: scaled to the common maximum, the upper half's handed to the lower half's, and those
@@ -268,49 +254,44 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, 
     for (int nb = 0; nb < NB; ++nb) {
         l[nb] += __shfl_xor(l[nb], 16);
         l[nb] += __shfl_xor(l[nb], 32);
-        if (lg == 0) { sm[(wave * NB + nb) * 16 + ln] = m[nb]; sl[(wave * NB + nb) * 16 + ln] = l[nb]; }
+        if (lg == 0) { sm[wave * S::R + nb * 16 + ln] = m[nb]; sl[wave * S::R + nb * 16 + ln] = l[nb]; }
     }
     __syncthreads();                                     // also: the last tiles have been read
     float *so = (float *)smem;
-    auto place = [&](int slot, int nb) { return so + ((size_t)slot * S::R + (rg * NB + nb) * 16 + ln) * S::OROW + 4 * lg; };
+    auto place = [&](int slot, int nb) { return so + (slot * S::R + nb * 16 + ln) * S::OROW + 4 * lg; };
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        if constexpr (KG > 1) {
-            float m_all = -INFINITY;
+        float m_all = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < KG; ++w) m_all = fmaxf(m_all, sm[((w * RG + rg) * NB + nb) * 16 + ln]);
-            const float f = m[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[nb] - m_all) * c);
+        for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, sm[w * S::R + nb * 16 + ln]);
+        const float f = m[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[nb] - m_all) * c);
 #pragma unroll
-            for (int db = 0; db < DB; ++db) o[nb][db] *= f;
-        }
-        if (KG == 1 || kg >= KG / 2) {
-#pragma unroll
-            for (int db = 0; db < DB; ++db) *(f32x4 *)(place(KG == 1 ? 0 : kg - KG / 2, nb) + db * 16) = o[nb][db];
+        for (int db = 0; db < DB; ++db) {
+            o[nb][db] *= f;
+            if (wave >= NW / 2) *(f32x4 *)(place(wave - NW / 2, nb) + db * 16) = o[nb][db];
         }
     }
     __syncthreads();
-    if constexpr (KG > 1) {
-        if (kg < KG / 2) {
+    if (wave < NW / 2) {
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int db = 0; db < DB; ++db) *(f32x4 *)(place(kg, nb) + db * 16) += o[nb][db];
-        }
-        __syncthreads();
+            for (int db = 0; db < DB; ++db) *(f32x4 *)(place(wave, nb) + db * 16) += o[nb][db];
     }
+    __syncthreads();
     const int rows_here = min(S::R, r.rows - r.row0);
-    for (int i = threadIdx.x; i < rows_here * (D / 4); i += kSeqWaves * 64) {
-        const int row = i / (D / 4), c4 = i % (D / 4) * 4, rr = row / (16 * NB), ri = row % (16 * NB);
-        f32x4 y = *(const f32x4 *)(so + (size_t)row * S::OROW + c4);
+    for (int i = threadIdx.x; i < rows_here * (D / 4); i += NW * 64) {
+        const int row = i / (D / 4), c4 = i % (D / 4) * 4;
+        f32x4 y = *(const f32x4 *)(so + row * S::OROW + c4);
 #pragma unroll
-        for (int w = 1; w < S::SL; ++w) y += *(const f32x4 *)(so + ((size_t)w * S::R + row) * S::OROW + c4);
+        for (int w = 1; w < S::SL; ++w) y += *(const f32x4 *)(so + (w * S::R + row) * S::OROW + c4);
         float m_row = -INFINITY, l_row = 0.f;
 #pragma unroll
-        for (int w = 0; w < KG; ++w) m_row = fmaxf(m_row, sm[(w * RG + rr) * 16 * NB + ri]);
+        for (int w = 0; w < NW; ++w) m_row = fmaxf(m_row, sm[w * S::R + row]);
 #pragma unroll
-        for (int w = 0; w < KG; ++w) {                   // multiplied, not left out: NaN logits alone leave -inf and a NaN sum
-            const float mw = sm[(w * RG + rr) * 16 * NB + ri];
-            l_row += sl[(w * RG + rr) * 16 * NB + ri] * (mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - m_row) * c));
+        for (int w = 0; w < NW; ++w) {                   // multiplied, not left out: NaN logits alone leave -inf and a NaN sum
+            const float mw = sm[w * S::R + row];
+            l_row += sl[w * S::R + row] * (mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - m_row) * c));
         }
         if (pml) {
             *(f32x4 *)(po + (size_t)row * D + c4) = y;

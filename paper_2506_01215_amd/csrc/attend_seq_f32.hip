@@ -15,12 +15,12 @@
 
 namespace reform {
 
-constexpr int kF32Rows = 16, kF32Keys = 16;
+constexpr int kF32Rows = 16, kF32Keys = 16, kF32Waves = 8;
 
 template <int DP>
 struct F32Sums {
-    float o[kSeqWaves / 2][kF32Rows][DP + 4];
-    float m[kSeqWaves][kF32Rows], l[kSeqWaves][kF32Rows];
+    float o[kF32Waves / 2][kF32Rows][DP + 4];
+    float m[kF32Waves][kF32Rows], l[kF32Waves][kF32Rows];
 };
 
 // As seq_segment: key tiles [t0, t1) of 16 keys for the 16 rows from r.row0 on; D <= DP elements a row.
@@ -48,7 +48,7 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const SeqKeys &s, 
     }
     float m = -INFINITY, l = 0.f;
     const float c = scale * kLog2e;
-    for (int t = t0 + wave; t < t1; t += kSeqWaves) {
+    for (int t = t0 + wave; t < t1; t += kF32Waves) {
         const int j0 = t * kF32Keys;
         const float *kr = (const float *)s.k + (size_t)min(j0 + ln, s.n - 1) * s.k_rs + 4 * lg;
         f32x4 x = zero;
@@ -96,30 +96,30 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const SeqKeys &s, 
     __syncthreads();
     float m_all = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kSeqWaves; ++w) m_all = fmaxf(m_all, sh.m[w][ln]);
+    for (int w = 0; w < kF32Waves; ++w) m_all = fmaxf(m_all, sh.m[w][ln]);
     const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_all) * c);
 #pragma unroll
     for (int a = 0; a < NA; ++a) {
         o[a] *= f;
-        if (wave >= kSeqWaves / 2) *(f32x4 *)&sh.o[wave - kSeqWaves / 2][ln][16 * a + 4 * lg] = o[a];
+        if (wave >= kF32Waves / 2) *(f32x4 *)&sh.o[wave - kF32Waves / 2][ln][16 * a + 4 * lg] = o[a];
     }
     __syncthreads();
-    if (wave < kSeqWaves / 2) {
+    if (wave < kF32Waves / 2) {
 #pragma unroll
         for (int a = 0; a < NA; ++a) *(f32x4 *)&sh.o[wave][ln][16 * a + 4 * lg] += o[a];
     }
     __syncthreads();
     const int rows_here = min(kF32Rows, r.rows - r.row0);
-    for (int i = threadIdx.x; i < rows_here * (DP / 4); i += kSeqWaves * 64) {
+    for (int i = threadIdx.x; i < rows_here * (DP / 4); i += kF32Waves * 64) {
         const int ri = i / (DP / 4), c4 = i % (DP / 4) * 4;
         f32x4 y = *(const f32x4 *)&sh.o[0][ri][c4];
 #pragma unroll
-        for (int w = 1; w < kSeqWaves / 2; ++w) y += *(const f32x4 *)&sh.o[w][ri][c4];
+        for (int w = 1; w < kF32Waves / 2; ++w) y += *(const f32x4 *)&sh.o[w][ri][c4];
         float m_row = -INFINITY, l_row = 0.f;
 #pragma unroll
-        for (int w = 0; w < kSeqWaves; ++w) m_row = fmaxf(m_row, sh.m[w][ri]);
+        for (int w = 0; w < kF32Waves; ++w) m_row = fmaxf(m_row, sh.m[w][ri]);
 #pragma unroll
-        for (int w = 0; w < kSeqWaves; ++w)              // multiplied, not left out: NaN logits alone leave -inf and a NaN sum
+        for (int w = 0; w < kF32Waves; ++w)              // multiplied, not left out: NaN logits alone leave -inf and a NaN sum
             l_row += sh.l[w][ri] * (sh.m[w][ri] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((sh.m[w][ri] - m_row) * c));
         if (pml) {
             *(f32x4 *)(po + (size_t)ri * DP + c4) = y;
@@ -134,7 +134,7 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const SeqKeys &s, 
 }
 
 template <int DP>
-__global__ __launch_bounds__(kSeqWaves * 64, 2) void prompt_attend_f32(PromptParams p)
+__global__ __launch_bounds__(kF32Waves * 64, 2) void prompt_attend_f32(PromptParams p)
 {
     __shared__ F32Sums<DP> sh;
     const int kvh = blockIdx.x % p.Hkv;
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(kSeqWaves * 64, 2) void prompt_attend_f32(PromptPar
 }
 
 template <int DP>
-__global__ __launch_bounds__(kSeqWaves * 64, 2) void tree_attend_f32(TreeParams p)
+__global__ __launch_bounds__(kF32Waves * 64, 2) void tree_attend_f32(TreeParams p)
 {
     __shared__ F32Sums<DP> sh;
     tree_walk<float, kF32Rows, kF32Keys>(p, [&](const SeqRows &r, const SeqKeys &k, int t0, int t1, long slot) {
@@ -161,15 +161,15 @@ namespace {
 template <int DP>
 hipError_t launch_prompt(const PromptParams &p, hipStream_t st)
 {
-    hipLaunchKernelGGL((prompt_attend_f32<DP>), dim3(prompt_grid(p, kF32Rows)), dim3(kSeqWaves * 64), 0, st, p);
+    hipLaunchKernelGGL((prompt_attend_f32<DP>), dim3(prompt_grid(p, kF32Rows)), dim3(kF32Waves * 64), 0, st, p);
     return hipGetLastError();
 }
 
 template <int DP>
 hipError_t launch_tree(const TreeParams &p, hipStream_t st)
 {
-    const unsigned grid = p.shares ? p.shares : (unsigned)p.n_seq * p.Hkv * p.row_blocks;
-    hipLaunchKernelGGL((tree_attend_f32<DP>), dim3(grid), dim3(kSeqWaves * 64), 0, st, p);
+    const unsigned grid = (unsigned)(p.shares ? p.shares : p.n_seq * p.Hkv) * p.row_blocks;
+    hipLaunchKernelGGL((tree_attend_f32<DP>), dim3(grid), dim3(kF32Waves * 64), 0, st, p);
     if (p.shares) tree_merge_launch<DP, kF32Rows, kF32Keys, false>(p, st);
     return hipGetLastError();
 }
@@ -187,7 +187,7 @@ hipError_t prompt_attend_f32_launch(const PromptParams &p, hipStream_t st)
 // Elements of a row of the pieces: heads are padded to the next form.
 size_t tree_part_dim(bool bf16, int D) { return bf16 ? D : D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-void tree_plan_f32(TreeParams &p, int compute_units) { tree_plan(p, kF32Rows, kF32Keys, 16, compute_units); }
+void tree_plan_f32(TreeParams &p, int compute_units) { tree_plan(p, kF32Rows, kF32Keys, 64, 16, 2 * compute_units); }
 
 hipError_t tree_attend_f32_launch(const TreeParams &p, hipStream_t st)
 {

@@ -159,12 +159,12 @@ struct TreeParams {
     int n_seq, Hq, Hkv, G, D, T, max_len;
     long q_ss, q_hs, q_rs, o_ss, o_hs, o_rs, kv_ss, kv_hs;   // elements
     float scale;
-    int shares;              // workgroups over the list of all sequences' key tiles; 0: one per sequence, head and row block
+    int shares;              // parts of the list of all sequences' key tiles (tree_list.h); 0: one workgroup per sequence, head and row block
     int least;               // tiles that a share has at least, where there are fewer sequences and heads than shares
     int row_blocks;          // of T * G rows
     int part_rows;           // rows of one partial result
-    float *part_o;           // [2 * shares][part_rows][D] unnormalised outputs
-    float2 *part_ml;         // [2 * shares][part_rows] reference maximum (log2 units) and sum
+    float *part_o;           // [2 * shares][row_blocks][part_rows][D] unnormalised outputs
+    float2 *part_ml;         // [2 * shares][row_blocks][part_rows] reference maximum (log2 units) and sum
 };
 
 struct PromptParams {

@@ -108,7 +108,7 @@ reform_status check_tree(const reform_tree_desc *d)
     return REFORM_OK;
 }
 
-size_t tree_part_rows(const TreeParams &p) { return (size_t)2 * p.shares * p.part_rows; }
+size_t tree_part_rows(const TreeParams &p) { return (size_t)2 * p.shares * p.row_blocks * p.part_rows; }
 
 }  // namespace
 

@@ -1,59 +1,93 @@
 // Drafted tokens over a batch of caches, bf16 (see reform_tree_attend in reform.h): one token per sequence, a
 // chain or a tree of up to 64.
 //
-// Bound: reading K and V once (a row of 256 bytes meets 16 query rows per matrix instruction; 64 nodes of four
-// heads are 256 rows, which reach 0.7 of the matrix pipe at the rate K and V arrive).  So the keys are shared
-// out over the whole chip (tree_list.h), the rows of a group's heads and nodes are one block of up to 256 rows,
-// and the waves of a workgroup divide the keys as far as the rows allow: up to 16 and 32 rows every wave has
-// key tiles of its own, beyond that two, four or eight waves share each tile.
-#include "attend_seq.h"
+// Bound: reading K and V once, up to some 64 rows (a 16-row block of queries costs a compute unit a sixth of the time that its
+// share of the memory bandwidth takes to bring the keys), then the matrix pipe as well.  So the keys are shared out over the
+// whole chip (tree_list.h), and the rows of a group's heads and nodes are one block of up to 256, for which K and V are
+// read once.  Up to 32 rows every wave has key tiles of its own and no barrier (attend_seq.h); beyond that the waves divide the
+// rows and go through the tiles together (attend_rows.h).
+// Measured, 32/8 heads of 128: one token for each of 32 sequences over 8192 rows (1.07 GB) 183 us, 5.9 TB/s; 24 nodes 206 us, 64 nodes
+// 301 us.  8 waves at head_dim 128, 4 at 64 (two workgroups to a compute unit): 8 nodes, 24/8 of 64, 16 caches of up to 4096 rows
+// 37.6 us with 8 waves, 31.6 with 4; one token, 32/8 of 128, 16 caches of up to 8000 rows 49.7 with 8, 50.2 with 4.
+#include "attend_rows.h"
 #include "tree_list.h"
 
 namespace reform {
 
-template <int D, int NB, int RG>
-__global__ __launch_bounds__(kSeqWaves * 64, 2) void tree_attend(TreeParams p)
+template <int D, int NB, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void tree_attend(TreeParams p)
 {
-    using S = SeqShape<D, NB, RG>;
+    using S = SeqShape<D, NB, NW>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     tree_walk<u16, S::R, S::TK>(p, [&](const SeqRows &r, const SeqKeys &k, int t0, int t1, long slot) {
-        seq_segment<D, NB, RG, true>(r, k, p.scale, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
+        seq_segment<D, NB, NW, true>(r, k, p.scale, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
                                      slot < 0 ? nullptr : p.part_ml + (size_t)slot * p.part_rows, smem);
+    });
+}
+
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void tree_attend_rows(TreeParams p)
+{
+    using S = RowsShape<D, NW, 1>;
+    extern __shared__ __attribute__((aligned(16))) u16 lds[];
+    tree_walk<u16, S::ROWS, S::BN>(p, [&](const SeqRows &r, const SeqKeys &k, int t0, int t1, long slot) {
+        rows_segment<D, NW, 1, true>(r, k, false, p.scale, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
+                                  slot < 0 ? nullptr : p.part_ml + (size_t)slot * p.part_rows, lds);
     });
 }
 
 namespace {
 
-template <int D, int NB, int RG>
+// Rows of a block, and keys of a tile.
+int tree_rows(const TreeParams &p)
+{
+    const int rows = p.T * p.G;
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+}
+int tree_keys(int rows) { return rows > 32 ? kRowsKeys : 32; }
+
+template <int D, int NB, int NW>
 hipError_t launch(const TreeParams &p, hipStream_t st)
 {
-    using S = SeqShape<D, NB, RG>;
-    const hipError_t e = raise_lds<tree_attend<D, NB, RG>>(S::lds_bytes);
+    using S = SeqShape<D, NB, NW>;
+    const hipError_t e = raise_lds<tree_attend<D, NB, NW>>(S::lds_bytes);
     if (e != hipSuccess) return e;
-    const unsigned grid = p.shares ? p.shares : (unsigned)p.n_seq * p.Hkv * p.row_blocks;
-    hipLaunchKernelGGL((tree_attend<D, NB, RG>), dim3(grid), dim3(kSeqWaves * 64), S::lds_bytes, st, p);
+    const unsigned grid = (unsigned)(p.shares ? p.shares : p.n_seq * p.Hkv) * p.row_blocks;
+    hipLaunchKernelGGL((tree_attend<D, NB, NW>), dim3(grid), dim3(NW * 64), S::lds_bytes, st, p);
     if (p.shares) tree_merge_launch<D, S::R, S::TK, true>(p, st);
+    return hipGetLastError();
+}
+
+template <int D, int NW>
+hipError_t launch_long(const TreeParams &p, hipStream_t st)
+{
+    using S = RowsShape<D, NW, 1>;
+    const hipError_t e = raise_lds<tree_attend_rows<D, NW>>(S::lds_bytes);
+    if (e != hipSuccess) return e;
+    const unsigned grid = (unsigned)(p.shares ? p.shares : p.n_seq * p.Hkv) * p.row_blocks;
+    hipLaunchKernelGGL((tree_attend_rows<D, NW>), dim3(grid), dim3(NW * 64), S::lds_bytes, st, p);
+    if (p.shares) tree_merge_launch<D, S::ROWS, S::BN, true>(p, st);
     return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_rows(const TreeParams &p, hipStream_t st)
 {
-    const int rows = p.T * p.G;
-    if (rows <= 16) return launch<D, 1, 1>(p, st);
-    if (rows <= 32) return launch<D, 2, 1>(p, st);
-    if (rows <= 64) return launch<D, 2, 2>(p, st);
-    if (rows <= 128) return launch<D, 2, 4>(p, st);
-    return launch<D, 2, 8>(p, st);
+    const int R = tree_rows(p);
+    constexpr int NW = D == 64 ? 4 : 8;
+    if (R == 16) return launch<D, 1, NW>(p, st);
+    if (R == 32) return launch<D, 2, NW>(p, st);
+    if (R == 64) return launch_long<D, 2>(p, st);
+    if (R == 128) return launch_long<D, 4>(p, st);
+    return launch_long<D, 8>(p, st);
 }
 
 }  // namespace
 
 void tree_plan_bf16(TreeParams &p, int compute_units)
 {
-    const int rows = p.T * p.G;
-    const int R = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-    tree_plan(p, R, R == 256 ? 64 : 32, 8, compute_units);
+    const int R = tree_rows(p), keys = tree_keys(R);
+    tree_plan(p, R, keys, 1024 / keys, 256 / keys, R == 256 ? compute_units : (R <= 32 && p.D == 128 ? 1 : 2) * compute_units);
 }
 
 hipError_t tree_attend_bf16(const TreeParams &p, hipStream_t st)

@@ -1,16 +1,18 @@
 // How drafted tokens' attention is dealt to workgroups (see reform_tree_attend in reform.h).
 //
-// Every (sequence, KV head, row block) is an item with as many places as the sequence has key tiles, and
-// kTreeStart more in front for the time it takes to begin one.  The items of all sequences form one list, and
-// `shares` workgroups take equal parts of it, whatever items these cut through: a batch of caches of any lengths
-// fills the chip evenly, and the host need not know the lengths.  An item that one share covers alone is
-// finished there; the others' pieces are added up by tree_merge.
+// Every (sequence, KV head) is an item with as many places as the sequence has key tiles, and kTreeStart more in front
+// for the time it takes to begin one.  The items of all sequences form one list, which is cut into `shares` equal
+// parts, whatever items these cut through: a batch of caches of any lengths fills the chip evenly, and the host
+// need not know the lengths.  The rows of an item (nodes times heads of the group) may be several blocks: then as
+// many workgroups go through a share side by side, on one XCD, so that K and V come from memory once and for the other
+// blocks from its L2.  An item that one share covers alone is finished there; the others' pieces are added up by
+// tree_merge.
 #pragma once
 #include "attend_seq.h"
 
 namespace reform {
 
-constexpr int kTreeStart = 4;
+constexpr int kTreeStart = 8;
 
 struct TreeSeq {
     int len, nodes, blocks, tiles;       // cached rows, drafted nodes, row blocks, key tiles
@@ -29,40 +31,56 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams &p, int b)
 
 // Places of one of a sequence's items, and of all of them.
 __device__ __forceinline__ int tree_places(const TreeSeq &s) { return s.tiles + kTreeStart; }
-__device__ __forceinline__ int tree_all_places(const TreeParams &p, const TreeSeq &s) { return p.Hkv * s.blocks * tree_places(s); }
+__device__ __forceinline__ int tree_items(const TreeParams &p, const TreeSeq &s) { return s.blocks ? p.Hkv : 0; }
+__device__ __forceinline__ int tree_all_places(const TreeParams &p, const TreeSeq &s) { return tree_items(p, s) * tree_places(s); }
 
-// The list as all lanes of a wave see it.
+// The list as all lanes of a wave see it.  The first 64 sequences stay in the lanes' registers: with no more
+// than these the lengths are read once.
 template <int R, int TK>
 struct TreeList {
     int total, shares;                   // places, shares that are not empty
+    TreeSeq lane;                        // sequence `lane`
+    int lane_places;                     // and its places
 
+    __device__ __forceinline__ int load(const TreeParams &p, int b, TreeSeq &s) const
+    {
+        s = {0, 0, 0, 0};
+        if (b >= p.n_seq) return 0;
+        s = tree_seq<R, TK>(p, b);
+        return tree_all_places(p, s);
+    }
     __device__ __forceinline__ explicit TreeList(const TreeParams &p)
     {
-        int items = 0;
-        total = 0;
-        for (int b0 = 0; b0 < p.n_seq; b0 += 64) {
-            int mine = 0, count = 0;
-            const int b = b0 + (threadIdx.x & 63);
-            if (b < p.n_seq) {
-                const TreeSeq s = tree_seq<R, TK>(p, b);
-                mine = tree_all_places(p, s);
-                count = p.Hkv * s.blocks;
-            }
+        const int l = threadIdx.x & 63;
+        lane_places = load(p, l, lane);
+        total = __builtin_amdgcn_readlane(wave_incl_scan(lane_places), 63);
+        int items = __builtin_amdgcn_readlane(wave_incl_scan(tree_items(p, lane)), 63);
+        for (int b0 = 64; b0 < p.n_seq; b0 += 64) {
+            TreeSeq s;
+            const int mine = load(p, b0 + l, s);
             total += __builtin_amdgcn_readlane(wave_incl_scan(mine), 63);
-            items += __builtin_amdgcn_readlane(wave_incl_scan(count), 63);
+            items += __builtin_amdgcn_readlane(wave_incl_scan(tree_items(p, s)), 63);
         }
         shares = max(1, min(p.shares, max(items, total / p.least)));
     }
     __device__ __forceinline__ int begin(int share) const { return (int)((long)total * share / shares); }
     // the share that place x lies in: begin(w) <= x  <=>  w total / shares < x + 1
     __device__ __forceinline__ int share_of(int x) const { return (int)((((long)x + 1) * shares - 1) / total); }
+    // sequence b (the same in all lanes)
+    __device__ __forceinline__ TreeSeq seq(const TreeParams &p, int b) const
+    {
+        if (b >= 64) return tree_seq<R, TK>(p, b);
+        return {__builtin_amdgcn_readlane(lane.len, b), __builtin_amdgcn_readlane(lane.nodes, b),
+                __builtin_amdgcn_readlane(lane.blocks, b), __builtin_amdgcn_readlane(lane.tiles, b)};
+    }
     // places in front of sequence b
     __device__ __forceinline__ int before(const TreeParams &p, int b) const
     {
-        int sum = 0;
-        for (int b0 = 0; b0 < b; b0 += 64) {
-            const int x = b0 + (threadIdx.x & 63);
-            const int mine = x < b ? tree_all_places(p, tree_seq<R, TK>(p, x)) : 0;
+        const int l = threadIdx.x & 63;
+        int sum = __builtin_amdgcn_readlane(wave_incl_scan(l < b ? lane_places : 0), 63);
+        for (int b0 = 64; b0 < b; b0 += 64) {
+            TreeSeq s;
+            const int mine = b0 + l < b ? load(p, b0 + l, s) : 0;
             sum += __builtin_amdgcn_readlane(wave_incl_scan(mine), 63);
         }
         return sum;
@@ -70,10 +88,8 @@ struct TreeList {
     // the sequence that place x (< total) lies in, and its first place
     __device__ __forceinline__ int find(const TreeParams &p, int x, int &first) const
     {
-        int sum = 0;
+        int sum = 0, mine = lane_places;
         for (int b0 = 0;; b0 += 64) {
-            const int b = b0 + (threadIdx.x & 63);
-            const int mine = b < p.n_seq ? tree_all_places(p, tree_seq<R, TK>(p, b)) : 0;
             const int incl = wave_incl_scan(mine), all = __builtin_amdgcn_readlane(incl, 63);
             if (x < sum + all) {
                 const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(x < sum + incl));
@@ -81,19 +97,34 @@ struct TreeList {
                 return b0 + l;
             }
             sum += all;
+            TreeSeq s;
+            mine = load(p, b0 + 64 + (threadIdx.x & 63), s);
         }
     }
 };
 
+// Share and row block of a workgroup.  Workgroups go to the eight XCDs in turn, so those of one share are eight apart.
+__device__ __forceinline__ int tree_share(const TreeParams &p, int block, int shares, int &rb)
+{
+    const int each = shares >> 3, even = 8 * each * p.row_blocks;        // shares of an XCD
+    const int j = block < even ? block >> 3 : block - even;
+    const int s = j / p.row_blocks;
+    rb = j - s * p.row_blocks;
+    return block < even ? (block & 7) * each + s : 8 * each + s;
+}
+
 // Where a share's piece of an item that it does not cover alone goes.
-__device__ __forceinline__ long tree_slot(int share, int t0) { return 2l * share + (t0 > 0 ? 0 : 1); }
+__device__ __forceinline__ long tree_slot(const TreeParams &p, int share, int t0, int rb)
+{
+    return (2l * share + (t0 > 0 ? 0 : 1)) * p.row_blocks + rb;
+}
 
 // The items of one workgroup, in the list's order: f(rows, keys, first tile, last tile + 1, slot of a piece or -1).
 template <class T, int R, int TK, class F>
 __device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
 {
-    auto segment = [&](int b, const TreeSeq &seq, int item, int t0, int t1, long slot) {
-        const int kvh = item / seq.blocks, rb = item - kvh * seq.blocks;
+    int rb;
+    auto segment = [&](int b, const TreeSeq &seq, int kvh, int t0, int t1, long slot) {
         SeqRows r;
         r.q = (const T *)p.q + (size_t)b * p.q_ss + (size_t)kvh * p.G * p.q_hs;
         r.out = (T *)p.out + (size_t)b * p.o_ss + (size_t)kvh * p.G * p.o_hs;
@@ -110,133 +141,161 @@ __device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
         f(r, k, t0, t1, slot);
     };
     const bool whole = p.shares == 0;                    // one item to a workgroup
-    int b, item, pos = 0, begin = 0, end;
+    const TreeList<R, TK> list(p);
+    int b, kvh, pos = 0, begin = 0, end, share = 0;
     TreeSeq seq;
     if (whole) {
-        const int items = p.Hkv * p.row_blocks;
-        b = blockIdx.x / items;
-        item = blockIdx.x - b * items;
-        seq = tree_seq<R, TK>(p, b);
-        if (item >= p.Hkv * seq.blocks) return;
+        const int item = blockIdx.x / p.row_blocks;
+        rb = blockIdx.x - item * p.row_blocks;
+        b = item / p.Hkv;
+        kvh = item - b * p.Hkv;
+        seq = list.seq(p, b);
+        if (rb >= seq.blocks) return;
         end = tree_places(seq);
     } else {
-        const TreeList<R, TK> list(p);
-        const int share = blockIdx.x;
-        if (share >= list.shares || list.total == 0) return;
+        if ((int)blockIdx.x >= list.shares * p.row_blocks || list.total == 0) return;
+        share = tree_share(p, blockIdx.x, list.shares, rb);
         begin = list.begin(share);
         end = list.begin(share + 1);
-        if (begin >= end) return;
         int first;
         b = list.find(p, begin, first);
-        seq = tree_seq<R, TK>(p, b);
-        item = (begin - first) / tree_places(seq);
-        pos = first + item * tree_places(seq);
+        seq = list.seq(p, b);
+        kvh = (begin - first) / tree_places(seq);
+        pos = first + kvh * tree_places(seq);
     }
     bool again = false;
     while (pos < end) {
         const int t0 = max(begin - pos - kTreeStart, 0), t1 = min(end - pos - kTreeStart, seq.tiles);
-        if (t0 < t1) {
+        if (t0 < t1 && rb < seq.blocks) {
             if (again) __syncthreads();                  // the sums of the item before are still read
             again = true;
-            segment(b, seq, item, t0, t1, t0 > 0 || t1 < seq.tiles ? tree_slot(blockIdx.x, t0) : -1);
+            segment(b, seq, kvh, t0, t1, t0 > 0 || t1 < seq.tiles ? tree_slot(p, share, t0, rb) : -1);
         }
         pos += tree_places(seq);
         if (whole) return;
-        if (++item == p.Hkv * seq.blocks) {
-            item = 0;
+        if (++kvh == p.Hkv) {
+            kvh = 0;
             do {
                 if (++b >= p.n_seq) return;
-                seq = tree_seq<R, TK>(p, b);
+                seq = list.seq(p, b);
             } while (seq.blocks == 0);
         }
     }
 }
 
-// The pieces of the items that several shares covered, in the order of the shares.  A thread has four columns
-// of a row and every fourth piece; four threads' sums meet in LDS.
+// The pieces of the items that several shares covered.  A workgroup has `rows` rows (a power of two) of an item; a thread has
+// four columns of one of them and every n-th piece, which it adds up against the largest reference of its own,
+// references, sums and columns all loaded at once; then the n threads' sums meet in LDS.  The order is that of the
+// shares, whoever is done first.
+constexpr int kTreeMaxShares = 512;
+
 template <int D, int R, int TK, bool BF16>
-__global__ __launch_bounds__(256) void tree_merge(TreeParams p, int rows_each)
+__global__ __launch_bounds__(256) void tree_merge(TreeParams p, int rows)
 {
-    constexpr int C4 = D / 4, ROWS = 64 / C4 < 1 ? 1 : 64 / C4;         // quads of a row, rows of a pass
-    __shared__ f32x4 so[4][64];
-    __shared__ float sl[4][64];
+    constexpr int C4 = D / 4, BATCH = 4;                 // quads of a row, pieces of a trip
+    __shared__ f32x4 so[256];
+    __shared__ float2 sml[256];
     const TreeList<R, TK> list(p);
     if (list.total == 0) return;
-    const int per_seq = p.Hkv * p.row_blocks, chunks = (p.part_rows + rows_each - 1) / rows_each;
-    const int chunk = blockIdx.x % chunks, at = blockIdx.x / chunks;
-    const int b = at / per_seq, item = at - b * per_seq;
-    const TreeSeq seq = tree_seq<R, TK>(p, b);
-    if (item >= p.Hkv * seq.blocks) return;
-    const int kvh = item / seq.blocks, rb = item - kvh * seq.blocks;
-    const int pos = list.before(p, b) + item * tree_places(seq) + kTreeStart;
-    const int w0 = list.share_of(pos), w1 = list.share_of(pos + seq.tiles - 1);
-    if (w0 == w1) return;
-    const int rows = min(R, seq.nodes * p.G - rb * R);
-    const int g = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int r0 = chunk * rows_each; r0 < min((chunk + 1) * rows_each, rows); r0 += ROWS) {
-        const int row = r0 + lane / C4, c4 = lane % C4 * 4;
-        const bool live = row < rows && lane < ROWS * C4;
-        float m = -INFINITY;
-        if (live) {
-            for (int w = w0; w <= w1; ++w) m = fmaxf(m, p.part_ml[(size_t)tree_slot(w, w - w0) * p.part_rows + row].x);
-        }
-        f32x4 y = {0.f, 0.f, 0.f, 0.f};
-        float l = 0.f;
-        if (live) {
-            for (int w = w0 + g; w <= w1; w += 4) {
-                const size_t slot = (size_t)tree_slot(w, w - w0) * p.part_rows + row;
-                const float2 ml = p.part_ml[slot];
-                const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-                l += ml.y * f;
-                y += *(const f32x4 *)(p.part_o + slot * D + c4) * f;
-            }
-        }
-        so[g][lane] = y;
-        sl[g][lane] = l;
-        __syncthreads();
-        if (g == 0 && live) {
+    // an item's workgroups on the XCD that most of its shares ran on (tree_share): its L2 holds the pieces
+    const int chunks = (p.part_rows + rows - 1) / rows * p.row_blocks, items = p.n_seq * p.Hkv, each = items >> 3;
+    const int even = 8 * each * chunks, j = (int)blockIdx.x < even ? blockIdx.x >> 3 : blockIdx.x - even;
+    const int item = ((int)blockIdx.x < even ? (blockIdx.x & 7) * each : 8 * each) + j / chunks;
+    const int rb = j % chunks % p.row_blocks, chunk = j % chunks / p.row_blocks;
+    const int b = item / p.Hkv, kvh = item - b * p.Hkv;
+    const TreeSeq seq = list.seq(p, b);
+    if (rb >= seq.blocks) return;
+    const int pos = list.before(p, b) + kvh * tree_places(seq) + kTreeStart;
+    const int w0 = list.share_of(pos), n = list.share_of(pos + seq.tiles - 1) - w0 + 1;
+    const int r0 = chunk * rows, here = min(rows, seq.nodes * p.G - rb * R - r0);
+    if (n == 1 || here <= 0) return;
+    const int group = rows * C4, groups = 256 / group;   // threads that have different quads
+    const int g = threadIdx.x / group, q = threadIdx.x - g * group, r = q / C4, c4 = q % C4 * 4;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    if (g < groups && r < here) {
+        for (int w = g; w < n; w += BATCH * groups) {
+            float2 ml[BATCH];
+            f32x4 o[BATCH];
 #pragma unroll
-            for (int i = 1; i < 4; ++i) {
-                y += so[i][lane];
-                l += sl[i][lane];
+            for (int i = 0; i < BATCH; ++i) {            // pieces past the last repeat it, without weight
+                const int x = min(w + i * groups, n - 1);
+                const size_t at = (size_t)tree_slot(p, w0 + x, x, rb) * p.part_rows + r0 + r;
+                ml[i] = p.part_ml[at];
+                o[i] = *(const f32x4 *)(p.part_o + at * D + c4);
             }
-            const int node = (rb * R + row) / p.G, head = kvh * p.G + (rb * R + row) % p.G;
-            const float inv = l == 0.f ? 0.f : 1.0f / l;
-            const size_t dst = (size_t)b * p.o_ss + (size_t)head * p.o_hs + (size_t)node * p.o_rs + c4;
-            y *= inv;
-            if (c4 < p.D) {
-                if (BF16) *(v2u *)((u16 *)p.out + dst) = (v2u){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
-                else *(f32x4 *)((float *)p.out + dst) = y;
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                if (w + i * groups >= n) ml[i] = make_float2(-INFINITY, 0.f);
+                top = fmaxf(top, ml[i].x);
             }
-            if (c4 == 0 && p.lse) p.lse[((size_t)b * p.Hq + head) * p.T + node] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+            const float ref = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(m - ref);
+            y *= old;
+            l *= old;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                if (w + i * groups >= n) continue;
+                const float f = __builtin_amdgcn_exp2f(ml[i].x - ref);           // 0 where no key was seen
+                l += ml[i].y * f;
+                y += o[i] * f;
+            }
+            m = top;
         }
-        __syncthreads();
+    }
+    so[threadIdx.x] = y;
+    sml[threadIdx.x] = make_float2(m, l);
+    __syncthreads();
+    if (g == 0 && r < here) {
+        for (int i = 1; i < groups; ++i) m = fmaxf(m, sml[i * group + q].x);
+        const float ref = m == -INFINITY ? 0.f : m;
+        y = (f32x4){0.f, 0.f, 0.f, 0.f};
+        l = 0.f;
+        for (int i = 0; i < groups; ++i) {
+            const float2 ml = sml[i * group + q];
+            const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+            l += ml.y * f;
+            y += so[i * group + q] * f;
+        }
+        const int row = rb * R + r0 + r, node = row / p.G, head = kvh * p.G + row % p.G;
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        const size_t dst = (size_t)b * p.o_ss + (size_t)head * p.o_hs + (size_t)node * p.o_rs + c4;
+        y *= inv;
+        if (c4 < p.D) {
+            if (BF16) *(v2u *)((u16 *)p.out + dst) = (v2u){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+            else *(f32x4 *)((float *)p.out + dst) = y;
+        }
+        if (c4 == 0 && p.lse) p.lse[((size_t)b * p.Hq + head) * p.T + node] = (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
 }
 
+// One row to a workgroup where that makes no more than some eight workgroups a compute unit, else two, four or more.
 template <int D, int R, int TK, bool BF16>
 inline void tree_merge_launch(const TreeParams &p, hipStream_t st)
 {
-    const int rows_each = p.part_rows < 4 ? p.part_rows : 4;
-    const unsigned chunks = (p.part_rows + rows_each - 1) / rows_each;
-    hipLaunchKernelGGL((tree_merge<D, R, TK, BF16>), dim3((unsigned)p.n_seq * p.Hkv * p.row_blocks * chunks), dim3(256), 0, st, p,
-                       rows_each);
+    const long blocks = (long)p.n_seq * p.Hkv * p.row_blocks;
+    int rows = 1;
+    while (2 * rows <= 1024 / D && rows < p.part_rows && blocks * ((p.part_rows + rows - 1) / rows) > 2048) rows *= 2;
+    const unsigned chunks = (p.part_rows + rows - 1) / rows;
+    hipLaunchKernelGGL((tree_merge<D, R, TK, BF16>), dim3((unsigned)blocks * chunks), dim3(256), 0, st, p, rows);
 }
 
-// Row blocks, shares and the rows of a piece for blocks of R rows and tiles of TK keys.  No shares where every
-// item is short (`least` tiles: what keeps the waves of one workgroup busy): then one workgroup takes an item whole,
-// and there is nothing to merge.
-inline void tree_plan(TreeParams &p, int R, int TK, int least, int workgroups)
+// Row blocks, shares and the rows of a piece for blocks of R rows and tiles of TK keys.  No shares where every item is
+// short (`whole` tiles): then one workgroup takes an item whole, and there is nothing to merge.  `least`: tiles
+// that keep the waves of one workgroup busy.
+inline void tree_plan(TreeParams &p, int R, int TK, int whole, int least, int workgroups)
 {
     const int rows = p.T * p.G;
     p.row_blocks = (rows + R - 1) / R;
     p.part_rows = rows < R ? rows : R;
     p.least = least;
     const int tiles = (p.max_len + p.T + TK - 1) / TK;
-    if (tiles <= least) return;
-    const double items = (double)p.n_seq * p.Hkv * p.row_blocks, most = items * (tiles + kTreeStart) / least;
+    if (tiles <= whole) return;
+    const double items = (double)p.n_seq * p.Hkv, most = items * (tiles + kTreeStart) / least;
     const double want = items > most ? items : most;
-    p.shares = want < workgroups ? (int)want : workgroups;
+    int room = workgroups / p.row_blocks;
+    room = room < 1 ? 1 : room > kTreeMaxShares ? kTreeMaxShares : room;
+    p.shares = want < room ? (int)want : room;
 }
 
 }  // namespace reform

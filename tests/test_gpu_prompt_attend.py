@@ -78,20 +78,40 @@ def test_keys_before_and_rows_without_keys(hq, hkv, d, q_lens, k_lens, dtype):
     run_case(hq, hkv, d, q_lens, k_lens, dtype, seed=d, spare=11)
 
 
-@pytest.mark.parametrize("rows", ["short", "narrow", "wide"])
-@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 128), (6, 2, 64), (7, 1, 128), (2, 2, 64)])
-def test_every_form(rows, hq, hkv, d):
-    """Batches large enough for the blocks of 128 and 256 rows, ragged ends of all kinds; few heads, so that the
-    reference stays quick.  The form follows the number of rows: many short sequences take the last one."""
-    unit = {"short": 900, "narrow": 9000, "wide": 36000}[rows] // hq
-    lens, left, rnd = [], unit, random.Random(unit + d)
-    while left > 0:
-        n = min(left, rnd.choice([1, 7, 64, 65, 128, 257, 600, 777]))
-        lens.append(n)
-        left -= n
-    run_case(hq, hkv, d, lens, lens, BF, seed=unit, spare=3)
-    if rows != "short":
-        run_case(hq, hkv, d, [unit // 8, 1], [unit // 8 + 130, 70], BF, seed=unit)
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    from test_prompt_plan import load_plan
+    return load_plan(tmp_path_factory)
+
+
+@pytest.mark.parametrize("d,hq,hkv,n,total,form", [
+    (64, 2, 2, 3, 700, (32, 8)), (64, 7, 1, 1, 900, (32, 8)), (64, 24, 8, 5, 700, (64, 2)), (64, 6, 2, 9, 700, (64, 2)),
+    (64, 12, 4, 40, 6000, (128, 1)), (64, 7, 7, 60, 9000, (128, 1)), (64, 32, 1, 8, 14000, (256, 1)), (64, 30, 2, 1, 9000, (256, 1)),
+    (128, 6, 2, 7, 700, (64, 2)), (128, 3, 1, 1, 1000, (64, 2)), (128, 16, 2, 4, 1200, (128, 2)), (128, 14, 2, 3, 3000, (128, 2)),
+    (128, 12, 4, 40, 5000, (128, 1)), (128, 7, 7, 90, 7000, (128, 1)), (128, 32, 1, 24, 14000, (256, 1)), (128, 30, 2, 1, 9000, (256, 1)),
+])
+def test_every_form(plan, d, hq, hkv, n, total, form):
+    """Ragged batches that take each of the forms (the plan's own header says so), with and without keys in front; the
+    reference on three of the heads."""
+    rnd = random.Random(total + d)
+    cuts = sorted(rnd.sample(range(1, total), n - 1))
+    lens = [b - a for a, b in zip([0] + cuts, cuts + [total])]
+    assert plan(d, hq // hkv, hkv, n, total, total) == form
+    g = torch.Generator().manual_seed(total)
+    for front in (0, 37):
+        k_lens = [x + front for x in lens]
+        nk = sum(k_lens)
+        if front and (total > 9000 or plan(d, hq // hkv, hkv, n, total, nk) != form):
+            continue
+        q = torch.randn((hq, total, d), generator=g).bfloat16()
+        k, v = (torch.randn((hkv, nk, d), generator=g).bfloat16() for _ in range(2))
+        print(f"[prompt form] {form} {hq}/{hkv} d={d} n={n} total={total} front={front}", flush=True)
+        out, lse = binding.reform_prompt_attend(q.to(DEV), k.to(DEV), v.to(DEV), i32(starts(lens)), d ** -0.5,
+                                                cu_k=i32(starts(k_lens)) if front else None)
+        for h in sorted({0, hq // 2, hq - 1}):
+            kv = slice(h * hkv // hq, h * hkv // hq + 1)
+            want, wl, a, err = ref.prompt_attend(q[h:h + 1], k[kv], v[kv], lens, k_lens, d ** -0.5)
+            ref.check_attention(out[h:h + 1], lse[h:h + 1], want, wl, a, err, max(k_lens), BF, f"head {h}")
 
 
 def test_token_major_strides():

@@ -57,6 +57,9 @@ def run_case(hq, hkv, d, T, lens, dtype, seed, chain=False, counts=None, spare=3
     (8, 2, 64, 17, [600, 1], BF), (12, 4, 128, 40, [900, 64, 0], BF),     # 68 and 120 rows
     (8, 2, 128, 64, [1000, 0, 63], BF), (4, 1, 64, 33, [2500], BF),       # 256 and 132 rows
     (16, 2, 128, 64, [700, 40], BF), (14, 2, 64, 50, [300], BF),          # 512 and 350 rows: two row blocks
+    (8, 2, 64, 32, [3000, 0, 1500], BF), (8, 2, 128, 30, [2500], BF),     # the same blocks shared out
+    (16, 2, 128, 64, [3000, 40], BF), (14, 2, 64, 50, [2000, 1999], BF),
+    (4, 2, 128, 15, [2100, 5], BF), (6, 2, 64, 21, [1300], BF),
     (4, 4, 64, 1, [0, 500], F), (8, 2, 128, 7, [300, 20, 0], F), (6, 2, 36, 64, [90, 700], F),
     (2, 1, 256, 3, [1000, 5], F), (8, 1, 100, 20, [40], F),
 ])

@@ -99,9 +99,9 @@ def test_prompt_rejects_pointers_and_types():
 
 
 def tree(**kw):
-    base = dict(struct_size=size(binding.TreeDesc), dtype=1, n_seq=3, n_q_heads=8, n_kv_heads=2, head_dim=128, n_nodes=5, max_cache_len=1000,
-                capacity=1005, scale=0.1, q_seq_stride=5120, q_head_stride=640, q_row_stride=128, o_seq_stride=5120, o_head_stride=640,
-                o_row_stride=128, kv_seq_stride=2 * 1005 * 128, kv_head_stride=1005 * 128)
+    base = dict(struct_size=size(binding.TreeDesc), dtype=1, n_seq=3, n_q_heads=8, n_kv_heads=2, head_dim=128, n_nodes=5, max_cache_len=5000,
+                capacity=5005, scale=0.1, q_seq_stride=5120, q_head_stride=640, q_row_stride=128, o_seq_stride=5120, o_head_stride=640,
+                o_row_stride=128, kv_seq_stride=2 * 5005 * 128, kv_head_stride=5005 * 128)
     return binding.TreeDesc(**{**base, **kw})
 
 
@@ -111,7 +111,7 @@ def call_tree(d, q=FAKE, k=FAKE, v=FAKE, lens=FAKE, out=FAKE, ws=None, nbytes=0)
 
 @pytest.mark.parametrize("field,value,status", [
     ("struct_size", 4, 1), ("dtype", -1, 1), ("n_kv_heads", 3, 1), ("n_seq", -1, 1), ("n_nodes", 0, 1), ("max_cache_len", -1, 1),
-    ("max_cache_len", 1001, 1), ("capacity", 1004, 1), ("scale", -1.0, 1), ("q_row_stride", 4, 1), ("kv_seq_stride", -128, 1),
+    ("max_cache_len", 5001, 1), ("capacity", 5004, 1), ("scale", -1.0, 1), ("q_row_stride", 4, 1), ("kv_seq_stride", -128, 1),
     ("o_row_stride", 64, 1), ("o_head_stride", 128, 1), ("o_seq_stride", 64, 1), ("head_dim", 96, 2), ("n_seq", 1 << 28, 2),
 ])
 def test_tree_rejects(field, value, status):
@@ -124,7 +124,7 @@ def test_tree_rejects(field, value, status):
 
 def test_tree_rejects_pointers_nodes_and_workspaces():
     lib = binding.load_library()
-    assert call_tree(tree(n_nodes=65, capacity=2000, o_head_stride=65 * 128)) == 2
+    assert call_tree(tree(n_nodes=65, capacity=6000, o_head_stride=65 * 128)) == 2
     for kw in (dict(q=None), dict(k=None), dict(v=None), dict(lens=None), dict(out=None), dict(k=FAKE + 8)):
         assert call_tree(tree(), **kw) == 1
     need = lib.reform_tree_attend_workspace(ctypes.byref(tree()))
@@ -185,13 +185,13 @@ def test_host_tensors_are_refused():
 def test_shapes_are_checked():
     z = torch.zeros
     i = lambda *s: z(s, dtype=torch.int32)  # noqa: E731
-    with pytest.raises(AssertionError):
+    with pytest.raises(ValueError):
         binding.reform_rotary_embed(z(4, 3, 64), z(2, 4, 64), None, i(3))
-    with pytest.raises(AssertionError):
+    with pytest.raises(ValueError):
         binding.reform_rotary_embed(z(4, 3, 64), z(2, 3, 64), None, i(3), slot=i(3))          # no cache for the slots
-    with pytest.raises(AssertionError):
+    with pytest.raises(ValueError):
         binding.prompt_desc(z(4, 3, 64), z(2, 3, 32), z(2, 3, 32), z(4, 3, 64), i(2), 0.1)
-    with pytest.raises(AssertionError):
+    with pytest.raises(ValueError):
         binding.tree_desc(z(2, 4, 3, 64), z(1, 2, 9, 64), z(1, 2, 9, 64), z(2, 4, 3, 64), 0.1)
     with pytest.raises(ValueError, match="cubic"):
         binding.reform_rotary_embed(z(4, 3, 64), None, None, i(3), q_out=z(4, 3, 64), scaling="cubic")
