@@ -410,7 +410,7 @@ reform_status reform_gather_rows(const reform_rows_desc *desc, const void *table
  * place); other overlaps of outputs with inputs or each other are not allowed.
  * Supported: head_dim <= 512 and a multiple of 16 bytes; rotary_dim even, at most head_dim, a multiple of 16
  * bytes (REFORM_PAIRS_ADJACENT) or of 32 (REFORM_PAIRS_HALVES); strides multiples of 16 bytes, pointers
- * 16-byte aligned; n_tokens = 0 does nothing.
+ * 16-byte aligned; n_tokens times the 16-byte pieces of a row below 2^31; n_tokens = 0 does nothing.
  */
 typedef enum { REFORM_PAIRS_HALVES = 0, REFORM_PAIRS_ADJACENT = 1 } reform_rope_pairs;
 typedef enum {
@@ -458,10 +458,12 @@ reform_status reform_rotary_embed(const reform_rotary_desc *desc, const void *q,
  * The lengths are read on the device, so a captured call follows them.  Boundaries outside [0, n_q_rows]
  * or [0, n_k_rows] are moved into it and a descending pair counts as an empty sequence, so that nothing
  * outside the tensors is read or written; sequences must not overlap in q.
- * Arithmetic as in reform_chunk_attend_score, bitwise reproducible.
+ * Arithmetic as in reform_chunk_attend_score, bitwise reproducible.  Keys and values that are not finite stay
+ * within their sequence; there, rows before such a value may become NaN as well as those that see it (its
+ * weight 0 is multiplied with it).  The same holds in reform_tree_attend for the nodes of one sequence.
  * Supported: REFORM_BF16 with head_dim 64 or 128; REFORM_F32 with head_dim % 4 == 0, <= 256; at most 65536
- * sequences; n_q_heads * n_q_rows and n_kv_heads * n_k_rows below 2^30; row strides of k and v below 2^24.
- * n_q_rows = 0 does nothing.
+ * sequences; n_q_heads * n_q_rows / 16 + n_kv_heads * n_seq below 2^23, n_kv_heads * n_k_rows below 2^30; row
+ * strides of k and v below 2^24.  n_q_rows = 0 does nothing.
  */
 typedef struct {
     uint32_t struct_size;
@@ -498,8 +500,8 @@ reform_status reform_prompt_attend(const reform_prompt_desc *desc, const void *q
  *                moved into it.  Rows of out and lse from node_count[b] on keep what they held.
  *     lse        [n_seq][n_q_heads][n_nodes] fp32, may be NULL
  * Supported: n_nodes in [1, 64]; types and head_dim as reform_prompt_attend; max_cache_len + n_nodes <=
- * capacity; with B = ceil(n_nodes * G / 16), n_seq * n_kv_heads * B * ((max_cache_len + n_nodes) / 16 + 64) below 2^31.
- * n_seq = 0 does nothing.
+ * capacity; n_seq * n_q_heads * n_nodes at most 2^22; with B = ceil(n_nodes * G / 16), n_seq * n_kv_heads * B *
+ * ((max_cache_len + n_nodes) / 16 + 64) below 2^31.  n_seq = 0 does nothing.
  * The workspace takes partial results where long caches are shared out over workgroups.  Without it, or
  * with less than the query asks for, the call returns REFORM_ERR_WORKSPACE.  Results depend on the batch
  * that a sequence is computed in by rounding only (fp32 sums of the same terms in another order) and are
@@ -538,7 +540,7 @@ reform_status reform_tree_attend(const reform_tree_desc *desc, const void *q, co
  *     next_token   [n_seq] int32 out: target of the path's last node, may be NULL
  *     new_len      [n_seq] int32 out: cache_len + accepted, may be NULL; must not be cache_len itself
  * Supported: n_nodes in [1, 64]; head_dim * sizeof(element) a multiple of 16, at most 4096 bytes;
- * n_layers * n_seq * n_kv_heads below 2^30.  n_seq = 0 does nothing.
+ * n_layers * n_seq * n_kv_heads at most 2^22.  n_seq = 0 does nothing.
  */
 typedef struct {
     uint32_t struct_size;

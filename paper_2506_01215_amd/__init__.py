@@ -9,4 +9,5 @@ from . import binding  # noqa: F401
 from .binding import (  # noqa: F401
     ReformError, load_library, library_path,
     reform_chunk_attend_score, reform_evict_topk_compact, reform_gather_topk,
+    reform_rotary_embed, reform_prompt_attend, reform_tree_attend, reform_tree_accept,
 )

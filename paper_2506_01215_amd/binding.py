@@ -439,7 +439,14 @@ def _packer(cls):
 
 
 _pack_rotary, _pack_prompt, _pack_tree, _pack_accept = map(_packer, (RotaryDesc, PromptDesc, TreeDesc, AcceptDesc))
-_DTYPES = {torch.float32: REFORM_F32, torch.bfloat16: REFORM_BF16}
+
+
+class _Codes(dict):
+    def __missing__(self, dtype):
+        raise TypeError(f"unsupported dtype {dtype}")
+
+
+_DTYPES = _Codes({torch.float32: REFORM_F32, torch.bfloat16: REFORM_BF16})
 _I32 = torch.int32
 
 
@@ -466,12 +473,39 @@ def _i32(t, n, dev, what):
         return None
     if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what}: {n} contiguous int32 expected")
-    return _at(t, dev)
+    if t.get_device() != dev:
+        raise ValueError("all tensors have to be on the current GPU")
+    return t.data_ptr()
 
 
-def _require(ok, what):
-    if not ok:
-        raise ValueError(what)
+def _stream_of(stream, dev):
+    """As _stream, for the current device's index."""
+    if stream is None and _RAW_STREAM is not None:
+        return _RAW_STREAM(dev)
+    return _stream(stream)
+
+
+def _new(make, shape, dtype, device, stream):
+    """A tensor that the call fills: made on the stream that the call runs on, so that nothing of another stream is still
+    using its memory and its own clearing comes first."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=device)
+
+
+def _scratch(query, desc, dev, workspace, first, stream):
+    """As _workspace, with the caller's one checked and a missing one made on the call's stream."""
+    if workspace is None:
+        nbytes = query(desc)
+        if nbytes == 0:
+            return None, 0
+        workspace = _new(torch.empty, (nbytes + 256,), torch.uint8, first.device, stream)
+        if stream is not None:
+            workspace.record_stream(stream)
+    elif workspace.get_device() != dev:
+        raise ValueError("all tensors have to be on the current GPU")
+    return _workspace(query, desc, None, workspace)
 
 
 ROPE_SCALING = {None: 0, "none": 0, "linear": 1, "base": 2, "parts": 3, "bands": 4}
@@ -487,64 +521,83 @@ def reform_rotary_embed(q, k, v, pos, theta=10000.0, rotary_dim=None, interleave
     Returns (q_out, k_out, v_out)."""
     lib = load_library()
     mode = ROPE_SCALING.get(scaling)
-    _require(mode is not None, f"scaling {scaling!r}: one of {list(ROPE_SCALING)}")
+    if mode is None:
+        raise ValueError(f"scaling {scaling!r}: one of {list(ROPE_SCALING)}")
     first = k if q is None else q
-    _require(first is not None and (v is None or k is not None), "queries, or keys with or without values")
+    if first is None or (k is None and v is not None):
+        raise ValueError("queries, or keys with or without values")
     dtype = first.dtype
-    _, n, d = first.shape
-    hq = hkv = block_len = n_blocks = block_stride = 0
+    shape = first.shape
+    hkv = block_len = n_blocks = block_stride = 0
     qs = ks = vs = qos = kvos = (0, 0, 1)
     if q is not None:
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
-        hq = q.shape[0]
+            q_out = _new(torch.empty, shape, dtype, q.device, stream)
+        hq, n, d = shape
         qs, qos = q.stride(), q_out.stride()
-        _require(q_out.shape == q.shape and q_out.dtype is dtype and qs[2] == qos[2] == 1, "q_out: like q, elements of a row contiguous")
+        if q_out.shape != shape or q_out.dtype is not dtype or qs[2] != 1 or qos[2] != 1:
+            raise ValueError("q_out: like q, elements of a row contiguous")
     else:
-        _require(q_out is None, "q_out without q")
+        hq, (_, n, d) = 0, shape
+        if q_out is not None:
+            raise ValueError("q_out without q")
     if k is not None:
-        hkv, nk, dk = k.shape
-        _require(nk == n and dk == d and k.dtype is dtype, "k: as many rows and elements as q, same type")
+        kshape = k.shape
+        hkv = kshape[0]
+        if kshape[1] != n or kshape[2] != d or k.dtype is not dtype:
+            raise ValueError("k: as many rows and elements as q, same type")
         if slot is None:
             if k_out is None:
-                k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
+                k_out = _new(torch.empty, kshape, dtype, k.device, stream)
             if v_out is None and v is not None:
-                v_out = torch.empty(v.shape, dtype=dtype, device=v.device)
-            _require(k_out.shape == k.shape, "k_out: like k")
+                v_out = _new(torch.empty, kshape, dtype, v.device, stream)
+            oshape, kvos = k_out.shape, k_out.stride()
+            if oshape != kshape:
+                raise ValueError("k_out: like k")
         else:
-            _require(k_out is not None and k_out.dim() in (3, 4), "slots need caches [heads, rows, d] or [blocks, heads, rows, d]")
-            shape = k_out.shape
-            _require(shape[-3] == hkv and shape[-1] == d, "caches with other heads or elements than k")
-            block_len = shape[-2]
-            n_blocks, block_stride = (shape[0], k_out.stride(0)) if len(shape) == 4 else (1, 0)
-        ks, kvos = k.stride(), k_out.stride()[-3:]
-        _require(k_out.dtype is dtype and ks[2] == kvos[2] == 1, "k_out: k's type, elements of a row contiguous")
-    else:
-        _require(k_out is None, "k_out without k")
-    if v is not None:
-        vs = v.stride()
-        _require(v.shape == k.shape and v.dtype is dtype and vs[2] == 1 and v_out is not None, "v: like k, and a v_out")
-        _require(v_out.shape == k_out.shape and v_out.stride() == k_out.stride() and v_out.dtype is dtype, "v_out: like k_out")
-    else:
-        _require(v_out is None, "v_out without v")
+            if k_out is None or k_out.dim() not in (3, 4):
+                raise ValueError("slots need caches [heads, rows, d] or [blocks, heads, rows, d]")
+            oshape, kvos = k_out.shape, k_out.stride()
+            n_blocks = 1
+            if len(oshape) == 4:
+                n_blocks, block_stride = oshape[0], kvos[0]
+            block_len = oshape[-2]
+            if oshape[-3] != hkv or oshape[-1] != d:
+                raise ValueError("caches with other heads or elements than k")
+        ks = k.stride()
+        if k_out.dtype is not dtype or ks[2] != 1 or kvos[-1] != 1:
+            raise ValueError("k_out: k's type, elements of a row contiguous")
+        if v is not None:
+            vs = v.stride()
+            if v_out is None or v.shape != kshape or v.dtype is not dtype or vs[2] != 1:
+                raise ValueError("v: like k, and a v_out")
+            if v_out.shape != oshape or v_out.stride() != kvos or v_out.dtype is not dtype:
+                raise ValueError("v_out: like k_out")
+        elif v_out is not None:
+            raise ValueError("v_out without v")
+    elif k_out is not None or v_out is not None:
+        raise ValueError("k_out or v_out without k")
     desc = _pack_rotary(_DTYPES[dtype], n, hq, hkv, d, d if rotary_dim is None else rotary_dim, 1 if interleaved else 0,
                         1 if inverse else 0, mode, theta, factor, turns_high, turns_low, original_len, magnitude, block_len,
-                        n_blocks, block_stride, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], qos[0], qos[1], kvos[0], kvos[1])
+                        n_blocks, block_stride, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], qos[0], qos[1], kvos[-3], kvos[-2])
     dev = _gpu(first)
     rc = lib.reform_rotary_embed(desc, _at(q, dev), _at(k, dev), _at(v, dev), _i32(pos, n, dev, "pos"), _i32(slot, n, dev, "slot"),
-                                 _at(q_out, dev), _at(k_out, dev), _at(v_out, dev), _stream(stream))
+                                 _at(q_out, dev), _at(k_out, dev), _at(v_out, dev), _stream_of(stream, dev))
     _check(rc, "reform_rotary_embed")
     return q_out, k_out, v_out
 
 
 def _prompt_fields(q, k, v, out, n_seq, scale):
-    Hq, nq, d = q.shape
-    Hkv, nk, dk = k.shape
-    dtype = q.dtype
+    shape, kshape, dtype = q.shape, k.shape, q.dtype
+    Hq, nq, d = shape
+    Hkv, nk, dk = kshape
     qs, ks, vs, os = q.stride(), k.stride(), v.stride(), out.stride()
-    _require(dk == d and v.shape == k.shape and out.shape == q.shape, "shapes of q, k, v and out")
-    _require(k.dtype is dtype and v.dtype is dtype and out.dtype is dtype, "types of q, k, v and out")
-    _require(qs[2] == ks[2] == vs[2] == os[2] == 1, "elements of a row have to be contiguous")
+    if dk != d or v.shape != kshape or out.shape != shape:
+        raise ValueError("shapes of q, k, v and out")
+    if k.dtype is not dtype or v.dtype is not dtype or out.dtype is not dtype:
+        raise ValueError("types of q, k, v and out")
+    if qs[2] != 1 or ks[2] != 1 or vs[2] != 1 or os[2] != 1:
+        raise ValueError("elements of a row have to be contiguous")
     return (_DTYPES[dtype], Hq, Hkv, d, n_seq, nq, nk, scale, 0, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os[0], os[1])
 
 
@@ -558,30 +611,35 @@ def reform_prompt_attend(q, k, v, cu_q, scale, cu_k=None, out=None, lse=None, wo
     keys.  Returns (out, lse [Hq, nq])."""
     lib = load_library()
     if out is None:
-        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        out = _new(torch.zeros, q.shape, q.dtype, q.device, stream)
     if lse is None:
-        lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
+        lse = _new(torch.zeros, q.shape[:2], torch.float32, q.device, stream)
     n = cu_q.numel()
     fields = _prompt_fields(q, k, v, out, n - 1, scale)
-    _require(n >= 1 and (cu_k is not None or fields[6] == fields[5]), "cu_k is needed where there are more or fewer key rows")
-    _require(lse.dtype is torch.float32 and lse.is_contiguous() and lse.numel() == fields[1] * fields[5], "lse: [heads, rows] fp32")
+    if n < 1 or (cu_k is None and fields[6] != fields[5]):
+        raise ValueError("cu_k is needed where there are more or fewer key rows")
+    if lse.dtype is not torch.float32 or lse.numel() != fields[1] * fields[5] or not lse.is_contiguous():
+        raise ValueError("lse: [heads, rows] fp32")
     dev = _gpu(q)
     desc = _pack_prompt(*fields)
-    ws, ws_bytes = _workspace(lib.reform_prompt_attend_workspace, desc, q.device, workspace, stream)
+    ws, ws_bytes = _scratch(lib.reform_prompt_attend_workspace, desc, dev, workspace, q, stream)
     rc = lib.reform_prompt_attend(desc, q.data_ptr(), _at(k, dev), _at(v, dev), _i32(cu_q, n, dev, "cu_q"),
-                                  _i32(cu_k, n, dev, "cu_k"), _at(out, dev), _at(lse, dev), ws, ws_bytes, _stream(stream))
+                                  _i32(cu_k, n, dev, "cu_k"), _at(out, dev), _at(lse, dev), ws, ws_bytes, _stream_of(stream, dev))
     _check(rc, "reform_prompt_attend")
     return out, lse
 
 
 def _tree_fields(q, k, v, out, scale, max_cache_len):
-    S, Hq, T, d = q.shape
-    Sk, Hkv, cap, dk = k.shape
-    dtype = q.dtype
+    shape, kshape, dtype = q.shape, k.shape, q.dtype
+    S, Hq, T, d = shape
+    Sk, Hkv, cap, dk = kshape
     qs, ks, os = q.stride(), k.stride(), out.stride()
-    _require(Sk == S and dk == d and v.shape == k.shape and v.stride() == ks and out.shape == q.shape, "shapes of q, k, v and out")
-    _require(k.dtype is dtype and v.dtype is dtype and out.dtype is dtype, "types of q, k, v and out")
-    _require(qs[3] == os[3] == ks[3] == 1 and (ks[2] == d or cap == 1), "contiguous elements, and rows of the caches")
+    if Sk != S or dk != d or v.shape != kshape or v.stride() != ks or out.shape != shape:
+        raise ValueError("shapes of q, k, v and out")
+    if k.dtype is not dtype or v.dtype is not dtype or out.dtype is not dtype:
+        raise ValueError("types of q, k, v and out")
+    if qs[3] != 1 or os[3] != 1 or ks[3] != 1 or (ks[2] != d and cap != 1):
+        raise ValueError("elements of a row, and rows of the caches, have to be contiguous")
     return (_DTYPES[dtype], S, Hq, Hkv, d, T, cap - T if max_cache_len is None else max_cache_len, cap, scale,
             qs[0], qs[1], qs[2], os[0], os[1], os[2], ks[0], ks[1])
 
@@ -597,18 +655,19 @@ def reform_tree_attend(q, k, v, cache_len, scale, parent=None, node_count=None, 
     (None: T each).  max_cache_len bounds cache_len (None: cap - T).  Returns (out, lse [S, Hq, T])."""
     lib = load_library()
     if out is None:
-        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        out = _new(torch.zeros, q.shape, q.dtype, q.device, stream)
     if lse is None:
-        lse = torch.zeros(q.shape[:3], dtype=torch.float32, device=q.device)
+        lse = _new(torch.zeros, q.shape[:3], torch.float32, q.device, stream)
     fields = _tree_fields(q, k, v, out, scale, max_cache_len)
     S, T = fields[1], fields[5]
-    _require(lse.dtype is torch.float32 and lse.is_contiguous() and lse.numel() == S * fields[2] * T, "lse: [sequences, heads, nodes] fp32")
+    if lse.dtype is not torch.float32 or lse.numel() != S * fields[2] * T or not lse.is_contiguous():
+        raise ValueError("lse: [sequences, heads, nodes] fp32")
     dev = _gpu(q)
     desc = _pack_tree(*fields)
-    ws, ws_bytes = _workspace(lib.reform_tree_attend_workspace, desc, q.device, workspace, stream)
+    ws, ws_bytes = _scratch(lib.reform_tree_attend_workspace, desc, dev, workspace, q, stream)
     rc = lib.reform_tree_attend(desc, q.data_ptr(), _at(k, dev), _at(v, dev), _i32(cache_len, S, dev, "cache_len"),
                                 _i32(parent, S * T, dev, "parent"), _i32(node_count, S, dev, "node_count"), _at(out, dev),
-                                _at(lse, dev), ws, ws_bytes, _stream(stream))
+                                _at(lse, dev), ws, ws_bytes, _stream_of(stream, dev))
     _check(rc, "reform_tree_attend")
     return out, lse
 
@@ -620,26 +679,29 @@ def reform_tree_accept(parent, drafted, target, cache_len, k=None, v=None, node_
     lib = load_library()
     S, T = drafted.shape
     if path is None or accepted is None or next_token is None or new_len is None:
-        i32 = dict(dtype=_I32, device=drafted.device)
-        path = torch.empty((S, T), **i32) if path is None else path
-        accepted, next_token, new_len = (torch.empty((S,), **i32) if t is None else t for t in (accepted, next_token, new_len))
+        device = drafted.device
+        path = _new(torch.empty, (S, T), _I32, device, stream) if path is None else path
+        accepted, next_token, new_len = (_new(torch.empty, (S,), _I32, device, stream) if t is None else t
+                                         for t in (accepted, next_token, new_len))
     dtype, Hkv, cap, d, layers, strides = REFORM_F32, 1, (1 << 31) - 1, 4, 1, (0, 0, 0)
     if k is not None:
         shape, ks = k.shape, k.stride()
-        _require(len(shape) in (4, 5) and v is not None and v.shape == shape and v.stride() == ks and v.dtype is k.dtype, "k and v: alike, 4 or 5 dimensions")
+        if len(shape) not in (4, 5) or v is None or v.shape != shape or v.stride() != ks or v.dtype is not k.dtype:
+            raise ValueError("k and v: alike, 4 or 5 dimensions")
         Hkv, cap, d = shape[-3:]
-        _require(shape[-4] == S and ks[-1] == 1 and (ks[-2] == d or cap == 1), "caches of other sequences, or rows not contiguous")
+        if shape[-4] != S or ks[-1] != 1 or (ks[-2] != d and cap != 1):
+            raise ValueError("caches of other sequences, or rows not contiguous")
         dtype = _DTYPES[k.dtype]
         layers, strides = (shape[0], (ks[1], ks[2], ks[0])) if len(shape) == 5 else (1, (ks[0], ks[1], 0))
-    else:
-        _require(v is None, "v without k")
+    elif v is not None:
+        raise ValueError("v without k")
     dev = _gpu(drafted)
     n = S * T
     rc = lib.reform_tree_accept(_pack_accept(dtype, S, Hkv, d, T, cap, layers, *strides), _i32(parent, n, dev, "parent"),
                                 _i32(drafted, n, dev, "drafted"), _i32(target, n, dev, "target"), _i32(cache_len, S, dev, "cache_len"),
                                 _i32(node_count, S, dev, "node_count"), _at(k, dev), _at(v, dev), _i32(path, n, dev, "path"),
                                 _i32(accepted, S, dev, "accepted"), _i32(next_token, S, dev, "next_token"),
-                                _i32(new_len, S, dev, "new_len"), _stream(stream))
+                                _i32(new_len, S, dev, "new_len"), _stream_of(stream, dev))
     _check(rc, "reform_tree_accept")
     return path, accepted, next_token, new_len
 

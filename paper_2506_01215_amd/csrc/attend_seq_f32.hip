@@ -37,27 +37,60 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const SeqKeys &s, 
     const int lim = s.shift + at;
     if (TREE) line = ((unsigned long long)(unsigned)__shfl((int)(line >> 32), at) << 32) | (unsigned)__shfl((int)line, at);
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    // elements behind the head's last one count as 0: loaded from the row's start, so that no load hangs on a branch
+    auto quad = [&](const float *from, int a) {
+        const bool in = 16 * a + 4 * lg < D;
+        const f32x4 x = *(const f32x4 *)(from + (in ? 16 * a : -4 * lg));
+        return in ? x : zero;
+    };
     f32x4 q[NA], o[NA];
     {
         const float *src = (const float *)r.q + (size_t)(row % r.G) * r.q_hs + (size_t)at * r.q_rs + 4 * lg;
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-            q[a] = 16 * a + 4 * lg < D ? *(const f32x4 *)(src + 16 * a) : zero;
+            q[a] = quad(src, a);
             o[a] = zero;
         }
     }
     float m = -INFINITY, l = 0.f;
     const float c = scale * kLog2e;
-    for (int t = t0 + wave; t < t1; t += kF32Waves) {
+    // K of the next tile and V of this one are on their way while the tile's logits are formed (rows of up to 128
+    // elements: there are no registers for it beyond)
+    constexpr bool AHEAD = DP <= 128;
+    f32x4 k[NA];
+    auto load_keys = [&](int t) {
+        const float *kr = (const float *)s.k + (size_t)min(t * kF32Keys + ln, s.n - 1) * s.k_rs + 4 * lg;
+#pragma unroll
+        for (int a = 0; a < NA; ++a) k[a] = quad(kr, a);
+    };
+    int t = t0 + wave;
+    if (AHEAD && t < t1) load_keys(t);
+    // as in seq_segment: Q has to be there before the loop
+#pragma unroll
+    for (int a = 0; a < NA; ++a) asm volatile("" : "+v"(q[a]));
+    for (; t < t1; t += kF32Waves) {
         const int j0 = t * kF32Keys;
-        const float *kr = (const float *)s.k + (size_t)min(j0 + ln, s.n - 1) * s.k_rs + 4 * lg;
+        if (!AHEAD) load_keys(t);
+        float v[4][NA];
+        auto load_values = [&](int e) {
+            const float *vr = (const float *)s.v + (size_t)min(j0 + 4 * lg + e, s.n - 1) * s.v_rs + ln;
+#pragma unroll
+            for (int a = 0; a < NA; ++a) {
+                const bool in = 16 * a + ln < D;
+                const float x = vr[in ? 16 * a : -ln];
+                v[e][a] = in ? x : 0.f;
+            }
+        };
+        if (AHEAD) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) load_values(e);
+        }
         f32x4 x = zero;
 #pragma unroll
-        for (int a = 0; a < NA; ++a) {
-            const f32x4 k = 16 * a + 4 * lg < D ? *(const f32x4 *)(kr + 16 * a) : zero;
+        for (int a = 0; a < NA; ++a)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q[a][e], x, 0, 0, 0);
-        }
+            for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(k[a][e], q[a][e], x, 0, 0, 0);
+        if (AHEAD && t + kF32Waves < t1) load_keys(t + kF32Waves);
         if (j0 + kF32Keys - 1 >= s.open) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -81,12 +114,9 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const SeqKeys &s, 
         for (int a = 0; a < NA; ++a) o[a] *= alpha;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float *vr = (const float *)s.v + (size_t)min(j0 + 4 * lg + e, s.n - 1) * s.v_rs + ln;
+            if (!AHEAD) load_values(e);
 #pragma unroll
-            for (int a = 0; a < NA; ++a) {
-                const float v = 16 * a + ln < D ? vr[16 * a] : 0.f;
-                o[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[e], o[a], 0, 0, 0);
-            }
+            for (int a = 0; a < NA; ++a) o[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][a], p[e], o[a], 0, 0, 0);
         }
     }
     // the waves' sums, as in seq_segment

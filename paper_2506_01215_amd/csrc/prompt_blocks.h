@@ -49,7 +49,11 @@ __device__ __forceinline__ PromptBlock prompt_block(const PromptParams &p, int i
     const int lane = threadIdx.x & 63;
     PromptSeq s = {0, 0, 0, 0, 0};
     int rb;
-    if (p.n_seq <= 64) {
+    if (p.n_seq == 1) {                                  // late (long) ones first
+        s = prompt_seq<ROWS>(p, 0);
+        rb = s.blocks - 1 - idx;
+        if (rb < 0) return {-1, 0, 0, 0, 0, 0};
+    } else if (p.n_seq <= 64) {
         if (lane < p.n_seq) s = prompt_seq<ROWS>(p, lane);
         auto count = [&](int tiles, int &mine) {
             mine = prompt_blocks_with<ROWS, TK>(p, s, tiles);

@@ -47,6 +47,7 @@ reform_status check_heads(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t dim,
     return REFORM_OK;
 }
 
+constexpr double kMaxGroups = 8388607.0;                 // workgroups of 512 threads in a grid
 constexpr int64_t kMaxRowStride = 1 << 24;               // offsets inside a tile of 64 rows stay within 32 bits
 
 reform_status check_prompt(const reform_prompt_desc *d)
@@ -62,8 +63,9 @@ reform_status check_prompt(const reform_prompt_desc *d)
         if (s < 0 || (s * es) % 16) return REFORM_ERR_INVALID_ARG;
     if (bad_out_strides(d->o_head_stride, d->o_row_stride, d->n_q_heads, d->n_q_rows, d->head_dim)) return REFORM_ERR_INVALID_ARG;
     if (rc != REFORM_OK) return rc;
-    if (d->n_seq > 65536 || (int64_t)d->n_q_heads * d->n_q_rows >= (1ll << 30) || (int64_t)d->n_kv_heads * d->n_k_rows >= (1ll << 30))
-        return REFORM_ERR_UNSUPPORTED;
+    if (d->n_seq > 65536 || (int64_t)d->n_kv_heads * d->n_k_rows >= (1ll << 30)) return REFORM_ERR_UNSUPPORTED;
+    // workgroups of up to 512 threads, of which a grid has fewer than 2^32
+    if ((double)d->n_q_heads * d->n_q_rows / 16.0 + (double)d->n_kv_heads * d->n_seq > kMaxGroups) return REFORM_ERR_UNSUPPORTED;
     if (d->k_row_stride >= kMaxRowStride || d->v_row_stride >= kMaxRowStride) return REFORM_ERR_UNSUPPORTED;
     return REFORM_OK;
 }
@@ -102,6 +104,7 @@ reform_status check_tree(const reform_tree_desc *d)
     if (rc != REFORM_OK) return rc;
     if (d->n_nodes > 64) return REFORM_ERR_UNSUPPORTED;
     // the list of all key tiles is counted in 32 bits (tree_list.h): 16 rows and 16 keys are the smallest blocks and tiles
+    if ((double)d->n_seq * d->n_q_heads * d->n_nodes > 4194304.0) return REFORM_ERR_UNSUPPORTED;
     const double blocks = std::ceil((double)d->n_nodes * (d->n_q_heads / d->n_kv_heads) / 16.0);
     if ((double)d->n_seq * d->n_kv_heads * blocks * (((double)d->max_cache_len + d->n_nodes) / 16.0 + 64.0) >= 2147483648.0)
         return REFORM_ERR_UNSUPPORTED;
@@ -234,6 +237,7 @@ reform_status reform_rotary_embed(const reform_rotary_desc *d, const void *q, co
     for (const void *x : {q, k, v, (const void *)q_out, (const void *)k_out, (const void *)v_out})
         if (!aligned16(x)) return REFORM_ERR_UNSUPPORTED;
     if ((int64_t)d->n_q_heads + 2 * (int64_t)d->n_kv_heads > 65535) return REFORM_ERR_UNSUPPORTED;
+    if ((double)d->n_tokens * (d->head_dim * es / 16) >= 2147483648.0) return REFORM_ERR_UNSUPPORTED;     // a thread for two pieces at least
     if (!work) return REFORM_OK;
     RotaryParams p;
     std::memset(&p, 0, sizeof(p));
@@ -316,7 +320,7 @@ reform_status reform_tree_accept(const reform_accept_desc *d, const int32_t *par
     if (k && ((d->kv_seq_stride * es) % 16 || (d->kv_head_stride * es) % 16 || (d->kv_layer_stride * es) % 16 ||
               !aligned16(k) || !aligned16(v)))
         return REFORM_ERR_UNSUPPORTED;
-    if ((double)d->n_layers * d->n_seq * d->n_kv_heads >= (double)(1 << 30)) return REFORM_ERR_UNSUPPORTED;
+    if ((double)d->n_layers * d->n_seq * d->n_kv_heads > 4194304.0) return REFORM_ERR_UNSUPPORTED;
     AcceptParams p;
     std::memset(&p, 0, sizeof(p));
     p.parent = parent; p.drafted = drafted; p.target = target; p.cache_len = cache_len; p.node_count = node_count;

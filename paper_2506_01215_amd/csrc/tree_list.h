@@ -39,6 +39,7 @@ __device__ __forceinline__ int tree_all_places(const TreeParams &p, const TreeSe
 template <int R, int TK>
 struct TreeList {
     int total, shares;                   // places, shares that are not empty
+    int each, more;                      // places of a share; the first `more` shares have one place more
     TreeSeq lane;                        // sequence `lane`
     int lane_places;                     // and its places
 
@@ -61,11 +62,16 @@ struct TreeList {
             total += __builtin_amdgcn_readlane(wave_incl_scan(mine), 63);
             items += __builtin_amdgcn_readlane(wave_incl_scan(tree_items(p, s)), 63);
         }
-        shares = max(1, min(p.shares, max(items, total / p.least)));
+        shares = max(1, min(p.shares, max(items, total / max(p.least, 1))));
+        each = (int)((unsigned)total / (unsigned)shares);
+        more = total - each * shares;
     }
-    __device__ __forceinline__ int begin(int share) const { return (int)((long)total * share / shares); }
-    // the share that place x lies in: begin(w) <= x  <=>  w total / shares < x + 1
-    __device__ __forceinline__ int share_of(int x) const { return (int)((((long)x + 1) * shares - 1) / total); }
+    __device__ __forceinline__ int begin(int share) const { return share * each + min(share, more); }
+    __device__ __forceinline__ int share_of(int x) const           // the share that place x lies in
+    {
+        const int y = x - more * (each + 1);
+        return y < 0 ? (int)((unsigned)x / (unsigned)(each + 1)) : more + (int)((unsigned)y / (unsigned)each);
+    }
     // sequence b (the same in all lanes)
     __device__ __forceinline__ TreeSeq seq(const TreeParams &p, int b) const
     {

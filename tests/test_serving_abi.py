@@ -60,6 +60,7 @@ def test_rotary_rejects_scalings_pointers_and_slots():
                    (dict(block_stride=2 * 64 * 128 + 4), 2), (dict(kv_out_head_stride=128), 1),
                    (dict(block_len=1 << 20, n_blocks=1 << 12, kv_out_head_stride=1 << 27), 2)):
         assert call_rotary(rotary(**{**ok, **kw}), slot=FAKE) == rc, kw
+    assert call_rotary(rotary(n_tokens=1 << 28, q_out_head_stride=1 << 40, kv_out_head_stride=1 << 40)) == 2
     none = rotary(n_tokens=0)
     assert call_rotary(none, None, None, None, None, None, None, None, None) == 0
 
@@ -79,13 +80,15 @@ def call_prompt(d, q=FAKE, k=FAKE, v=FAKE, cu=FAKE, out=FAKE):
     ("struct_size", 4, 1), ("dtype", 3, 1), ("n_kv_heads", 3, 1), ("n_kv_heads", 0, 1), ("n_seq", -1, 1), ("n_q_rows", -1, 1),
     ("n_k_rows", -1, 1), ("scale", 0.0, 1), ("scale", float("nan"), 1), ("reserved", 1, 1), ("q_head_stride", -8, 1),
     ("k_row_stride", 132, 1), ("o_row_stride", 64, 1), ("o_head_stride", 128, 1), ("head_dim", 96, 2), ("head_dim", 256, 2),
-    ("n_seq", 65537, 2), ("n_k_rows", 1 << 29, 2), ("k_row_stride", 1 << 24, 2), ("v_row_stride", 1 << 25, 2),
+    ("n_seq", 65537, 2), ("n_k_rows", 1 << 29, 2), ("n_q_rows", 1 << 24, 2), ("k_row_stride", 1 << 24, 2), ("v_row_stride", 1 << 25, 2),
 ])
 def test_prompt_rejects(field, value, status):
     d = prompt()
     setattr(d, field, value)
     if field == "head_dim":
         d.o_row_stride, d.o_head_stride = 256, 25600
+    if field == "n_q_rows" and value > 0:
+        d.o_head_stride = value * 128
     assert call_prompt(d) == status
 
 
@@ -125,6 +128,7 @@ def test_tree_rejects(field, value, status):
 def test_tree_rejects_pointers_nodes_and_workspaces():
     lib = binding.load_library()
     assert call_tree(tree(n_nodes=65, capacity=6000, o_head_stride=65 * 128)) == 2
+    assert call_tree(tree(n_seq=1 << 17, o_seq_stride=1 << 20)) == 2
     for kw in (dict(q=None), dict(k=None), dict(v=None), dict(lens=None), dict(out=None), dict(k=FAKE + 8)):
         assert call_tree(tree(), **kw) == 1
     need = lib.reform_tree_attend_workspace(ctypes.byref(tree()))
@@ -164,7 +168,7 @@ def test_accept_rejects_pointers():
         assert call_accept(accept(), **kw) == 1
     assert call_accept(accept(), k=FAKE + 8) == 2
     assert call_accept(accept(head_dim=4096, capacity=8, kv_head_stride=1 << 20, kv_seq_stride=1 << 24)) == 2
-    assert call_accept(accept(n_seq=1 << 28, kv_seq_stride=1 << 20, n_kv_heads=8)) == 2
+    assert call_accept(accept(n_seq=1 << 20, kv_seq_stride=1 << 20, n_kv_heads=8)) == 2
     assert call_accept(accept(n_seq=0), None, None, None) == 0
 
 
@@ -193,5 +197,9 @@ def test_shapes_are_checked():
         binding.prompt_desc(z(4, 3, 64), z(2, 3, 32), z(2, 3, 32), z(4, 3, 64), i(2), 0.1)
     with pytest.raises(ValueError):
         binding.tree_desc(z(2, 4, 3, 64), z(1, 2, 9, 64), z(1, 2, 9, 64), z(2, 4, 3, 64), 0.1)
+    with pytest.raises(TypeError, match="float16"):
+        binding.reform_rotary_embed(z(4, 3, 64, dtype=torch.float16), None, None, i(3))
+    with pytest.raises(TypeError, match="float16"):
+        binding.prompt_desc(*(z(2, 3, 64, dtype=torch.float16) for _ in range(4)), i(2), 0.1)
     with pytest.raises(ValueError, match="cubic"):
         binding.reform_rotary_embed(z(4, 3, 64), None, None, i(3), q_out=z(4, 3, 64), scaling="cubic")
