@@ -457,7 +457,8 @@ reform_status reform_rotary_embed(const reform_rotary_desc *desc, const void *q,
  *     lse      [n_q_heads][n_q_rows] fp32, may be NULL
  * The lengths are read on the device, so a captured call follows them.  Boundaries outside [0, n_q_rows]
  * or [0, n_k_rows] are moved into it and a descending pair counts as an empty sequence, so that nothing
- * outside the tensors is read or written; sequences must not overlap in q.
+ * outside the tensors is read or written; sequences must not overlap in q.  (Beyond 1024 sequences a cu_q that
+ * descends anywhere leaves it open which of its rows are computed, still with nothing outside touched.)
  * Arithmetic as in reform_chunk_attend_score, bitwise reproducible.  Keys and values that are not finite stay
  * within their sequence; there, rows before such a value may become NaN as well as those that see it (its
  * weight 0 is multiplied with it).  The same holds in reform_tree_attend for the nodes of one sequence.

@@ -9,6 +9,11 @@
 
 namespace reform {
 
+constexpr int kPromptSorted = 64;        // sequences whose blocks are sorted, one to a lane
+// Beyond so many, counting the blocks in front of its own costs a workgroup more than the empty workgroups of places that are found by
+// a search (8 heads of 128 over 2; counted / searched, us): 512 prompts of 32 rows 32 / 48, 2048 of 32 202 / 176, 8192 of 8 1085 / 255.
+constexpr int kPromptCounted = 1024;
+
 struct PromptBlock {
     int rb;                  // block of the sequence, -1: none is left
     int q0, nq, k0, nk;      // the sequence's rows
@@ -53,7 +58,7 @@ __device__ __forceinline__ PromptBlock prompt_block(const PromptParams &p, int i
         s = prompt_seq<ROWS>(p, 0);
         rb = s.blocks - 1 - idx;
         if (rb < 0) return {-1, 0, 0, 0, 0, 0};
-    } else if (p.n_seq <= 64) {
+    } else if (p.n_seq <= kPromptSorted) {
         if (lane < p.n_seq) s = prompt_seq<ROWS>(p, lane);
         auto count = [&](int tiles, int &mine) {
             mine = prompt_blocks_with<ROWS, TK>(p, s, tiles);
@@ -76,7 +81,7 @@ __device__ __forceinline__ PromptBlock prompt_block(const PromptParams &p, int i
         rb = __builtin_amdgcn_readlane(rb, l);
         s = {__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.nq, l), __builtin_amdgcn_readlane(s.k0, l),
              __builtin_amdgcn_readlane(s.nk, l), 0};
-    } else {                 // so many sequences fill the chip in any order
+    } else if (p.n_seq <= kPromptCounted) {              // so many sequences fill the chip in any order: theirs
         int sum = 0;
         for (int s0 = 0;; s0 += 64) {
             if (s0 >= p.n_seq) return {-1, 0, 0, 0, 0, 0};
@@ -92,6 +97,18 @@ __device__ __forceinline__ PromptBlock prompt_block(const PromptParams &p, int i
             }
             sum += all;
         }
+    } else {
+        // sequence s has the places from front(s) on, at least as many as its rows can make blocks: found by 64 lanes at a time
+        auto front = [&](int x) { return min(max(p.cu_q[x], 0), p.n_q) * p.G / ROWS + x; };
+        int at = 0;
+        for (int step = p.n_seq > 4096 ? 4096 : 64; step > 0; step /= 64) {
+            const int x = at + lane * step;
+            const int fit = __builtin_popcountll(__builtin_amdgcn_ballot_w64(x < p.n_seq && front(min(x, p.n_seq - 1)) <= idx));
+            at += step * (max(fit, 1) - 1);
+        }
+        s = prompt_seq<ROWS>(p, at);
+        rb = s.blocks - 1 - (idx - front(at));           // late ones first
+        if (rb < 0 || rb >= s.blocks) return {-1, 0, 0, 0, 0, 0};
     }
     const int last = s.nk - s.nq + (min((rb + 1) * ROWS, s.nq * p.G) - 1) / p.G;         // last key that the block sees
     // the same in every lane; said here, since the compiler would keep them and all that follows in vector registers
@@ -120,7 +137,7 @@ __device__ __forceinline__ void prompt_block_operands(const PromptParams &p, con
 // Workgroups that the blocks of any lengths fit: every sequence has at most one block that is not full.
 inline unsigned prompt_grid(const PromptParams &p, int rows)
 {
-    const long full = (long)p.n_q * p.G / rows, part = p.n_seq < p.n_q ? p.n_seq : p.n_q;
+    const long full = (long)p.n_q * p.G / rows, part = p.n_seq > kPromptCounted || p.n_seq < p.n_q ? p.n_seq : p.n_q;
     return (unsigned)((full + part) * p.Hkv);
 }
 

@@ -50,18 +50,19 @@ struct TreeList {
         s = tree_seq<R, TK>(p, b);
         return tree_all_places(p, s);
     }
-    __device__ __forceinline__ explicit TreeList(const TreeParams &p)
+    __device__ __forceinline__ void read(const TreeParams &p)
     {
         const int l = threadIdx.x & 63;
         lane_places = load(p, l, lane);
-        total = __builtin_amdgcn_readlane(wave_incl_scan(lane_places), 63);
-        int items = __builtin_amdgcn_readlane(wave_incl_scan(tree_items(p, lane)), 63);
-        for (int b0 = 64; b0 < p.n_seq; b0 += 64) {
+        int places = lane_places, items = tree_items(p, lane);
+#pragma unroll 4
+        for (int b = 64 + l; b < p.n_seq; b += 64) {
             TreeSeq s;
-            const int mine = load(p, b0 + l, s);
-            total += __builtin_amdgcn_readlane(wave_incl_scan(mine), 63);
-            items += __builtin_amdgcn_readlane(wave_incl_scan(tree_items(p, s)), 63);
+            places += load(p, b, s);
+            items += tree_items(p, s);
         }
+        total = __builtin_amdgcn_readlane(wave_incl_scan(places), 63);
+        items = __builtin_amdgcn_readlane(wave_incl_scan(items), 63);
         shares = max(1, min(p.shares, max(items, total / max(p.least, 1))));
         each = (int)((unsigned)total / (unsigned)shares);
         more = total - each * shares;
@@ -83,39 +84,54 @@ struct TreeList {
     __device__ __forceinline__ int before(const TreeParams &p, int b) const
     {
         const int l = threadIdx.x & 63;
-        int sum = __builtin_amdgcn_readlane(wave_incl_scan(l < b ? lane_places : 0), 63);
-        for (int b0 = 64; b0 < b; b0 += 64) {
+        int places = l < b ? lane_places : 0;
+#pragma unroll 4
+        for (int x = 64 + l; x < b; x += 64) {
             TreeSeq s;
-            const int mine = b0 + l < b ? load(p, b0 + l, s) : 0;
-            sum += __builtin_amdgcn_readlane(wave_incl_scan(mine), 63);
+            places += load(p, x, s);
         }
-        return sum;
+        return __builtin_amdgcn_readlane(wave_incl_scan(places), 63);
     }
     // the sequence that place x (< total) lies in, and its first place
     __device__ __forceinline__ int find(const TreeParams &p, int x, int &first) const
     {
-        int sum = 0, mine = lane_places;
-        for (int b0 = 0;; b0 += 64) {
-            const int incl = wave_incl_scan(mine), all = __builtin_amdgcn_readlane(incl, 63);
+        const int l = threadIdx.x & 63;
+        int sum = 0, mine[4] = {lane_places, 0, 0, 0};
+        for (int b0 = 0, n = 1;; b0 += 64 * n, n = 4) {  // n sequences to a lane
+            if (b0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    TreeSeq s;
+                    mine[i] = load(p, b0 + 4 * l + i, s);
+                }
+            }
+            const int own = mine[0] + mine[1] + mine[2] + mine[3], incl = wave_incl_scan(own), all = __builtin_amdgcn_readlane(incl, 63);
             if (x < sum + all) {
-                const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(x < sum + incl));
-                first = sum + __builtin_amdgcn_readlane(incl - mine, l);
-                return b0 + l;
+                const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(x < sum + incl));
+                first = sum + __builtin_amdgcn_readlane(incl - own, at);
+                int b = b0 + n * at;
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    const int places = __builtin_amdgcn_readlane(mine[i], at);
+                    if (x < first + places) return b;
+                    first += places;
+                    ++b;
+                }
+                return b;
             }
             sum += all;
-            TreeSeq s;
-            mine = load(p, b0 + 64 + (threadIdx.x & 63), s);
         }
     }
 };
 
-// Share and row block of a workgroup.  Workgroups go to the eight XCDs in turn, so those of one share are eight apart.
-__device__ __forceinline__ int tree_share(const TreeParams &p, int block, int shares, int &rb)
+// Share of a workgroup, and which one of the share's `side` workgroups it is.  Workgroups go to the eight XCDs in turn, so those of
+// one share are eight apart.
+__device__ __forceinline__ int tree_share(int block, int shares, int side, int &which)
 {
-    const int each = shares >> 3, even = 8 * each * p.row_blocks;        // shares of an XCD
+    const int each = shares >> 3, even = 8 * each * side;                // shares of an XCD
     const int j = block < even ? block >> 3 : block - even;
-    const int s = j / p.row_blocks;
-    rb = j - s * p.row_blocks;
+    const int s = j / side;
+    which = j - s * side;
     return block < even ? (block & 7) * each + s : 8 * each + s;
 }
 
@@ -147,7 +163,7 @@ __device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
         f(r, k, t0, t1, slot);
     };
     const bool whole = p.shares == 0;                    // one item to a workgroup
-    const TreeList<R, TK> list(p);
+    TreeList<R, TK> list;
     int b, kvh, pos = 0, begin = 0, end, share = 0;
     TreeSeq seq;
     if (whole) {
@@ -155,12 +171,13 @@ __device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
         rb = blockIdx.x - item * p.row_blocks;
         b = item / p.Hkv;
         kvh = item - b * p.Hkv;
-        seq = list.seq(p, b);
+        seq = tree_seq<R, TK>(p, b);
         if (rb >= seq.blocks) return;
         end = tree_places(seq);
     } else {
+        list.read(p);
         if ((int)blockIdx.x >= list.shares * p.row_blocks || list.total == 0) return;
-        share = tree_share(p, blockIdx.x, list.shares, rb);
+        share = tree_share(blockIdx.x, list.shares, p.row_blocks, rb);
         begin = list.begin(share);
         end = list.begin(share + 1);
         int first;
@@ -189,30 +206,47 @@ __device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
     }
 }
 
-// The pieces of the items that several shares covered.  A workgroup has `rows` rows (a power of two) of an item; a thread has
+// The pieces of the items that several shares covered.  A workgroup has `rows` rows (a power of two) of the item that the end of its
+// share cuts (by_share), or of an item whether it is cut or not; a thread has
 // four columns of one of them and every n-th piece, which it adds up against the largest reference of its own,
 // references, sums and columns all loaded at once; then the n threads' sums meet in LDS.  The order is that of the
 // shares, whoever is done first.
 constexpr int kTreeMaxShares = 512;
 
 template <int D, int R, int TK, bool BF16>
-__global__ __launch_bounds__(256) void tree_merge(TreeParams p, int rows)
+__global__ __launch_bounds__(256) void tree_merge(TreeParams p, int rows, int by_share)
 {
     constexpr int C4 = D / 4, BATCH = 4;                 // quads of a row, pieces of a trip
     __shared__ f32x4 so[256];
     __shared__ float2 sml[256];
-    const TreeList<R, TK> list(p);
+    TreeList<R, TK> list;
+    list.read(p);
     if (list.total == 0) return;
-    // an item's workgroups on the XCD that most of its shares ran on (tree_share): its L2 holds the pieces
-    const int chunks = (p.part_rows + rows - 1) / rows * p.row_blocks, items = p.n_seq * p.Hkv, each = items >> 3;
-    const int even = 8 * each * chunks, j = (int)blockIdx.x < even ? blockIdx.x >> 3 : blockIdx.x - even;
-    const int item = ((int)blockIdx.x < even ? (blockIdx.x & 7) * each : 8 * each) + j / chunks;
-    const int rb = j % chunks % p.row_blocks, chunk = j % chunks / p.row_blocks;
-    const int b = item / p.Hkv, kvh = item - b * p.Hkv;
-    const TreeSeq seq = list.seq(p, b);
+    const int chunks = (p.part_rows + rows - 1) / rows * p.row_blocks;
+    int b, kvh, pos, rb, w0, own = -1;
+    TreeSeq seq;
+    if (by_share) {                                      // the item that the share's end cuts
+        if ((int)blockIdx.x >= list.shares * chunks) return;
+        own = tree_share(blockIdx.x, list.shares, chunks, rb);
+        const int x = list.begin(own + 1) - 1;
+        b = list.find(p, x, pos);
+        seq = list.seq(p, b);
+        kvh = (x - pos) / tree_places(seq);
+    } else {
+        // an item's workgroups on the XCD that most of its shares ran on (tree_share): its L2 holds the pieces
+        const int item = tree_share(blockIdx.x, p.n_seq * p.Hkv, chunks, rb);
+        b = item / p.Hkv;
+        kvh = item - b * p.Hkv;
+        seq = list.seq(p, b);
+        pos = list.before(p, b);
+    }
+    const int chunk = rb / p.row_blocks;
+    rb -= chunk * p.row_blocks;
     if (rb >= seq.blocks) return;
-    const int pos = list.before(p, b) + kvh * tree_places(seq) + kTreeStart;
-    const int w0 = list.share_of(pos), n = list.share_of(pos + seq.tiles - 1) - w0 + 1;
+    pos += kvh * tree_places(seq) + kTreeStart;
+    w0 = list.share_of(pos);
+    if (by_share && w0 != own) return;
+    const int n = list.share_of(pos + seq.tiles - 1) - w0 + 1;
     const int r0 = chunk * rows, here = min(rows, seq.nodes * p.G - rb * R - r0);
     if (n == 1 || here <= 0) return;
     const int group = rows * C4, groups = 256 / group;   // threads that have different quads
@@ -275,15 +309,19 @@ __global__ __launch_bounds__(256) void tree_merge(TreeParams p, int rows)
     }
 }
 
+// With more items than shares most are finished by one workgroup, so the shares' ends are gone through, else the items (32/8 heads of
+// 128, 30 nodes, caches of up to 2000 rows, us, by share / by item: 512 caches 556 / 690, 16 caches 44 / 36; 8 nodes,
+// 8/2 heads, 8192 caches of 1000 rows 1715 / 3225).
 // One row to a workgroup where that makes no more than some eight workgroups a compute unit, else two, four or more.
 template <int D, int R, int TK, bool BF16>
 inline void tree_merge_launch(const TreeParams &p, hipStream_t st)
 {
-    const long blocks = (long)p.n_seq * p.Hkv * p.row_blocks;
+    const bool by_share = (long)p.n_seq * p.Hkv > p.shares;
+    const long blocks = (by_share ? p.shares : (long)p.n_seq * p.Hkv) * p.row_blocks;
     int rows = 1;
     while (2 * rows <= 1024 / D && rows < p.part_rows && blocks * ((p.part_rows + rows - 1) / rows) > 2048) rows *= 2;
     const unsigned chunks = (p.part_rows + rows - 1) / rows;
-    hipLaunchKernelGGL((tree_merge<D, R, TK, BF16>), dim3((unsigned)blocks * chunks), dim3(256), 0, st, p, rows);
+    hipLaunchKernelGGL((tree_merge<D, R, TK, BF16>), dim3((unsigned)blocks * chunks), dim3(256), 0, st, p, rows, (int)by_share);
 }
 
 // Row blocks, shares and the rows of a piece for blocks of R rows and tiles of TK keys.  No shares where every item is

@@ -187,3 +187,38 @@ def test_runs_are_bitwise_alike_and_lse_may_be_missing():
     rc = binding.load_library().reform_prompt_attend(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), cu.data_ptr(), None,
                                                      out.data_ptr(), None, None, 0, torch.cuda.current_stream().cuda_stream)
     assert rc == 0 and torch.equal(out, first[0])
+
+
+@pytest.mark.parametrize("n,d,dtype", [(1025, 64, BF), (1500, 128, BF), (4500, 64, BF), (1100, 32, F)])
+def test_sequences_that_are_searched(n, d, dtype):
+    """More sequences than are counted one by one, and than one step of the search has lanes for; many of them empty, the first
+    boundary behind rows of no sequence."""
+    rnd = random.Random(n)
+    lens = [rnd.choice([0, 0, 1, 2, rnd.randint(0, 9)]) for _ in range(n)]
+    lens[n // 3], lens[-1] = 150, 70
+    run_case(4, 2, d, lens, lens, dtype, seed=n, spare=5)
+    q_lens = [9] + lens          # the first sequence is left out of the call: its rows keep what they held
+    g = torch.Generator().manual_seed(n)
+    q, k, v = (ref.randn(g, h, sum(q_lens), d, dtype=dtype) for h in (4, 2, 2))
+    cu = i32(starts(q_lens)[1:])
+    out = torch.full(q.shape, KEPT, dtype=dtype, device=DEV)
+    got, lse = binding.reform_prompt_attend(q.to(DEV), k.to(DEV), v.to(DEV), cu, d ** -0.5, out=out)
+    whole, whole_lse = binding.reform_prompt_attend(q.to(DEV)[:, 9:], k.to(DEV)[:, 9:], v.to(DEV)[:, 9:], i32(starts(lens)), d ** -0.5)
+    assert torch.equal(got[:, 9:], whole) and torch.equal(lse[:, 9:], whole_lse) and bool((got[:, :9] == KEPT).all())
+
+
+def test_descending_boundaries_of_many_sequences_touch_nothing_outside():
+    """Where boundaries descend, it is open what rows are computed; the tensors' surroundings stay as they were, and so does the
+    next call's result."""
+    rnd = random.Random(9)
+    g = torch.Generator().manual_seed(9)
+    n, rows = 1400, 600
+    cu = [rnd.choice([-5, 0, rows, 1 << 30, rnd.randint(0, rows)]) for _ in range(n + 1)]
+    held = torch.full((4, rows + 200, 64), KEPT, dtype=BF, device=DEV)
+    q, k, v = (ref.randn(g, h, rows, 64, dtype=BF).to(DEV) for h in (4, 2, 2))
+    out = held[:, 100:100 + rows]
+    binding.reform_prompt_attend(q, k, v, i32(cu), 0.125, out=out)
+    assert bool((held[:, :100] == KEPT).all()) and bool((held[:, 100 + rows:] == KEPT).all())
+    out, lse = binding.reform_prompt_attend(q, k, v, i32([0, rows]), 0.125)
+    want, wl, a, err = ref.prompt_attend(q.cpu(), k.cpu(), v.cpu(), [rows], [rows], 0.125)
+    ref.check_attention(out, lse, want, wl, a, err, rows, BF)

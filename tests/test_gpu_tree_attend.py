@@ -156,3 +156,25 @@ def test_workspace_is_needed_and_results_repeat():
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
     with pytest.raises(binding.ReformError, match="WORKSPACE"):
         binding.reform_tree_attend(q, k, v, lens, 0.1, workspace=ws[:need // 2])
+
+
+@pytest.mark.parametrize("hq,hkv,d,T,n,dtype", [
+    (4, 2, 64, 1, 300, BF), (8, 2, 128, 6, 280, BF), (8, 2, 64, 20, 270, BF),     # 2, 24 and 80 rows, 560 and more items
+    (16, 2, 128, 40, 130, BF), (2, 2, 64, 3, 300, F),                             # 320 rows: two row blocks; fp32
+])
+def test_more_sequences_than_shares(hq, hkv, d, T, n, dtype):
+    """More items than the caches are shared out to workgroups: most are finished by one, and those that a share's end
+    cuts are put together; padded ones among them."""
+    rnd = random.Random(n + T)
+    lens = [rnd.choice([0, 1, 33, rnd.randint(0, 60), rnd.randint(0, 200)]) for _ in range(n)]
+    lens[3], lens[n // 2], lens[-1] = 1500, 1100, 900
+    counts = [rnd.choice([T, T, rnd.randint(0, T)]) for _ in lens]
+    run_case(hq, hkv, d, T, lens, dtype, seed=n, counts=counts)
+
+
+def test_many_short_caches():
+    """One workgroup to a sequence and head, more sequences than a wave has lanes."""
+    rnd = random.Random(5)
+    lens = [rnd.choice([0, 1, 64, rnd.randint(0, 90)]) for _ in range(200)]
+    run_case(4, 2, 64, 2, lens, BF, seed=5, counts=[rnd.randint(0, 2) for _ in lens])
+    run_case(2, 2, 16, 2, lens, F, seed=5)
