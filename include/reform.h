@@ -463,7 +463,7 @@ reform_status reform_rotary_embed(const reform_rotary_desc *desc, const void *q,
  * within their sequence; there, rows before such a value may become NaN as well as those that see it (its
  * weight 0 is multiplied with it).  The same holds in reform_tree_attend for the nodes of one sequence.
  * Supported: REFORM_BF16 with head_dim 64 or 128; REFORM_F32 with head_dim % 4 == 0, <= 256; at most 65536
- * sequences; n_q_heads * n_q_rows / 16 + n_kv_heads * n_seq below 2^23, n_kv_heads * n_k_rows below 2^30; row
+ * sequences; out and lse apart from the inputs; n_q_heads * n_q_rows / 16 + n_kv_heads * n_seq below 2^23, n_kv_heads * n_k_rows below 2^30; row
  * strides of k and v below 2^24.  n_q_rows = 0 does nothing.
  */
 typedef struct {
@@ -500,7 +500,7 @@ reform_status reform_prompt_attend(const reform_prompt_desc *desc, const void *q
  *     node_count [n_seq] int32 in device memory or NULL (all have n_nodes); values outside [0, n_nodes] are
  *                moved into it.  Rows of out and lse from node_count[b] on keep what they held.
  *     lse        [n_seq][n_q_heads][n_nodes] fp32, may be NULL
- * Supported: n_nodes in [1, 64]; types and head_dim as reform_prompt_attend; max_cache_len + n_nodes <=
+ * Supported: n_nodes in [1, 64]; types and head_dim as reform_prompt_attend, out and lse as there; max_cache_len + n_nodes <=
  * capacity; n_seq * n_q_heads * n_nodes at most 2^22; with B = ceil(n_nodes * G / 16), n_seq * n_kv_heads * B *
  * ((max_cache_len + n_nodes) / 16 + 64) below 2^31.  n_seq = 0 does nothing.
  * The workspace takes partial results where long caches are shared out over workgroups.  Without it, or
@@ -540,6 +540,7 @@ reform_status reform_tree_attend(const reform_tree_desc *desc, const void *q, co
  *     accepted     [n_seq] int32 out: nodes on the path, may be NULL
  *     next_token   [n_seq] int32 out: target of the path's last node, may be NULL
  *     new_len      [n_seq] int32 out: cache_len + accepted, may be NULL; must not be cache_len itself
+ * Outputs must not overlap the inputs or one another, nor the caches.
  * Supported: n_nodes in [1, 64]; head_dim * sizeof(element) a multiple of 16, at most 4096 bytes;
  * n_layers * n_seq * n_kv_heads at most 2^22.  n_seq = 0 does nothing.
  */

@@ -23,11 +23,10 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_embed(RotaryParams p, i
     // units: first those that rotate, then those that are copied, two pieces each (the last may have one)
     const int rot_units = ADJACENT ? (rot_pieces + 1) / 2 : rot_pieces / 2;
     const int units = rot_units + (pieces - rot_pieces + 1) / 2;
-    const long gid = (long)blockIdx.x * kRotaryThreads + threadIdx.x;
-    // 32-bit division where it suffices: the 64-bit one is some hundred instructions
-    const long row = gid < (1l << 31) ? (long)((unsigned)gid / (unsigned)units) : gid / units;
-    const bool live = row < p.n;
-    const int token = live ? (int)row : 0, unit = (int)(gid - row * units);
+    const unsigned gid = blockIdx.x * kRotaryThreads + threadIdx.x;      // tokens x units are below 2^31
+    const unsigned row = gid / (unsigned)units;
+    const bool live = row < (unsigned)p.n;
+    const int token = live ? (int)row : 0, unit = (int)(gid - row * (unsigned)units);
     const bool turns = unit < rot_units;
     int a, b;                                            // the unit's pieces; b < 0: it has one
     if (turns) {

@@ -3,8 +3,10 @@
 #include "../../include/reform.h"
 #include "common.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 namespace reform {
 hipError_t rotary_embed_launch(const RotaryParams &p, bool bf16, bool adjacent, hipStream_t st);
@@ -26,14 +28,25 @@ inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 inline int64_t elt_size(int dtype) { return dtype == REFORM_BF16 ? 2 : 4; }
 inline bool known_dtype(int dtype) { return dtype == REFORM_F32 || dtype == REFORM_BF16; }
 
-// Strides of something that is written: rows and heads must not overlap.
-inline bool bad_out_strides(int64_t head, int64_t row, int32_t heads, int32_t rows, int32_t dim)
+struct Walk {
+    int64_t n, step;
+};
+
+// Strides of something that is written: its pieces of `extent` elements, at every combination of the walks' steps, must not
+// overlap.  Sorted by their steps, each walk's step has to pass over all that the ones before it cover.
+bool bad_out_strides(int64_t extent, std::initializer_list<Walk> walks)
 {
-    if (head < 0 || row < 0) return true;
-    if (heads > 1 && head < dim) return true;
-    if (rows > 1 && row < dim) return true;
-    if (heads > 1 && rows > 1) {                         // one of the two walks inside a step of the other
-        if (row <= head ? head < (int64_t)(rows - 1) * row + dim : row < (int64_t)(heads - 1) * head + dim) return true;
+    Walk w[4];
+    int n = 0;
+    for (const Walk &x : walks) {
+        if (x.step < 0) return true;
+        if (x.n > 1) w[n++] = x;
+    }
+    std::sort(w, w + n, [](const Walk &x, const Walk &y) { return x.step < y.step; });
+    double covered = (double)extent;
+    for (int i = 0; i < n; ++i) {
+        if ((double)w[i].step < covered) return true;
+        covered += (double)(w[i].n - 1) * (double)w[i].step;
     }
     return false;
 }
@@ -61,7 +74,7 @@ reform_status check_prompt(const reform_prompt_desc *d)
     const int64_t es = elt_size(d->dtype);
     for (int64_t s : strides)
         if (s < 0 || (s * es) % 16) return REFORM_ERR_INVALID_ARG;
-    if (bad_out_strides(d->o_head_stride, d->o_row_stride, d->n_q_heads, d->n_q_rows, d->head_dim)) return REFORM_ERR_INVALID_ARG;
+    if (bad_out_strides(d->head_dim, {{d->n_q_heads, d->o_head_stride}, {d->n_q_rows, d->o_row_stride}})) return REFORM_ERR_INVALID_ARG;
     if (rc != REFORM_OK) return rc;
     if (d->n_seq > 65536 || (int64_t)d->n_kv_heads * d->n_k_rows >= (1ll << 30)) return REFORM_ERR_UNSUPPORTED;
     // workgroups of up to 512 threads, of which a grid has fewer than 2^32
@@ -98,9 +111,6 @@ reform_status check_tree(const reform_tree_desc *d)
     const int64_t es = elt_size(d->dtype);
     for (int64_t s : strides)
         if (s < 0 || (s * es) % 16) return REFORM_ERR_INVALID_ARG;
-    if (bad_out_strides(d->o_head_stride, d->o_row_stride, d->n_q_heads, d->n_nodes, d->head_dim) ||
-        (d->n_seq > 1 && d->o_seq_stride < d->head_dim))
-        return REFORM_ERR_INVALID_ARG;
     if (rc != REFORM_OK) return rc;
     if (d->n_nodes > 64) return REFORM_ERR_UNSUPPORTED;
     // the list of all key tiles is counted in 32 bits (tree_list.h): 16 rows and 16 keys are the smallest blocks and tiles
@@ -108,6 +118,8 @@ reform_status check_tree(const reform_tree_desc *d)
     const double blocks = std::ceil((double)d->n_nodes * (d->n_q_heads / d->n_kv_heads) / 16.0);
     if ((double)d->n_seq * d->n_kv_heads * blocks * (((double)d->max_cache_len + d->n_nodes) / 16.0 + 64.0) >= 2147483648.0)
         return REFORM_ERR_UNSUPPORTED;
+    if (bad_out_strides(d->head_dim, {{d->n_seq, d->o_seq_stride}, {d->n_q_heads, d->o_head_stride}, {d->n_nodes, d->o_row_stride}}))
+        return REFORM_ERR_INVALID_ARG;
     return REFORM_OK;
 }
 
@@ -211,16 +223,15 @@ reform_status reform_rotary_embed(const reform_rotary_desc *d, const void *q, co
     for (int64_t s : strides)
         if (s < 0) return REFORM_ERR_INVALID_ARG;
     const int64_t es = elt_size(d->dtype);
-    if (has_q && bad_out_strides(d->q_out_head_stride, d->q_out_row_stride, d->n_q_heads, d->n_tokens, d->head_dim))
+    if (has_q && bad_out_strides(d->head_dim, {{d->n_q_heads, d->q_out_head_stride}, {d->n_tokens, d->q_out_row_stride}}))
         return REFORM_ERR_INVALID_ARG;
     if (has_k && slot) {
         if (d->block_len < 1 || d->n_blocks < 1 || d->block_stride < 0) return REFORM_ERR_INVALID_ARG;
         if ((int64_t)d->block_len * d->n_blocks >= (1ll << 31)) return REFORM_ERR_UNSUPPORTED;
-        if (bad_out_strides(d->kv_out_head_stride, d->kv_out_row_stride, d->n_kv_heads, d->block_len, d->head_dim))
+        if (bad_out_strides(d->head_dim, {{d->n_blocks, d->block_stride}, {d->n_kv_heads, d->kv_out_head_stride}, {d->block_len, d->kv_out_row_stride}}))
             return REFORM_ERR_INVALID_ARG;
-        if (d->n_blocks > 1 && d->block_stride < d->head_dim) return REFORM_ERR_INVALID_ARG;
         if ((d->block_stride * es) % 16) return REFORM_ERR_UNSUPPORTED;
-    } else if (has_k && bad_out_strides(d->kv_out_head_stride, d->kv_out_row_stride, d->n_kv_heads, d->n_tokens, d->head_dim)) {
+    } else if (has_k && bad_out_strides(d->head_dim, {{d->n_kv_heads, d->kv_out_head_stride}, {d->n_tokens, d->kv_out_row_stride}})) {
         return REFORM_ERR_INVALID_ARG;
     }
     // in place: the same tensor in the same layout
@@ -239,6 +250,7 @@ reform_status reform_rotary_embed(const reform_rotary_desc *d, const void *q, co
     if ((int64_t)d->n_q_heads + 2 * (int64_t)d->n_kv_heads > 65535) return REFORM_ERR_UNSUPPORTED;
     if ((double)d->n_tokens * (d->head_dim * es / 16) >= 2147483648.0) return REFORM_ERR_UNSUPPORTED;     // a thread for two pieces at least
     if (!work) return REFORM_OK;
+    if ((q_out && (q_out == k_out || q_out == v_out)) || (k_out && k_out == v_out)) return REFORM_ERR_INVALID_ARG;
     RotaryParams p;
     std::memset(&p, 0, sizeof(p));
     const void *src[3] = {q, k, v};
@@ -306,20 +318,26 @@ reform_status reform_tree_accept(const reform_accept_desc *d, const int32_t *par
     if (d->n_nodes < 1 || d->capacity < d->n_nodes) return REFORM_ERR_INVALID_ARG;
     if ((k == nullptr) != (v == nullptr)) return REFORM_ERR_INVALID_ARG;
     if (d->n_seq > 0 && (!drafted || !target || !cache_len)) return REFORM_ERR_INVALID_ARG;
-    if (new_len && new_len == cache_len) return REFORM_ERR_INVALID_ARG;
+    // every workgroup of a sequence reads the inputs, one of them writes the outputs
+    const int32_t *const in[5] = {parent, drafted, target, cache_len, node_count}, *const outs[4] = {path, accepted, next_token, new_len};
+    for (int i = 0; i < 4 && d->n_seq > 0; ++i) {
+        for (const int32_t *x : in)
+            if (outs[i] && outs[i] == x) return REFORM_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (outs[i] && outs[i] == outs[j]) return REFORM_ERR_INVALID_ARG;
+    }
     const int64_t es = elt_size(d->dtype), cache = (int64_t)d->capacity * d->head_dim;
     if (k) {
         if (k == v) return REFORM_ERR_INVALID_ARG;
         if (d->kv_seq_stride < 0 || d->kv_head_stride < 0 || d->kv_layer_stride < 0) return REFORM_ERR_INVALID_ARG;
-        if ((d->n_kv_heads > 1 && d->kv_head_stride < cache) || (d->n_seq > 1 && d->kv_seq_stride < cache) ||
-            (d->n_layers > 1 && d->kv_layer_stride < cache))
-            return REFORM_ERR_INVALID_ARG;
     }
     if (d->n_nodes > 64) return REFORM_ERR_UNSUPPORTED;
     if ((d->head_dim * es) % 16 || d->head_dim * es > 4096) return REFORM_ERR_UNSUPPORTED;
     if (k && ((d->kv_seq_stride * es) % 16 || (d->kv_head_stride * es) % 16 || (d->kv_layer_stride * es) % 16 ||
               !aligned16(k) || !aligned16(v)))
         return REFORM_ERR_UNSUPPORTED;
+    if (k && bad_out_strides(cache, {{d->n_layers, d->kv_layer_stride}, {d->n_seq, d->kv_seq_stride}, {d->n_kv_heads, d->kv_head_stride}}))
+        return REFORM_ERR_INVALID_ARG;
     if ((double)d->n_layers * d->n_seq * d->n_kv_heads > 4194304.0) return REFORM_ERR_UNSUPPORTED;
     AcceptParams p;
     std::memset(&p, 0, sizeof(p));

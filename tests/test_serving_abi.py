@@ -203,3 +203,30 @@ def test_shapes_are_checked():
         binding.prompt_desc(*(z(2, 3, 64, dtype=torch.float16) for _ in range(4)), i(2), 0.1)
     with pytest.raises(ValueError, match="cubic"):
         binding.reform_rotary_embed(z(4, 3, 64), None, None, i(3), q_out=z(4, 3, 64), scaling="cubic")
+
+
+def test_outputs_that_overlap_are_refused():
+    """Strides under which two rows of an output would share memory, and one tensor in two places."""
+    # sequences inside one another's heads, heads inside one another's rows
+    assert call_tree(tree(o_seq_stride=640)) == 1
+    assert call_tree(tree(o_seq_stride=128, o_row_stride=384, o_head_stride=1920), ws=None) == 3       # [heads][nodes][sequences]: apart
+    assert call_tree(tree(o_seq_stride=128, o_row_stride=256, o_head_stride=1920)) == 1
+    # a paged cache whose blocks begin inside the heads of the one before; heads outside the blocks are apart
+    paged = dict(block_len=64, n_blocks=3, kv_out_head_stride=64 * 128)
+    assert call_rotary(rotary(**paged, block_stride=64 * 128), slot=FAKE, vo=3 * FAKE) == 1
+    outside = rotary(n_tokens=1 << 28, block_len=64, n_blocks=3, kv_out_head_stride=3 * 64 * 128, block_stride=64 * 128,
+                     q_out_head_stride=1 << 40)
+    assert call_rotary(outside, slot=FAKE, ko=3 * FAKE, vo=4 * FAKE) == 2                              # refused for its tokens alone
+    for kw in (dict(ko=2 * FAKE, vo=3 * FAKE), dict(ko=3 * FAKE, vo=2 * FAKE), dict(ko=3 * FAKE, vo=3 * FAKE)):
+        assert call_rotary(rotary(), qo=2 * FAKE, **kw) == 1
+    # two sequences' caches in each other's heads, layers inside a sequence
+    assert call_accept(accept(kv_seq_stride=12800)) == 1
+    assert call_accept(accept(n_layers=2, kv_layer_stride=2 * 12800)) == 1
+    lib = binding.load_library()
+    for at in range(4):
+        outs = [None] * 4
+        for taken in (FAKE, 2 * FAKE, 3 * FAKE, 4 * FAKE, 5 * FAKE):                                   # an input
+            outs[at] = taken
+            assert lib.reform_tree_accept(ctypes.byref(accept()), FAKE, 2 * FAKE, 3 * FAKE, 4 * FAKE, 5 * FAKE, None, None, *outs, None) == 1
+        outs[at] = outs[at - 1] = 6 * FAKE                                                             # another output
+        assert lib.reform_tree_accept(ctypes.byref(accept()), FAKE, 2 * FAKE, 3 * FAKE, 4 * FAKE, 5 * FAKE, None, None, *outs, None) == 1
