@@ -242,7 +242,7 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
     int tl = -1;                                         // last tile of the group that the wave needs
     if (row0 < r.rows) {
         const int last = TREE ? k.n - 1 : M + min(row0 + 31 * rstep, r.rows - 1) / r.G;
-        if (last >= kg * BN) tl = (min(last / BN, ntiles - 1) - kg) / KG;
+        if (last >= kg * BN && kg < ntiles) tl = (min(last / BN, ntiles - 1) - kg) / KG;       // a range may have fewer tiles than groups
     }
     const int open = TREE ? k.open : M + row0 / r.G + 1; // keys below it are seen by all of the wave's rows
     unsigned long long *lines = (unsigned long long *)((char *)lds + S::line_at);

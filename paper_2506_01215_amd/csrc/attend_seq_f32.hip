@@ -217,7 +217,13 @@ hipError_t prompt_attend_f32_launch(const PromptParams &p, hipStream_t st)
 // Elements of a row of the pieces: heads are padded to the next form.
 size_t tree_part_dim(bool bf16, int D) { return bf16 ? D : D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-void tree_plan_f32(TreeParams &p, int compute_units) { tree_plan(p, kF32Rows, kF32Keys, 64, 16, 2 * compute_units); }
+// Fitted as in tree.hip, to 90 batches of 1 to 40 rows over 300 to 3000 keys in heads of 32 to 256: shares of a tile for each wave and more take
+// 0.87 of the time that two tiles for each take, whole items of up to 1024 keys up to 4.8 times as much where heads are wide.
+void tree_plan_f32(TreeParams &p, int compute_units)
+{
+    const int whole = p.D <= 32 ? 1200 : p.D <= 64 ? 850 : p.D <= 128 ? 350 : 200;
+    tree_plan(p, kF32Rows, kF32Keys, whole, kF32Waves, compute_units, 2 * compute_units);
+}
 
 hipError_t tree_attend_f32_launch(const TreeParams &p, hipStream_t st)
 {

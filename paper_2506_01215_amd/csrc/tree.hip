@@ -9,6 +9,9 @@
 // Measured, 32/8 heads of 128: one token for each of 32 sequences over 8192 rows (1.07 GB) 183 us, 5.9 TB/s; 24 nodes 206 us, 64 nodes
 // 301 us.  8 waves at head_dim 128, 4 at 64 (two workgroups to a compute unit): 8 nodes, 24/8 of 64, 16 caches of up to 4096 rows
 // 37.6 us with 8 waves, 31.6 with 4; one token, 32/8 of 128, 16 caches of up to 8000 rows 49.7 with 8, 50.2 with 4.
+// 64 rows: two groups of two waves that divide the tiles, one such workgroup to a compute unit, so that there are half as many pieces to
+// put together as with two workgroups of two waves (36 batches of 33 to 64 rows over 200 to 12500 keys, mean: 0.89 of the time; four groups at
+// head_dim 64 0.92).  128 rows: two groups take as long as two workgroups (25 batches, 1.00).
 #include "attend_rows.h"
 #include "tree_list.h"
 
@@ -25,13 +28,13 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_attend(TreeParams p)
     });
 }
 
-template <int D, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void tree_attend_rows(TreeParams p)
+template <int D, int NW, int KG>
+__global__ __launch_bounds__(NW * KG * 64, 2) void tree_attend_rows(TreeParams p)
 {
-    using S = RowsShape<D, NW, 1>;
+    using S = RowsShape<D, NW, KG>;
     extern __shared__ __attribute__((aligned(16))) u16 lds[];
     tree_walk<u16, S::ROWS, S::BN>(p, [&](const SeqRows &r, const SeqKeys &k, int t0, int t1, long slot) {
-        rows_segment<D, NW, 1, true>(r, k, false, p.scale, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
+        rows_segment<D, NW, KG, true>(r, k, false, p.scale, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
                                   slot < 0 ? nullptr : p.part_ml + (size_t)slot * p.part_rows, lds);
     });
 }
@@ -58,14 +61,14 @@ hipError_t launch(const TreeParams &p, hipStream_t st)
     return hipGetLastError();
 }
 
-template <int D, int NW>
+template <int D, int NW, int KG>
 hipError_t launch_long(const TreeParams &p, hipStream_t st)
 {
-    using S = RowsShape<D, NW, 1>;
-    const hipError_t e = raise_lds<tree_attend_rows<D, NW>>(S::lds_bytes);
+    using S = RowsShape<D, NW, KG>;
+    const hipError_t e = raise_lds<tree_attend_rows<D, NW, KG>>(S::lds_bytes);
     if (e != hipSuccess) return e;
     const unsigned grid = (unsigned)(p.shares ? p.shares : p.n_seq * p.Hkv) * p.row_blocks;
-    hipLaunchKernelGGL((tree_attend_rows<D, NW>), dim3(grid), dim3(NW * 64), S::lds_bytes, st, p);
+    hipLaunchKernelGGL((tree_attend_rows<D, NW, KG>), dim3(grid), dim3(NW * KG * 64), S::lds_bytes, st, p);
     if (p.shares) tree_merge_launch<D, S::ROWS, S::BN, true>(p, st);
     return hipGetLastError();
 }
@@ -77,9 +80,9 @@ hipError_t launch_rows(const TreeParams &p, hipStream_t st)
     constexpr int NW = D == 64 ? 4 : 8;
     if (R == 16) return launch<D, 1, NW>(p, st);
     if (R == 32) return launch<D, 2, NW>(p, st);
-    if (R == 64) return launch_long<D, 2>(p, st);
-    if (R == 128) return launch_long<D, 4>(p, st);
-    return launch_long<D, 8>(p, st);
+    if (R == 64) return launch_long<D, 2, 2>(p, st);
+    if (R == 128) return launch_long<D, 4, 1>(p, st);
+    return launch_long<D, 8, 1>(p, st);
 }
 
 }  // namespace
@@ -87,7 +90,15 @@ hipError_t launch_rows(const TreeParams &p, hipStream_t st)
 void tree_plan_bf16(TreeParams &p, int compute_units)
 {
     const int R = tree_rows(p), keys = tree_keys(R);
-    tree_plan(p, R, keys, 1024 / keys, 256 / keys, R == 256 ? compute_units : (R <= 32 && p.D == 128 ? 1 : 2) * compute_units);
+    const bool narrow = p.D == 64;
+    // Keys that one workgroup takes alone before sharing them out is faster, and that a share has at least: fitted to 360 batches of 1 to
+    // 512 rows, 1 to 64 sequences of 300 to 8000 keys, each whole and shared out with 128 and 256 keys or more.  240 other ones of 300 to 25000 keys
+    // against 1024 and 256 for all, means by rows: up to 16 0.96, 32 0.95, 64 0.90 (with the two groups), 128 0.97, 256 0.97, 512 0.98; at
+    // worst 1.12 (77 rows of 4 x 8 caches of up to 990 keys 14.8 -> 16.3 us).
+    const int whole = R == 16 ? (narrow ? 2000 : 1600) : R == 32 ? (narrow ? 2000 : 1300) : R == 64 ? (narrow ? 1600 : 1000) :
+                      R == 128 ? (narrow ? 1000 : 700) : narrow ? 800 : 600;
+    const int least = (R == 16 && narrow ? 256 : 128) / keys;
+    tree_plan(p, R, keys, whole, least, compute_units, (R == 128 || (R <= 32 && narrow) ? 2 : 1) * compute_units);
 }
 
 hipError_t tree_attend_bf16(const TreeParams &p, hipStream_t st)

@@ -10,6 +10,8 @@
 #pragma once
 #include "attend_seq.h"
 
+#include <cmath>
+
 namespace reform {
 
 constexpr int kTreeStart = 8;
@@ -63,7 +65,9 @@ struct TreeList {
         }
         total = __builtin_amdgcn_readlane(wave_incl_scan(places), 63);
         items = __builtin_amdgcn_readlane(wave_incl_scan(items), 63);
-        shares = max(1, min(p.shares, max(items, total / max(p.least, 1))));
+        // up to a share for every compute unit short ones, beyond that (two workgroups to a unit) of twice as many places at least
+        const int most = (int)((unsigned)total / (unsigned)max(p.least, 1));
+        shares = max(1, min(p.shares, max(items, max(min(most, p.units), most >> 1))));
         each = (int)((unsigned)total / (unsigned)shares);
         more = total - each * shares;
     }
@@ -324,18 +328,21 @@ inline void tree_merge_launch(const TreeParams &p, hipStream_t st)
     hipLaunchKernelGGL((tree_merge<D, R, TK, BF16>), dim3((unsigned)blocks * chunks), dim3(256), 0, st, p, rows, (int)by_share);
 }
 
-// Row blocks, shares and the rows of a piece for blocks of R rows and tiles of TK keys.  No shares where every item is
-// short (`whole` tiles): then one workgroup takes an item whole, and there is nothing to merge.  `least`: tiles
-// that keep the waves of one workgroup busy.
-inline void tree_plan(TreeParams &p, int R, int TK, int whole, int least, int workgroups)
+// Row blocks, shares and the rows of a piece for blocks of R rows and tiles of TK keys.  `least`: tiles that a share has at least (TreeList).
+// No shares where every item is short: then one workgroup takes an item whole, and there is nothing to merge.  Short is up to
+// `whole` keys where one item is alone on the chip, and up to 2.5 times as many where there are as many items as compute
+// units, since sharing these out gains only what their lengths differ by.
+inline void tree_plan(TreeParams &p, int R, int TK, int whole, int least, int compute_units, int workgroups)
 {
     const int rows = p.T * p.G;
     p.row_blocks = (rows + R - 1) / R;
     p.part_rows = rows < R ? rows : R;
     p.least = least;
-    const int tiles = (p.max_len + p.T + TK - 1) / TK;
-    if (tiles <= whole) return;
-    const double items = (double)p.n_seq * p.Hkv, most = items * (tiles + kTreeStart) / least;
+    p.units = compute_units;
+    const double items = (double)p.n_seq * p.Hkv, taken = items * p.row_blocks < compute_units ? items * p.row_blocks / compute_units : 1.0;
+    const double keys = (double)p.max_len + p.T;
+    if (keys * (1.0 - 0.6 * taken) <= whole) return;
+    const double most = items * (std::ceil(keys / TK) + kTreeStart) / least;
     const double want = items > most ? items : most;
     int room = workgroups / p.row_blocks;
     room = room < 1 ? 1 : room > kTreeMaxShares ? kTreeMaxShares : room;
