@@ -162,7 +162,8 @@ struct TreeParams {
     int shares;              // parts of the list of all sequences' key tiles (tree_list.h); 0: one workgroup per sequence, head and row block
     int least;               // tiles that a share has at least, where there are fewer sequences and heads than shares
     int units;               // compute units
-    int row_blocks;          // of T * G rows
+    int block;               // rows of a block of T * G rows
+    int row_blocks;
     int part_rows;           // rows of one partial result
     float *part_o;           // [2 * shares][row_blocks][part_rows][D] unnormalised outputs
     float2 *part_ml;         // [2 * shares][row_blocks][part_rows] reference maximum (log2 units) and sum

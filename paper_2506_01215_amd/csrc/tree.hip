@@ -3,9 +3,9 @@
 //
 // Bound: reading K and V once, up to some 64 rows (a 16-row block of queries costs a compute unit a sixth of the time that its
 // share of the memory bandwidth takes to bring the keys), then the matrix pipe as well.  So the keys are shared out over the
-// whole chip (tree_list.h), and the rows of a group's heads and nodes are one block of up to 256, for which K and V are
-// read once.  Up to 32 rows every wave has key tiles of its own and no barrier (attend_seq.h); beyond that the waves divide the
-// rows and go through the tiles together (attend_rows.h).
+// whole chip (tree_list.h), and where the chip is busy the rows of a group's heads and nodes are one block of up to 256, for which K and V are
+// read once; where it is not, smaller blocks (tree_rows).  In blocks of up to 32 rows every wave has key tiles of its own and no
+// barrier (attend_seq.h); in larger ones the waves divide the rows and go through the tiles together (attend_rows.h).
 // Measured, 32/8 heads of 128: one token for each of 32 sequences over 8192 rows (1.07 GB) 183 us, 5.9 TB/s; 24 nodes 206 us, 64 nodes
 // 301 us.  8 waves at head_dim 128, 4 at 64 (two workgroups to a compute unit): 8 nodes, 24/8 of 64, 16 caches of up to 4096 rows
 // 37.6 us with 8 waves, 31.6 with 4; one token, 32/8 of 128, 16 caches of up to 8000 rows 49.7 with 8, 50.2 with 4.
@@ -41,12 +41,23 @@ __global__ __launch_bounds__(NW * KG * 64, 2) void tree_attend_rows(TreeParams p
 
 namespace {
 
-// Rows of a block, and keys of a tile.
-int tree_rows(const TreeParams &p)
+// Rows of a block.  Blocks that take all rows read K and V least often, and are right where the chip is busy; where it is not, smaller blocks
+// are done sooner, being more.  What each unit would have to go through in blocks of R rows decides, in keys, with 400 for the time it
+// takes to begin a block.  Fitted to 230 batches of 17 to 512 rows over 300 to 12000 keys, 1 to 64 sequences, in every form: the choice takes
+// 1.3 % more time in the mean than the best form, at worst 1.34 times it; the smallest block that takes all rows 23 %.
+int tree_rows(const TreeParams &p, int compute_units)
 {
     const int rows = p.T * p.G;
-    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+    const double keys = ((double)p.max_len + p.T + 400) * p.n_seq * p.Hkv / compute_units;
+    const bool narrow = p.D == 64;
+    auto few = [&](int R, int limit) { return rows <= R || (rows + R - 1) / R * keys <= limit; };
+    if (few(16, narrow ? 1600 : 1300)) return 16;
+    if (few(32, narrow ? 1800 : 600)) return 32;
+    if (few(64, narrow ? 2000 : 1000)) return 64;
+    return rows > 128 && (rows + 127) / 128 % 2 == 0 ? 256 : 128;           // 256 where it is not half empty
 }
+
+// Keys of a tile.
 int tree_keys(int rows) { return rows > 32 ? kRowsKeys : 32; }
 
 template <int D, int NB, int NW>
@@ -76,7 +87,7 @@ hipError_t launch_long(const TreeParams &p, hipStream_t st)
 template <int D>
 hipError_t launch_rows(const TreeParams &p, hipStream_t st)
 {
-    const int R = tree_rows(p);
+    const int R = p.block;
     constexpr int NW = D == 64 ? 4 : 8;
     if (R == 16) return launch<D, 1, NW>(p, st);
     if (R == 32) return launch<D, 2, NW>(p, st);
@@ -89,7 +100,7 @@ hipError_t launch_rows(const TreeParams &p, hipStream_t st)
 
 void tree_plan_bf16(TreeParams &p, int compute_units)
 {
-    const int R = tree_rows(p), keys = tree_keys(R);
+    const int R = tree_rows(p, compute_units), keys = tree_keys(R);
     const bool narrow = p.D == 64;
     // Keys that one workgroup takes alone before sharing them out is faster, and that a share has at least: fitted to 360 batches of 1 to
     // 512 rows, 1 to 64 sequences of 300 to 8000 keys, each whole and shared out with 128 and 256 keys or more.  240 other ones of 300 to 25000 keys

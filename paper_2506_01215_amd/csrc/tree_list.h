@@ -335,6 +335,7 @@ inline void tree_merge_launch(const TreeParams &p, hipStream_t st)
 inline void tree_plan(TreeParams &p, int R, int TK, int whole, int least, int compute_units, int workgroups)
 {
     const int rows = p.T * p.G;
+    p.block = R;
     p.row_blocks = (rows + R - 1) / R;
     p.part_rows = rows < R ? rows : R;
     p.least = least;

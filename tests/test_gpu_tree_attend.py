@@ -178,3 +178,36 @@ def test_many_short_caches():
     lens = [rnd.choice([0, 1, 64, rnd.randint(0, 90)]) for _ in range(200)]
     run_case(4, 2, 64, 2, lens, BF, seed=5, counts=[rnd.randint(0, 2) for _ in lens])
     run_case(2, 2, 16, 2, lens, F, seed=5)
+
+
+@pytest.mark.parametrize("hq,hkv,d,T,lens,block", [
+    (4, 4, 128, 11, [3000, 0, 40], 16), (8, 2, 64, 4, [700, 3000, 1, 0], 16), (8, 2, 64, 7, [63, 2000, 500, 5], 32),
+    (16, 4, 128, 8, [1, 2500], 32), (6, 2, 64, 11, [100, 0, 1000, 31], 64), (16, 4, 128, 16, [3000, 17], 64),
+    (8, 2, 128, 9, [257, 2000, 3, 64], 64), (8, 8, 64, 64, [1300], 64), (8, 2, 64, 17, [600, 1, 64, 128], 128), (12, 4, 128, 40, [900, 64, 0], 128),
+    (4, 2, 128, 64, [63, 1999, 0, 20], 128), (28, 4, 64, 10, [1, 300], 128), (8, 2, 128, 64, [1000, 0, 63, 65], 256),
+    (16, 4, 64, 33, [2500, 0], 256), (28, 4, 64, 50, [300, 1], 128), (32, 4, 128, 64, [700, 40], 256), (28, 4, 128, 23, [1, 3000], 256),
+])
+def test_every_form_shared_out(hq, hkv, d, T, lens, block):
+    """Short caches in a large capacity, which is what the host chooses by: each form, with lengths where its tiles and shares end.  The
+    workspace's size tells the rows of a block."""
+    cap, rows, units = 40000, T * hq // hkv, torch.cuda.get_device_properties(0).multi_processor_count if torch.cuda.is_available() else 256
+    side = -(-rows // block)
+    shares = min((2 if block == 128 or (block <= 32 and d == 64) else 1) * units // side, 512)
+    desc = binding.tree_desc(*(torch.empty(s, dtype=BF, device="meta") for s in
+                               ((len(lens), hq, T, d), (len(lens), hkv, cap, d), (len(lens), hkv, cap, d), (len(lens), hq, T, d))), 0.1)
+    assert binding.tree_workspace_bytes(desc) == 2 * shares * side * min(rows, block) * (4 * d + 8)
+    run_case(hq, hkv, d, T, lens, BF, seed=block + T, spare=cap - max(lens) - T)
+    run_case(hq, hkv, d, T, lens, BF, seed=block + T + 1, spare=cap - max(lens) - T, chain=True, counts=[max(T - 3 * i - 1, 0) for i in range(len(lens))])
+
+
+@pytest.mark.parametrize("hq,hkv,d,T,n,top", [
+    (8, 8, 64, 16, 60, 300), (8, 2, 128, 8, 250, 70), (16, 8, 64, 30, 80, 90), (8, 2, 128, 28, 200, 30), (16, 4, 64, 60, 130, 64),
+    (16, 4, 128, 60, 110, 100), (21, 3, 64, 64, 100, 70),
+])
+def test_every_form_whole(hq, hkv, d, T, n, top):
+    """Many short caches: one workgroup to each sequence, KV head and row block, in every form."""
+    rnd = random.Random(T)
+    lens = [rnd.choice([0, 1, top, rnd.randint(0, top)]) for _ in range(n)]
+    q, kv = torch.empty((n, hq, T, d), dtype=BF, device="meta"), torch.empty((n, hkv, top + T, d), dtype=BF, device="meta")
+    assert binding.tree_workspace_bytes(binding.tree_desc(q, kv, kv, q, 0.1)) == 0
+    run_case(hq, hkv, d, T, lens, BF, seed=T + n, spare=0, counts=[rnd.choice([T, T, rnd.randint(0, T)]) for _ in lens])
