@@ -2,7 +2,7 @@
 //
 //   prompt_attend<D,NW,KG>   a workgroup takes a block of 32 NW rows of one KV head (counted over query rows and the heads
 //                            of the group) over all keys that the block sees; KG groups of its waves divide the key tiles
-//   prompt_attend_short      blocks of 32 rows whose eight waves divide the keys (attend_seq.h)
+//   prompt_attend_short<D,NB,NW>   blocks of 16 NB rows whose NW waves divide the keys (attend_seq.h)
 //
 // Large blocks read K and V less often, small ones and divided keys fill the chip with few rows and make the longest
 // block's chain of tiles shorter; prompt_plan.h says which when.
@@ -29,10 +29,10 @@ __global__ __launch_bounds__(NW * KG * 64, 2) void prompt_attend(PromptParams p)
     rows_segment<D, NW, KG, false>(r, k, p.by_head, p.scale, 0, blk.tiles, nullptr, nullptr, lds);
 }
 
-template <int D>
-__global__ __launch_bounds__(512, 2) void prompt_attend_short(PromptParams p)
+template <int D, int NB, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void prompt_attend_short(PromptParams p)
 {
-    using S = SeqShape<D, 2, 8>;
+    using S = SeqShape<D, NB, NW>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int kvh = blockIdx.x % p.Hkv;
     const PromptBlock blk = prompt_block<S::R, S::TK>(p, blockIdx.x / p.Hkv);
@@ -40,7 +40,7 @@ __global__ __launch_bounds__(512, 2) void prompt_attend_short(PromptParams p)
     SeqRows r;
     SeqKeys k;
     prompt_block_operands<u16>(p, blk, kvh, blk.rb * S::R, r, k);
-    seq_segment<D, 2, 8, false>(r, k, p.scale, 0, blk.tiles, nullptr, nullptr, smem);
+    seq_segment<D, NB, NW, false>(r, k, p.scale, 0, blk.tiles, nullptr, nullptr, smem);
 }
 
 namespace {
@@ -56,13 +56,13 @@ hipError_t launch_long(PromptParams p, hipStream_t st)
     return hipGetLastError();
 }
 
-template <int D>
+template <int D, int NB, int NW>
 hipError_t launch_short(const PromptParams &p, hipStream_t st)
 {
-    using S = SeqShape<D, 2, 8>;
-    const hipError_t e = raise_lds<prompt_attend_short<D>>(S::lds_bytes);
+    using S = SeqShape<D, NB, NW>;
+    const hipError_t e = raise_lds<prompt_attend_short<D, NB, NW>>(S::lds_bytes);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((prompt_attend_short<D>), dim3(prompt_grid(p, S::R)), dim3(512), S::lds_bytes, st, p);
+    hipLaunchKernelGGL((prompt_attend_short<D, NB, NW>), dim3(prompt_grid(p, S::R)), dim3(NW * 64), S::lds_bytes, st, p);
     return hipGetLastError();
 }
 
@@ -71,10 +71,10 @@ hipError_t launch(const PromptParams &p, hipStream_t st)
 {
     const int units = device_compute_units() > 0 ? device_compute_units() : 256;
     const PromptForm &f = prompt_forms(D)[prompt_choose(D, p.G, p.Hkv, p.n_seq, p.n_q, p.n_k, units)];
-    if (f.rows == 256) return launch_long<D, 8, 1>(p, st);
-    if (f.rows == 64) return launch_long<D, 2, 2>(p, st);
+    if (f.rows == 32) return launch_short<D, 2, 4>(p, st);
+    if (f.rows == 16) return launch_short<D, 1, 8>(p, st);
     if constexpr (D == 64) {
-        if (f.rows == 32) return launch_short<D>(p, st);
+        if (f.rows == 256) return launch_long<D, 8, 1>(p, st);
     } else {
         if (f.groups == 2) return launch_long<D, 4, 2>(p, st);
     }

@@ -5,12 +5,14 @@
 // time in microseconds: what all blocks' steps take at the rate of the whole chip, and what the longest block takes by
 // itself.  A step is one key tile of each of the form's groups of waves.
 //
-// The constants were fitted to measurements of 136 batches (60 to 12000 rows, 1 to 24 sequences, 1 to 8 heads a group, with
-// and without keys in front) in every form: mean error 5 to 9 %, and the form that is chosen takes 1 to 2 % more time in
-// the mean than the best, at worst 24 %.  Examples, us, blocks of 256 / 128 / 128 with two groups / 64 with two groups / 32
-// with eight: head_dim 64, one prompt of 700, 24/8 heads 18 / 15 / 14 / 12 / 19, of 700, 4/4 heads 18 / 14 / 13 / 11 / 9, 24 of
-// together 11988, 24/8 68 / 66 / 102 / 89 / 246; head_dim 128, one of 1500, 32/8 46 / 39 / 35 / 50 / 74, of 3200, 8/8 82 / 64 / 52 /
-// 44 / 59, six of together 11996, 32/8 371 / 365 / 427 / 675 / 886.
+// The constants were fitted to measurements of 370 batches (1 to 32000 rows, 1 to 50 sequences, 1 to 8 heads a group, with
+// and without keys in front) in eight forms: error 6 to 15 % (root mean square), and the one of these four that is chosen takes 2 % more time in
+// the mean than the best of the eight, at worst 47 %.  (256 rows at head_dim 128, 64 by two groups, 32 by eight and 16 by four add nothing; without the last two forms
+// it is 4 % at head_dim 64 and 16 % at 128.)  Measured, us, blocks of 256 / 128 / 128 with two groups (head_dim 128) / 32 / 16:
+//   head_dim 64: 32 prompts of together 14586 behind 500 keys each, 8/4 heads 60 / 46 / - / 71 / -, four of 2445, 3/1 17.5 / 14.3 / - / 9.3 / 11.5, one
+//   row behind 3000 keys, 2/1 39 / 40 / - / 16 / 11.5, one of 32768, 32/8 4658 / 4799
+//   head_dim 128: 50 of together 2859, 56/8 44 / 37 / 59 / 85 / -, one of 6673, 8/1 171 / 135 / 102 / 146 / 270, one of 2674, 4/4 69 / 53 / 43 / 27 / 34,
+//   eight of together 75 behind 3000 keys each, 8/8 54 / 56 / - / 28 / 24, one of 16384, 32/8 1877 / 1884, of 32768 7769 / 7427
 #pragma once
 #include <algorithm>
 #include <cmath>
@@ -29,10 +31,10 @@ constexpr int kPromptForms = 4;
 
 inline const PromptForm *prompt_forms(int head_dim)
 {
-    static const PromptForm wide64[kPromptForms] = {{256, 1, 64, 1.07, 1.05, 7.5, 4.2}, {128, 1, 64, 0.551, 0.726, 6.6, 2.02},
-                                                    {64, 2, 64, 0.634, 0.782, 6.66, 1.97}, {32, 8, 32, 0.852, 0.780, 6.0, 4.2}};
-    static const PromptForm wide128[kPromptForms] = {{256, 1, 64, 1.67, 1.50, 8.0, 6.6}, {128, 1, 64, 0.860, 1.138, 7.1, 3.3},
-                                                     {128, 2, 64, 1.908, 1.650, 8.1, 5.8}, {64, 2, 64, 1.476, 1.371, 6.3, 5.1}};
+    static const PromptForm wide64[kPromptForms] = {{256, 1, 64, 1.13, 0.790, 6.30, 8.50}, {128, 1, 64, 0.592, 0.790, 5.20, 2.62},
+                                                    {32, 4, 32, 0.382, 0.522, 5.54, 1.57}, {16, 8, 32, 0.812, 0.788, 3.30, 3.40}};
+    static const PromptForm wide128[kPromptForms] = {{128, 1, 64, 0.900, 1.117, 6.43, 4.30}, {128, 2, 64, 2.030, 1.671, 7.17, 6.81},
+                                                     {32, 4, 32, 0.748, 0.872, 6.78, 3.08}, {16, 8, 32, 1.465, 1.620, 3.66, 4.23}};
     return head_dim == 64 ? wide64 : wide128;
 }
 

@@ -85,10 +85,10 @@ def plan(tmp_path_factory):
 
 
 @pytest.mark.parametrize("d,hq,hkv,n,total,form", [
-    (64, 2, 2, 3, 700, (32, 8)), (64, 7, 1, 1, 900, (32, 8)), (64, 24, 8, 5, 700, (64, 2)), (64, 6, 2, 9, 700, (64, 2)),
-    (64, 12, 4, 40, 6000, (128, 1)), (64, 7, 7, 60, 9000, (128, 1)), (64, 32, 1, 8, 14000, (256, 1)), (64, 30, 2, 1, 9000, (256, 1)),
-    (128, 6, 2, 7, 700, (64, 2)), (128, 3, 1, 1, 1000, (64, 2)), (128, 16, 2, 4, 1200, (128, 2)), (128, 14, 2, 3, 3000, (128, 2)),
-    (128, 12, 4, 40, 5000, (128, 1)), (128, 7, 7, 90, 7000, (128, 1)), (128, 32, 1, 24, 14000, (256, 1)), (128, 30, 2, 1, 9000, (256, 1)),
+    (64, 2, 2, 3, 700, (16, 8)), (64, 7, 1, 1, 900, (32, 4)), (64, 24, 8, 5, 700, (128, 1)), (64, 6, 2, 9, 700, (32, 4)),
+    (64, 12, 4, 40, 6000, (128, 1)), (64, 7, 7, 60, 9000, (128, 1)), (64, 8, 1, 1, 12000, (256, 1)), (64, 30, 2, 1, 12000, (256, 1)),
+    (128, 6, 2, 7, 700, (32, 4)), (128, 3, 1, 1, 1000, (16, 8)), (128, 7, 1, 2, 3000, (32, 4)), (128, 16, 2, 4, 1200, (128, 2)),
+    (128, 14, 2, 3, 3000, (128, 2)), (128, 12, 4, 40, 5000, (128, 1)), (128, 7, 7, 90, 7000, (128, 1)),
 ])
 def test_every_form(plan, d, hq, hkv, n, total, form):
     """Ragged batches that take each of the forms (the plan's own header says so), with and without keys in front; the
