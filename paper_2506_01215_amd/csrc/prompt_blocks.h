@@ -3,7 +3,8 @@
 // A sequence's rows, counted over its query rows and the G heads of a KV group, are cut into blocks of ROWS.  The
 // lengths are on the device, so the host launches as many workgroups as there can be blocks, and workgroup number i
 // takes the i-th longest block: causal blocks differ by the length of their sequence, and the chip is filled
-// evenly to the end only if the long ones begin first.
+// evenly to the end only if the long ones begin first.  (The search is 2.2 us of a block's time at 12 sequences; three thresholds side by side, half
+// as many steps, changed no batch.)
 #pragma once
 #include "attend_seq.h"
 
