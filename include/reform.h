@@ -465,6 +465,8 @@ reform_status reform_rotary_embed(const reform_rotary_desc *desc, const void *q,
  * Supported: REFORM_BF16 with head_dim 64 or 128; REFORM_F32 with head_dim % 4 == 0, <= 256; at most 65536
  * sequences; out and lse apart from the inputs; n_q_heads * n_q_rows / 16 + n_kv_heads * n_seq below 2^23, n_kv_heads * n_k_rows below 2^30; row
  * strides of k and v below 2^24.  n_q_rows = 0 does nothing.
+ * The workspace takes partial results where few rows stand behind many keys, which are then shared out over workgroups; the query
+ * gives 0 elsewhere.  Without it, or with less than the query asks for, the call returns REFORM_ERR_WORKSPACE.
  */
 typedef struct {
     uint32_t struct_size;

@@ -4,6 +4,8 @@
 //                            of the group) over all keys that the block sees; KG groups of its waves divide the key tiles
 //   prompt_attend_short<D,NB,NW>   blocks of 16 NB rows whose NW waves divide the keys (attend_seq.h)
 //
+//   prompt_attend_shared<D,NB,NW>  the same blocks, their keys shared out over the chip: few rows behind many keys (prompt_share.h)
+//
 // Large blocks read K and V less often, small ones and divided keys fill the chip with few rows and make the longest
 // block's chain of tiles shorter; prompt_plan.h says which when.
 //
@@ -14,6 +16,7 @@
 #include "attend_rows.h"
 #include "prompt_blocks.h"
 #include "prompt_plan.h"
+#include "prompt_share.h"
 
 namespace reform {
 
@@ -45,6 +48,17 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_short(PromptParams p
     seq_segment<D, NB, NW, false>(r, k, p.scale, 0, blk.tiles, nullptr, nullptr, smem);
 }
 
+template <int D, int NB, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void prompt_attend_shared(PromptParams p)
+{
+    using S = SeqShape<D, NB, NW>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    prompt_walk<u16, S::R, S::TK>(p, [&](const SeqRows &r, const SeqKeys &k, int t0, int t1, long slot) {
+        seq_segment<D, NB, NW, false>(r, k, p.scale, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
+                                      slot < 0 ? nullptr : p.part_ml + (size_t)slot * p.part_rows, smem);
+    });
+}
+
 namespace {
 
 template <int D, int NW, int KG>
@@ -68,11 +82,25 @@ hipError_t launch_short(const PromptParams &p, hipStream_t st)
     return hipGetLastError();
 }
 
+template <int D, int NB, int NW>
+hipError_t launch_shared(const PromptParams &p, hipStream_t st)
+{
+    using S = SeqShape<D, NB, NW>;
+    const hipError_t e = raise_lds<prompt_attend_shared<D, NB, NW>>(S::lds_bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((prompt_attend_shared<D, NB, NW>), dim3(p.shares), dim3(NW * 64), S::lds_bytes, st, p);
+    prompt_merge_launch<D, S::R, S::TK, true>(p, st);
+    return hipGetLastError();
+}
+
 template <int D>
 hipError_t launch(const PromptParams &p, hipStream_t st)
 {
-    const int units = device_compute_units() > 0 ? device_compute_units() : 256;
-    const PromptForm &f = prompt_forms(D)[prompt_choose(D, p.G, p.Hkv, p.n_seq, p.n_q, p.n_k, units)];
+    if (p.shares) {
+        constexpr int NW = D == 64 ? 4 : 8;
+        return p.block == 16 ? launch_shared<D, 1, NW>(p, st) : launch_shared<D, 2, NW>(p, st);
+    }
+    const PromptForm &f = prompt_forms(D)[prompt_choose(D, p.G, p.Hkv, p.n_seq, p.n_q, p.n_k, p.units)];
     if (f.rows == 32) return launch_short<D, 2, 4>(p, st);
     if (f.rows == 16) return launch_short<D, 1, 8>(p, st);
     if constexpr (D == 64) {
@@ -84,6 +112,18 @@ hipError_t launch(const PromptParams &p, hipStream_t st)
 }
 
 }  // namespace
+
+void prompt_plan_bf16(PromptParams &p)
+{
+    PromptShared f;
+    p.block = prompt_share_rows(p.D, p.G, p.Hkv, p.n_seq, p.n_q, p.n_k, p.units, f);
+    if (!p.block) return;
+    const int rows = p.n_q * p.G;
+    p.part_rows = rows < p.block ? rows : p.block;
+    p.least = f.least / f.form.keys;
+    p.shares = (p.D == 64 ? 2 : 1) * p.units;
+    if (p.shares > kTreeMaxShares) p.shares = kTreeMaxShares;
+}
 
 hipError_t prompt_attend_bf16(const PromptParams &p, hipStream_t st)
 {

@@ -12,8 +12,7 @@
 // at the sizes of checks, latency (three prompts of up to 301 rows, 4 heads of 64: 11 us).  32 rows to a workgroup, so that K and V are read half
 // as often: the same time for large batches, twice as long for small ones (60 batches, 1.27).
 #include "attend_seq.h"
-#include "prompt_blocks.h"
-#include "tree_list.h"
+#include "prompt_share.h"
 
 namespace reform {
 
@@ -179,6 +178,16 @@ __global__ __launch_bounds__(kF32Waves * 64, 2) void prompt_attend_f32(PromptPar
 }
 
 template <int DP>
+__global__ __launch_bounds__(kF32Waves * 64, 2) void prompt_attend_f32_shared(PromptParams p)
+{
+    __shared__ F32Sums<DP> sh;
+    prompt_walk<float, kF32Rows, kF32Keys>(p, [&](const SeqRows &r, const SeqKeys &k, int t0, int t1, long slot) {
+        f32_segment<DP, false>(r, k, p.D, p.scale, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * DP,
+                               slot < 0 ? nullptr : p.part_ml + (size_t)slot * p.part_rows, sh);
+    });
+}
+
+template <int DP>
 __global__ __launch_bounds__(kF32Waves * 64, 2) void tree_attend_f32(TreeParams p)
 {
     __shared__ F32Sums<DP> sh;
@@ -193,6 +202,11 @@ namespace {
 template <int DP>
 hipError_t launch_prompt(const PromptParams &p, hipStream_t st)
 {
+    if (p.shares) {
+        hipLaunchKernelGGL((prompt_attend_f32_shared<DP>), dim3(p.shares), dim3(kF32Waves * 64), 0, st, p);
+        prompt_merge_launch<DP, kF32Rows, kF32Keys, false>(p, st);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL((prompt_attend_f32<DP>), dim3(prompt_grid(p, kF32Rows)), dim3(kF32Waves * 64), 0, st, p);
     return hipGetLastError();
 }
@@ -207,6 +221,23 @@ hipError_t launch_tree(const TreeParams &p, hipStream_t st)
 }
 
 }  // namespace
+
+// A step is eight tiles of 16 keys by the waves of a workgroup, some 0.03 us for each element of a row (3.7 us at 128, 1.9 at 64), whether the chip
+// is full or not.  What sharing out saves is the longest block's chain, for some 8 us; but where a sequence's blocks are then at different keys, each
+// brings them from memory (ten rows, 12/4 heads of 96 behind 16000 keys 430 -> 48 us; 282 rows, 12/4 of 256 behind 4 x 3000 221 -> 396).
+void prompt_plan_f32(PromptParams &p)
+{
+    const double step = 0.03 * (p.D <= 32 ? 32 : p.D <= 64 ? 64 : p.D <= 128 ? 128 : 256), keys = (double)p.n_k / p.n_seq;
+    const double blocks = ((double)p.n_q * p.G / kF32Rows + p.n_seq) * p.Hkv, full = blocks * (keys / 128.0 + 1.0) * step / p.units;
+    const double alone = keys / 128.0 * step, memory = blocks * keys * p.D * 8.0 / 3.5e6;
+    if (alone < 8.0 || p.n_seq > 64 || blocks * ((double)p.n_k / kF32Keys + 16.0) >= 1073741824.0) return;
+    if (std::cbrt(full * full * full + alone * alone * alone) < 8.0 + (full > memory ? full : memory)) return;
+    const int rows = p.n_q * p.G;
+    p.block = kF32Rows;
+    p.part_rows = rows < kF32Rows ? rows : kF32Rows;
+    p.least = kF32Waves;
+    p.shares = 2 * p.units > kTreeMaxShares ? kTreeMaxShares : 2 * p.units;
+}
 
 hipError_t prompt_attend_f32_launch(const PromptParams &p, hipStream_t st)
 {

@@ -178,6 +178,12 @@ struct PromptParams {
     long q_hs, q_rs, k_hs, k_rs, v_hs, v_rs, o_hs, o_rs;     // elements
     float scale;
     int by_head;             // as in AttnParams
+    int units;               // compute units
+    int shares;              // parts of the list of all sequences' key tiles (prompt_share.h); 0: every block by one workgroup
+    int least;               // tiles that a share has at least
+    int block, part_rows;    // rows of a block then, and of one partial result
+    float *part_o;           // as in TreeParams, [2 * shares][part_rows][D]
+    float2 *part_ml;
 };
 
 struct EmbedParams {

@@ -68,4 +68,34 @@ inline int prompt_choose(int head_dim, int G, int Hkv, int n_seq, int n_q, int n
     return best;
 }
 
+// Blocks whose keys are shared out (prompt_share.h): no block takes longer than its share, but there is a second launch.  130 batches of 1 to 9000
+// rows, 1 to 50 sequences behind up to 16000 keys each, whole and shared out: with these constants (2.2 times the rates of the
+// whole forms) the choice takes 0.5 % more time in the mean than the better one, at worst 17 %, and 0.93 (head_dim 64) and 0.80 (128) of the
+// whole forms' time.  Three rows behind 16000 keys, 4/1 heads of 128 80.9 -> 18.5 us, two sequences of three rows, 64/8 heads 84 -> 33; eight of
+// together 364, 56/8 heads 261 whole, 734 shared out.
+struct PromptShared {
+    PromptForm form;
+    int least;               // keys that a share has at least
+};
+
+// Rows of such a block where sharing out is faster than the best form, else 0; `shared`: how.
+inline int prompt_share_rows(int head_dim, int G, int Hkv, int n_seq, int n_q, int n_k, int units, PromptShared &shared)
+{
+    static const PromptShared forms64[2] = {{{16, 4, 32, 0.73, 0.0, 12.0, 2.3}, 256}, {{32, 4, 32, 0.84, 0.0, 12.0, 3.45}, 128}};
+    static const PromptShared forms128[2] = {{{16, 8, 32, 3.2, 0.0, 12.0, 9.3}, 128}, {{32, 8, 32, 4.1, 0.0, 12.0, 12.7}, 128}};
+    if ((double)n_k / n_seq * (head_dim == 64 ? 0.788 : 1.62) < 256.0 * 2.5) return 0;      // a block's chain takes less than the second launch
+    // places are counted in 32 bits, sequences one to a lane
+    if (n_seq > 64 || ((double)n_q * G / 16.0 + n_seq) * Hkv * ((double)n_k / 32.0 + 16.0) >= 1073741824.0) return 0;
+    const PromptForm *whole = prompt_forms(head_dim);
+    double least = prompt_estimate(whole[0], G, Hkv, n_seq, n_q, n_k, units);
+    for (int i = 1; i < kPromptForms; ++i) least = std::min(least, prompt_estimate(whole[i], G, Hkv, n_seq, n_q, n_k, units));
+    int rows = 0;
+    for (int i = 0; i < 2; ++i) {
+        const PromptShared &f = head_dim == 64 ? forms64[i] : forms128[i];
+        const double t = prompt_estimate(f.form, G, Hkv, n_seq, n_q, n_k, units);
+        if (t < least) { least = t; shared = f; rows = f.form.rows; }
+    }
+    return rows;
+}
+
 }  // namespace reform

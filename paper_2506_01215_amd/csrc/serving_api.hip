@@ -11,6 +11,8 @@
 namespace reform {
 hipError_t rotary_embed_launch(const RotaryParams &p, bool bf16, bool adjacent, hipStream_t st);
 hipError_t tree_accept_launch(const AcceptParams &p, hipStream_t st);
+void prompt_plan_bf16(PromptParams &p);
+void prompt_plan_f32(PromptParams &p);
 hipError_t prompt_attend_bf16(const PromptParams &p, hipStream_t st);
 hipError_t prompt_attend_f32_launch(const PromptParams &p, hipStream_t st);
 void tree_plan_bf16(TreeParams &p, int compute_units);
@@ -83,6 +85,29 @@ reform_status check_prompt(const reform_prompt_desc *d)
     return REFORM_OK;
 }
 
+int compute_units()
+{
+    const int n = device_compute_units();
+    return n > 0 ? n : 256;
+}
+
+PromptParams prompt_sizes(const reform_prompt_desc *d)
+{
+    PromptParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.Hq = d->n_q_heads; p.Hkv = d->n_kv_heads; p.G = p.Hq / p.Hkv; p.D = d->head_dim;
+    p.n_seq = d->n_seq; p.n_q = d->n_q_rows; p.n_k = d->n_k_rows;
+    p.q_hs = d->q_head_stride; p.q_rs = d->q_row_stride; p.k_hs = d->k_head_stride; p.k_rs = d->k_row_stride;
+    p.v_hs = d->v_head_stride; p.v_rs = d->v_row_stride; p.o_hs = d->o_head_stride; p.o_rs = d->o_row_stride;
+    p.scale = d->scale;
+    p.units = compute_units();
+    if (d->dtype == REFORM_BF16) prompt_plan_bf16(p);
+    else prompt_plan_f32(p);
+    return p;
+}
+
+size_t prompt_part_rows(const PromptParams &p) { return (size_t)2 * p.shares * p.part_rows; }
+
 TreeParams tree_sizes(const reform_tree_desc *d)
 {
     TreeParams p;
@@ -93,9 +118,8 @@ TreeParams tree_sizes(const reform_tree_desc *d)
     p.o_ss = d->o_seq_stride; p.o_hs = d->o_head_stride; p.o_rs = d->o_row_stride;
     p.kv_ss = d->kv_seq_stride; p.kv_hs = d->kv_head_stride;
     p.scale = d->scale;
-    const int units = device_compute_units() > 0 ? device_compute_units() : 256;
-    if (d->dtype == REFORM_BF16) tree_plan_bf16(p, units);
-    else tree_plan_f32(p, units);
+    if (d->dtype == REFORM_BF16) tree_plan_bf16(p, compute_units());
+    else tree_plan_f32(p, compute_units());
     return p;
 }
 
@@ -132,29 +156,29 @@ extern "C" {
 // ---------------------------------------------------------------------------------------
 size_t reform_prompt_attend_workspace(const reform_prompt_desc *d)
 {
-    (void)check_prompt(d);
-    return 0;
+    if (check_prompt(d) != REFORM_OK || d->n_seq == 0 || d->n_q_rows == 0) return 0;
+    const PromptParams p = prompt_sizes(d);
+    return prompt_part_rows(p) * (tree_part_dim(d->dtype == REFORM_BF16, p.D) * sizeof(float) + sizeof(float2));
 }
 
 reform_status reform_prompt_attend(const reform_prompt_desc *d, const void *q, const void *k, const void *v,
                                    const int32_t *cu_q, const int32_t *cu_k, void *out, float *lse, void *workspace,
                                    size_t workspace_bytes, void *hip_stream)
 {
-    (void)workspace;
-    (void)workspace_bytes;
     const reform_status rc = check_prompt(d);
     if (rc != REFORM_OK) return rc;
     if (d->n_q_rows == 0 || d->n_seq == 0) return REFORM_OK;
     if (!q || !out || !cu_q || (d->n_k_rows > 0 && (!k || !v))) return REFORM_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return REFORM_ERR_INVALID_ARG;
-    PromptParams p;
-    std::memset(&p, 0, sizeof(p));
+    PromptParams p = prompt_sizes(d);
     p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse; p.cu_q = cu_q; p.cu_k = cu_k;
-    p.Hq = d->n_q_heads; p.Hkv = d->n_kv_heads; p.G = p.Hq / p.Hkv; p.D = d->head_dim;
-    p.n_seq = d->n_seq; p.n_q = d->n_q_rows; p.n_k = d->n_k_rows;
-    p.q_hs = d->q_head_stride; p.q_rs = d->q_row_stride; p.k_hs = d->k_head_stride; p.k_rs = d->k_row_stride;
-    p.v_hs = d->v_head_stride; p.v_rs = d->v_row_stride; p.o_hs = d->o_head_stride; p.o_rs = d->o_row_stride;
-    p.scale = d->scale;
+    if (p.shares) {
+        const size_t row = tree_part_dim(d->dtype == REFORM_BF16, p.D) * sizeof(float);
+        if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < prompt_part_rows(p) * (row + sizeof(float2)))
+            return REFORM_ERR_WORKSPACE;
+        p.part_o = (float *)workspace;
+        p.part_ml = (float2 *)((char *)workspace + prompt_part_rows(p) * row);
+    }
     hipStream_t st = (hipStream_t)hip_stream;
     const hipError_t e = d->dtype == REFORM_BF16 ? prompt_attend_bf16(p, st) : prompt_attend_f32_launch(p, st);
     return e == hipSuccess ? REFORM_OK : REFORM_ERR_RUNTIME;

@@ -210,19 +210,78 @@ __device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
     }
 }
 
-// The pieces of the items that several shares covered.  A workgroup has `rows` rows (a power of two) of the item that the end of its
-// share cuts (by_share), or of an item whether it is cut or not; a thread has
-// four columns of one of them and every n-th piece, which it adds up against the largest reference of its own,
-// references, sums and columns all loaded at once; then the n threads' sums meet in LDS.  The order is that of the
-// shares, whoever is done first.
 constexpr int kTreeMaxShares = 512;
 
-template <int D, int R, int TK, bool BF16>
-__global__ __launch_bounds__(256) void tree_merge(TreeParams p, int rows, int by_share)
+// Row r0 + r of an item's n pieces, piece x in slot slot(x), put together by a workgroup of 256 threads that has `rows` rows (a power of
+// two), of which `here` exist.  A thread has four columns of one of them and every n-th piece, which it adds up against the largest
+// reference of its own, references, sums and columns all loaded at once; then the n threads' sums meet in LDS.  The order is that
+// of the shares, whoever is done first.  True for the threads that then have the result of row r, columns c4 on.
+template <int D, class SLOT>
+__device__ __forceinline__ bool merge_pieces(const float *part_o, const float2 *part_ml, int part_rows, int n, int r0, int here, int rows,
+                                             SLOT slot, int &r, int &c4, f32x4 &y, float &m, float &l)
 {
     constexpr int C4 = D / 4, BATCH = 4;                 // quads of a row, pieces of a trip
     __shared__ f32x4 so[256];
     __shared__ float2 sml[256];
+    const int group = rows * C4, groups = 256 / group;   // threads that have different quads
+    const int g = threadIdx.x / group, q = threadIdx.x - g * group;
+    r = q / C4;
+    c4 = q % C4 * 4;
+    y = (f32x4){0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
+    if (g < groups && r < here) {
+        for (int w = g; w < n; w += BATCH * groups) {
+            float2 ml[BATCH];
+            f32x4 o[BATCH];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {            // pieces past the last repeat it, without weight
+                const int x = min(w + i * groups, n - 1);
+                const size_t at = (size_t)slot(x) * part_rows + r0 + r;
+                ml[i] = part_ml[at];
+                o[i] = *(const f32x4 *)(part_o + at * D + c4);
+            }
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                if (w + i * groups >= n) ml[i] = make_float2(-INFINITY, 0.f);
+                top = fmaxf(top, ml[i].x);
+            }
+            const float ref = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(m - ref);
+            y *= old;
+            l *= old;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                if (w + i * groups >= n) continue;
+                const float f = __builtin_amdgcn_exp2f(ml[i].x - ref);           // 0 where no key was seen
+                l += ml[i].y * f;
+                y += o[i] * f;
+            }
+            m = top;
+        }
+    }
+    so[threadIdx.x] = y;
+    sml[threadIdx.x] = make_float2(m, l);
+    __syncthreads();
+    if (g != 0 || r >= here) return false;
+    for (int i = 1; i < groups; ++i) m = fmaxf(m, sml[i * group + q].x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    y = (f32x4){0.f, 0.f, 0.f, 0.f};
+    l = 0.f;
+    for (int i = 0; i < groups; ++i) {
+        const float2 ml = sml[i * group + q];
+        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+        l += ml.y * f;
+        y += so[i * group + q] * f;
+    }
+    return true;
+}
+
+// The pieces of the items that several shares covered.  A workgroup has `rows` rows of the item that the end of its share cuts (by_share), or
+// of an item whether it is cut or not.
+template <int D, int R, int TK, bool BF16>
+__global__ __launch_bounds__(256) void tree_merge(TreeParams p, int rows, int by_share)
+{
     TreeList<R, TK> list;
     list.read(p);
     if (list.total == 0) return;
@@ -253,64 +312,20 @@ __global__ __launch_bounds__(256) void tree_merge(TreeParams p, int rows, int by
     const int n = list.share_of(pos + seq.tiles - 1) - w0 + 1;
     const int r0 = chunk * rows, here = min(rows, seq.nodes * p.G - rb * R - r0);
     if (n == 1 || here <= 0) return;
-    const int group = rows * C4, groups = 256 / group;   // threads that have different quads
-    const int g = threadIdx.x / group, q = threadIdx.x - g * group, r = q / C4, c4 = q % C4 * 4;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    if (g < groups && r < here) {
-        for (int w = g; w < n; w += BATCH * groups) {
-            float2 ml[BATCH];
-            f32x4 o[BATCH];
-#pragma unroll
-            for (int i = 0; i < BATCH; ++i) {            // pieces past the last repeat it, without weight
-                const int x = min(w + i * groups, n - 1);
-                const size_t at = (size_t)tree_slot(p, w0 + x, x, rb) * p.part_rows + r0 + r;
-                ml[i] = p.part_ml[at];
-                o[i] = *(const f32x4 *)(p.part_o + at * D + c4);
-            }
-            float top = m;
-#pragma unroll
-            for (int i = 0; i < BATCH; ++i) {
-                if (w + i * groups >= n) ml[i] = make_float2(-INFINITY, 0.f);
-                top = fmaxf(top, ml[i].x);
-            }
-            const float ref = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(m - ref);
-            y *= old;
-            l *= old;
-#pragma unroll
-            for (int i = 0; i < BATCH; ++i) {
-                if (w + i * groups >= n) continue;
-                const float f = __builtin_amdgcn_exp2f(ml[i].x - ref);           // 0 where no key was seen
-                l += ml[i].y * f;
-                y += o[i] * f;
-            }
-            m = top;
-        }
+    int r, c4;
+    f32x4 y;
+    float m, l;
+    if (!merge_pieces<D>(p.part_o, p.part_ml, p.part_rows, n, r0, here, rows, [&](int x) { return tree_slot(p, w0 + x, x, rb); }, r, c4, y, m, l))
+        return;
+    const int row = rb * R + r0 + r, node = row / p.G, head = kvh * p.G + row % p.G;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const size_t dst = (size_t)b * p.o_ss + (size_t)head * p.o_hs + (size_t)node * p.o_rs + c4;
+    y *= inv;
+    if (c4 < p.D) {
+        if (BF16) *(v2u *)((u16 *)p.out + dst) = (v2u){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+        else *(f32x4 *)((float *)p.out + dst) = y;
     }
-    so[threadIdx.x] = y;
-    sml[threadIdx.x] = make_float2(m, l);
-    __syncthreads();
-    if (g == 0 && r < here) {
-        for (int i = 1; i < groups; ++i) m = fmaxf(m, sml[i * group + q].x);
-        const float ref = m == -INFINITY ? 0.f : m;
-        y = (f32x4){0.f, 0.f, 0.f, 0.f};
-        l = 0.f;
-        for (int i = 0; i < groups; ++i) {
-            const float2 ml = sml[i * group + q];
-            const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-            l += ml.y * f;
-            y += so[i * group + q] * f;
-        }
-        const int row = rb * R + r0 + r, node = row / p.G, head = kvh * p.G + row % p.G;
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        const size_t dst = (size_t)b * p.o_ss + (size_t)head * p.o_hs + (size_t)node * p.o_rs + c4;
-        y *= inv;
-        if (c4 < p.D) {
-            if (BF16) *(v2u *)((u16 *)p.out + dst) = (v2u){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
-            else *(f32x4 *)((float *)p.out + dst) = y;
-        }
-        if (c4 == 0 && p.lse) p.lse[((size_t)b * p.Hq + head) * p.T + node] = (m + __builtin_amdgcn_logf(l)) * kLn2;
-    }
+    if (c4 == 0 && p.lse) p.lse[((size_t)b * p.Hq + head) * p.T + node] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // With more items than shares most are finished by one workgroup, so the shares' ends are gone through, else the items (32/8 heads of

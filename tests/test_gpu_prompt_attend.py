@@ -222,3 +222,40 @@ def test_descending_boundaries_of_many_sequences_touch_nothing_outside():
     out, lse = binding.reform_prompt_attend(q, k, v, i32([0, rows]), 0.125)
     want, wl, a, err = ref.prompt_attend(q.cpu(), k.cpu(), v.cpu(), [rows], [rows], 0.125)
     ref.check_attention(out, lse, want, wl, a, err, rows, BF)
+
+
+@pytest.mark.parametrize("hq,hkv,d,q_lens,k_lens,dtype", [
+    (8, 2, 128, [3], [9000], BF), (4, 4, 128, [1, 0, 5, 2], [4000, 0, 3, 6001], BF), (16, 2, 128, [7, 1], [5000, 64], BF),
+    (4, 4, 64, [1] * 3, [9000, 33, 8000], BF), (6, 2, 64, [9, 1, 30], [9000, 9000, 0], BF), (4, 1, 64, [40, 3], [9000, 2], BF),
+    (8, 2, 128, [20, 6], [4, 7000], BF), (2, 1, 128, [1] * 30, [4000] * 29 + [5], BF),
+    (4, 2, 64, [3, 0, 20], [3000, 5, 7], F), (2, 2, 128, [1, 2], [2500, 1], F), (8, 1, 36, [5], [6000], F), (4, 2, 200, [2, 9], [1200, 4], F),
+])
+def test_keys_shared_out(hq, hkv, d, q_lens, k_lens, dtype):
+    """Few rows behind many keys: blocks that several workgroups go through, beside sequences without rows or keys and rows that see nothing."""
+    q, kv = torch.empty((hq, sum(q_lens), d), dtype=dtype, device="meta"), torch.empty((hkv, sum(k_lens), d), dtype=dtype, device="meta")
+    assert binding.prompt_workspace_bytes(binding.prompt_desc(q, kv, kv, q, torch.empty(len(q_lens) + 1), 0.1)) > 0
+    got = run_case(hq, hkv, d, q_lens, k_lens, dtype, seed=sum(q_lens) + d, spare=3)
+    again = run_case(hq, hkv, d, q_lens, k_lens, dtype, seed=sum(q_lens) + d, spare=3)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+    run_case(hq, hkv, d, q_lens, k_lens, dtype, seed=d, layout="tokens", sharp=9.0)
+
+
+def test_shared_out_boundaries_and_workspace():
+    """Boundaries outside are moved in here as well; a workspace of NaN leaves no trace; one that is too small is refused."""
+    g = torch.Generator().manual_seed(31)
+    q, k, v = ref.randn(g, 4, 12, 128, dtype=BF).to(DEV), ref.randn(g, 2, 9000, 128, dtype=BF).to(DEV), ref.randn(g, 2, 9000, 128, dtype=BF).to(DEV)
+    cu_q, cu_k = i32([-3, 4, 4, 2, 6, 1 << 30]), i32([-9, 5000, 70, 100, 8000, 1 << 30])
+    need = binding.prompt_workspace_bytes(binding.prompt_desc(q, k, v, q, cu_q, 0.1))
+    assert need > 0
+    ws = torch.full((need + 256,), 0xff, dtype=torch.uint8, device=DEV)
+    out, lse = binding.reform_prompt_attend(q, k, v, cu_q, 0.1, cu_k=cu_k, workspace=ws)
+    # [0, 4) over keys [0, 5000), [2, 6) over [100, 8000), [6, 12) over [8000, 9000); rows 2 and 3 belong to two
+    for lo, hi, k0, k1, own in ((0, 4, 0, 5000, slice(0, 2)), (2, 6, 100, 8000, slice(2, 4)), (6, 12, 8000, 9000, slice(0, 6))):
+        want, wl, a, err = ref.prompt_attend(q[:, lo:hi].cpu(), k[:, k0:k1].cpu(), v[:, k0:k1].cpu(), [hi - lo], [k1 - k0], 0.1)
+        ref.check_attention(out[:, lo:hi][:, own], lse[:, lo:hi][:, own], want[:, own], wl[:, own], a[:, own], err[:, own], k1 - k0, BF, f"{lo}")
+    with pytest.raises(binding.ReformError, match="WORKSPACE"):
+        binding.reform_prompt_attend(q, k, v, cu_q, 0.1, cu_k=cu_k, workspace=ws[:need // 2])
+    # a broken sequence leaves its neighbours as they are
+    k[:, 20], v[:, 30] = math.nan, math.inf
+    dirty = binding.reform_prompt_attend(q, k, v, cu_q, 0.1, cu_k=cu_k, workspace=ws)
+    assert torch.equal(dirty[0][:, 4:], out[:, 4:]) and torch.equal(dirty[1][:, 4:], lse[:, 4:]) and bool(torch.isnan(dirty[0][:, :2]).all())

@@ -230,3 +230,14 @@ def test_outputs_that_overlap_are_refused():
             assert lib.reform_tree_accept(ctypes.byref(accept()), FAKE, 2 * FAKE, 3 * FAKE, 4 * FAKE, 5 * FAKE, None, None, *outs, None) == 1
         outs[at] = outs[at - 1] = 6 * FAKE                                                             # another output
         assert lib.reform_tree_accept(ctypes.byref(accept()), FAKE, 2 * FAKE, 3 * FAKE, 4 * FAKE, 5 * FAKE, None, None, *outs, None) == 1
+
+
+def test_prompts_that_need_a_workspace():
+    lib = binding.load_library()
+    many = prompt(n_q_rows=3, n_k_rows=20000, k_head_stride=20000 * 128, v_head_stride=20000 * 128)
+    need = lib.reform_prompt_attend_workspace(ctypes.byref(many))
+    assert need > 0 and call_prompt(many) == 3
+    for ws, nbytes in ((FAKE, need - 1), (FAKE + 16, need)):
+        assert lib.reform_prompt_attend(ctypes.byref(many), FAKE, FAKE, FAKE, FAKE, None, FAKE, None, ws, nbytes, None) == 3
+    for kw in (dict(n_q_rows=0), dict(n_seq=0), dict(n_q_rows=100), dict(n_seq=65), dict(scale=0.0)):
+        assert lib.reform_prompt_attend_workspace(ctypes.byref(prompt(**kw))) == 0
