@@ -230,7 +230,7 @@ void prompt_plan_f32(PromptParams &p)
     const double step = 0.03 * (p.D <= 32 ? 32 : p.D <= 64 ? 64 : p.D <= 128 ? 128 : 256), keys = (double)p.n_k / p.n_seq;
     const double blocks = ((double)p.n_q * p.G / kF32Rows + p.n_seq) * p.Hkv, full = blocks * (keys / 128.0 + 1.0) * step / p.units;
     const double alone = keys / 128.0 * step, memory = blocks * keys * p.D * 8.0 / 3.5e6;
-    if (alone < 8.0 || p.n_seq > 64 || blocks * ((double)p.n_k / kF32Keys + 16.0) >= 1073741824.0) return;
+    if (alone < 8.0 || p.n_seq > 64 || blocks * ((double)p.n_k / kF32Keys + 16.0) >= 33554432.0) return;          // as in prompt_share_rows
     if (std::cbrt(full * full * full + alone * alone * alone) < 8.0 + (full > memory ? full : memory)) return;
     const int rows = p.n_q * p.G;
     p.block = kF32Rows;

@@ -84,8 +84,8 @@ inline int prompt_share_rows(int head_dim, int G, int Hkv, int n_seq, int n_q, i
     static const PromptShared forms64[2] = {{{16, 4, 32, 0.73, 0.0, 12.0, 2.3}, 256}, {{32, 4, 32, 0.84, 0.0, 12.0, 3.45}, 128}};
     static const PromptShared forms128[2] = {{{16, 8, 32, 3.2, 0.0, 12.0, 9.3}, 128}, {{32, 8, 32, 4.1, 0.0, 12.0, 12.7}, 128}};
     if ((double)n_k / n_seq * (head_dim == 64 ? 0.788 : 1.62) < 256.0 * 2.5) return 0;      // a block's chain takes less than the second launch
-    // places are counted in 32 bits, sequences one to a lane
-    if (n_seq > 64 || ((double)n_q * G / 16.0 + n_seq) * Hkv * ((double)n_k / 32.0 + 16.0) >= 1073741824.0) return 0;
+    // sequences one to a lane, places counted in 32 bits, also where broken boundaries give all rows to every one of them
+    if (n_seq > 64 || ((double)n_q * G / 16.0 + n_seq) * Hkv * ((double)n_k / 32.0 + 16.0) >= 33554432.0) return 0;
     const PromptForm *whole = prompt_forms(head_dim);
     double least = prompt_estimate(whole[0], G, Hkv, n_seq, n_q, n_k, units);
     for (int i = 1; i < kPromptForms; ++i) least = std::min(least, prompt_estimate(whole[i], G, Hkv, n_seq, n_q, n_k, units));

@@ -259,3 +259,30 @@ def test_shared_out_boundaries_and_workspace():
     k[:, 20], v[:, 30] = math.nan, math.inf
     dirty = binding.reform_prompt_attend(q, k, v, cu_q, 0.1, cu_k=cu_k, workspace=ws)
     assert torch.equal(dirty[0][:, 4:], out[:, 4:]) and torch.equal(dirty[1][:, 4:], lse[:, 4:]) and bool(torch.isnan(dirty[0][:, :2]).all())
+
+
+def test_many_heads_of_one_group():
+    run_case(64, 1, 64, [70, 3, 0, 1], [70, 3, 0, 1], BF, seed=64)
+    run_case(64, 1, 128, [2, 1], [5000, 9000], BF, seed=65)
+    run_case(48, 1, 32, [9, 20], [9, 1700], F, seed=66)
+
+
+def test_shared_out_calls_replay_from_a_graph():
+    """Captured with its workspace, replayed on new lengths with eager calls of the same workspace in between."""
+    g = torch.Generator().manual_seed(77)
+    q, k, v = (ref.randn(g, h, n, 128, dtype=BF).to(DEV) for h, n in ((8, 20), (2, 12000), (2, 12000)))
+    cu_q, cu_k = i32([0, 4, 20]), i32([0, 5000, 12000])
+    out, lse = torch.zeros_like(q), torch.zeros((8, 20), device=DEV)
+    need = binding.prompt_workspace_bytes(binding.prompt_desc(q, k, v, out, cu_q, 0.1))
+    assert need > 0
+    ws = torch.empty(need + 256, dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.reform_prompt_attend(q, k, v, cu_q, 0.1, cu_k=cu_k, out=out, lse=lse, workspace=ws)
+    for cuts, ends in (([0, 4, 20], [0, 5000, 12000]), ([0, 19, 20], [0, 30, 12000]), ([0, 0, 20], [0, 11000, 11900]), ([0, 4, 20], [0, 5000, 12000])):
+        cu_q.copy_(torch.tensor(cuts))
+        cu_k.copy_(torch.tensor(ends))
+        graph.replay()
+        got = out.clone(), lse.clone()
+        eager = binding.reform_prompt_attend(q, k, v, cu_q, 0.1, cu_k=cu_k, workspace=ws)
+        assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1])

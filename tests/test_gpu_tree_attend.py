@@ -211,3 +211,10 @@ def test_every_form_whole(hq, hkv, d, T, n, top):
     q, kv = torch.empty((n, hq, T, d), dtype=BF, device="meta"), torch.empty((n, hkv, top + T, d), dtype=BF, device="meta")
     assert binding.tree_workspace_bytes(binding.tree_desc(q, kv, kv, q, 0.1)) == 0
     run_case(hq, hkv, d, T, lens, BF, seed=T + n, spare=0, counts=[rnd.choice([T, T, rnd.randint(0, T)]) for _ in lens])
+
+
+def test_many_heads_of_one_group():
+    """2560 rows of one KV head: up to 160 row blocks to a sequence."""
+    run_case(64, 1, 64, 40, [500, 3], BF, seed=64)
+    run_case(64, 1, 128, 40, [300], BF, seed=65, spare=40000)
+    run_case(48, 1, 32, 9, [700, 0], F, seed=66)
