@@ -21,10 +21,12 @@ namespace reform {
 
 constexpr int kRowsKeys = 64;
 
-// KG groups of NW waves each: the groups have the same rows and take every KG-th tile.
-template <int D, int NW, int KG>
+// KG groups of NW waves each: the groups have the same rows and take every KG-th tile.  THIN: 16 rows instead of 32 for the upper half
+// of eight waves.
+template <int D, int NW, int KG, bool THIN = false>
 struct RowsShape {
-    static constexpr int ROWS = NW * 32, BN = kRowsKeys, C8 = D / 8;
+    static_assert(!THIN || NW == 8, "two waves to a SIMD");
+    static constexpr int ROWS = THIN ? 192 : NW * 32, BN = kRowsKeys, C8 = D / 8;
     static constexpr int CHUNKS = BN * D / 512, PITCH = 512 + 16, TILE = CHUNKS * PITCH;      // elements
     static constexpr int LOADS = CHUNKS / NW;            // of a wave, for K and for V
     static constexpr bool LAG = NW == 8;                 // the upper half of the waves runs P.V one tile late
@@ -70,7 +72,7 @@ enum RowsStep { kRowsIdle, kRowsAll, kRowsFirst, kRowsLag, kRowsLast };
 
 // The pointers are to different tiles of the LDS; `next_*` are the ones that the loads under way fill.  That
 // they are different is what lets the compiler read the others without waiting for these loads.
-template <int D, int NW, int KG, int STEP, class MASK>
+template <int D, int NW, int KG, int STEP, int NB, class MASK>
 __device__ __forceinline__ void rows_tile(RowsWave<D> &w, const u16 *__restrict__ tk, const u16 *__restrict__ tv,
                                             u16 *__restrict__ next_k, u16 *__restrict__ next_v, const char *from_k, const char *from_v,
                                             size_t step_k, size_t step_v, bool loads, float c, MASK mask_tile)
@@ -100,7 +102,7 @@ __device__ __forceinline__ void rows_tile(RowsWave<D> &w, const u16 *__restrict_
 #pragma unroll
         for (int f = 0; f < NV; ++f) {
             w.o[0][f % DB] = mfma16(fw[f % kWin], w.pb[0][f / DB], w.o[0][f % DB]);
-            w.o[1][f % DB] = mfma16(fw[f % kWin], w.pb[1][f / DB], w.o[1][f % DB]);
+            if (NB == 2) w.o[1][f % DB] = mfma16(fw[f % kWin], w.pb[1][f / DB], w.o[1][f % DB]);
             const int g = f + kWin;
             if (g < NV) fw[f % kWin] = vfrag(g);
             else if (STEP == kRowsLag) fw[f % kWin] = kfrag(g - NV);
@@ -108,12 +110,12 @@ __device__ __forceinline__ void rows_tile(RowsWave<D> &w, const u16 *__restrict_
         __builtin_amdgcn_sched_group_barrier(0x100, 2 * kWin, 0);
 #pragma unroll
         for (int f = 0; f < NV - kWin; ++f) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);               // a V^T fragment is two reads
         }
 #pragma unroll
         for (int f = NV - kWin; f < NV; ++f) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, STEP == kRowsLag ? 1 : 0, 0);
         }
     }
@@ -122,15 +124,15 @@ __device__ __forceinline__ void rows_tile(RowsWave<D> &w, const u16 *__restrict_
 #pragma unroll
             for (int i = 0; i < kWin; ++i) fw[i] = kfrag(i);
         }
-        f32x4 s[2][4];
+        f32x4 s[NB][4];
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) s[nb][kb] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int f = 0; f < NK; ++f) {
             s[0][f & 3] = mfma16(fw[f % kWin], w.q[0][f >> 2], s[0][f & 3]);
-            s[1][f & 3] = mfma16(fw[f % kWin], w.q[1][f >> 2], s[1][f & 3]);
+            if (NB == 2) s[1][f & 3] = mfma16(fw[f % kWin], w.q[1][f >> 2], s[1][f & 3]);
             const int g = f + kWin;
             if (g < NK) fw[f % kWin] = kfrag(g);
             else if (STEP == kRowsAll) fw[f % kWin] = vfrag(g - NK);
@@ -138,22 +140,22 @@ __device__ __forceinline__ void rows_tile(RowsWave<D> &w, const u16 *__restrict_
         if (STEP != kRowsLag) __builtin_amdgcn_sched_group_barrier(0x100, kWin, 0);
 #pragma unroll
         for (int f = 0; f < NK - kWin; ++f) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
 #pragma unroll
         for (int f = NK - kWin; f < NK; ++f) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, STEP == kRowsAll ? 2 : 0, 0);
         }
         mask_tile(s);
-        float rs[2];
+        float rs[NB];
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb) rs[nb] = softmax_row(s[nb], c, w.m[nb] * c, w.pb[nb]);
-        if (__builtin_amdgcn_ballot_w64(!(rs[0] < kBigSum) || !(rs[1] < kBigSum)) != 0ull) {
+        for (int nb = 0; nb < NB; ++nb) rs[nb] = softmax_row(s[nb], c, w.m[nb] * c, w.pb[nb]);
+        if (__builtin_amdgcn_ballot_w64(!(rs[0] < kBigSum) || !(rs[NB - 1] < kBigSum)) != 0ull) {
             asm volatile("; rescale path" ::: "memory");
 #pragma unroll
-            for (int nb = 0; nb < 2; ++nb) {
+            for (int nb = 0; nb < NB; ++nb) {
                 float mx = s[nb][0][0];
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb)
@@ -173,19 +175,19 @@ __device__ __forceinline__ void rows_tile(RowsWave<D> &w, const u16 *__restrict_
                 rs[nb] = softmax_row(s[nb], c, ref, w.pb[nb]);
             }
         }
-        w.l[0] += rs[0];
-        w.l[1] += rs[1];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) w.l[nb] += rs[nb];
     }
     if constexpr (STEP == kRowsAll) {
 #pragma unroll
         for (int f = 0; f < NV; ++f) {
             w.o[0][f % DB] = mfma16(fw[f % kWin], w.pb[0][f / DB], w.o[0][f % DB]);
-            w.o[1][f % DB] = mfma16(fw[f % kWin], w.pb[1][f / DB], w.o[1][f % DB]);
+            if (NB == 2) w.o[1][f % DB] = mfma16(fw[f % kWin], w.pb[1][f / DB], w.o[1][f % DB]);
             if (f + kWin < NV) fw[f % kWin] = vfrag(f + kWin);
         }
 #pragma unroll
         for (int f = 0; f < NV - kWin; ++f) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
     }
@@ -193,11 +195,11 @@ __device__ __forceinline__ void rows_tile(RowsWave<D> &w, const u16 *__restrict_
 
 // Key tiles [t0, t1) of the sequence for the block of ROWS rows from r.row0 on, as seq_segment.  Prompts begin at
 // tile 0; by_head: how the rows are dealt to the waves.
-template <int D, int NW, int KG, bool TREE>
+template <int D, int NW, int KG, bool TREE, bool THIN = false>
 __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool by_head, float scale, int t0, int t1, float *po,
                                              float2 *pml, u16 *lds)
 {
-    using S = RowsShape<D, NW, KG>;
+    using S = RowsShape<D, NW, KG, THIN>;
     constexpr int BN = S::BN, TILE = S::TILE, KS = S::KS, DB = S::DB, C8 = S::C8;
     if (TREE) {                                          // keys are counted from the range's first one
         k.k = (const u16 *)k.k + (size_t)t0 * BN * k.k_rs;
@@ -211,7 +213,8 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
     u16 *ldsK = lds + kg * S::GROUP, *ldsV = ldsK + S::KSLOTS * TILE;        // [KSLOTS][TILE], [VSLOTS][TILE]
     // the wave's 32 rows: by_head (G divides the waves): consecutive query rows of one head, else consecutive rows
     const int slab = by_head ? wave / r.G : wave, rstep = by_head ? r.G : 1;
-    const int row0 = r.row0 + slab * 32 * rstep + (by_head ? wave % r.G : 0);
+    const bool thin = THIN && wave >= NW / 2;            // then the second 16 rows do not exist, and nothing of theirs is computed or stored
+    const int row0 = r.row0 + (thin ? 128 + (wave - NW / 2) * 16 : slab * 32 * rstep + (by_head ? wave % r.G : 0));
     // formed where needed, from values that the compiler cannot relate to the other uses: kept, they cost registers in the loop
     auto locate = [&](int nb, int &at, int &head) {
         int G = r.G, l = lane;
@@ -241,7 +244,7 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
     const int steps = (ntiles + KG - 1) / KG;
     int tl = -1;                                         // last tile of the group that the wave needs
     if (row0 < r.rows) {
-        const int last = TREE ? k.n - 1 : M + min(row0 + 31 * rstep, r.rows - 1) / r.G;
+        const int last = TREE ? k.n - 1 : M + min(row0 + 31 * rstep, r.rows - 1) / r.G;       // prompts have no thin waves
         if (last >= kg * BN && kg < ntiles) tl = (min(last / BN, ntiles - 1) - kg) / KG;       // a range may have fewer tiles than groups
     }
     const int open = TREE ? k.open : M + row0 / r.G + 1; // keys below it are seen by all of the wave's rows
@@ -272,12 +275,13 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(w.q[nb][ks]));
     int t = 0, kslot = 0, vslot = 0;                     // the slots of tile t: t mod KSLOTS, t mod VSLOTS
-    auto mask_tile = [&](f32x4 (&s)[2][4]) {
+    auto mask_tile = [&](auto &s) {
+        constexpr int NB = sizeof(s) / sizeof(s[0]);
         const int j0 = (t * KG + kg) * BN;
         if (j0 + BN > open) {
             asm volatile("; mask path" ::: "memory");
 #pragma unroll
-            for (int nb = 0; nb < 2; ++nb) {
+            for (int nb = 0; nb < NB; ++nb) {
                 int at, head;
                 locate(nb, at, head);
                 int l = lane;
@@ -303,8 +307,9 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
         }
     };
     // one tile for every wave of the workgroup, whatever it does with it
+    constexpr int LAG_NB = THIN ? 1 : 2;
     auto step = [&](auto what) {
-        constexpr int STEP = decltype(what)::value;
+        constexpr int STEP = decltype(what)::value, NB = STEP == kRowsFirst || STEP == kRowsLag || STEP == kRowsLast ? LAG_NB : 2;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // the wave's part of tile t is there ...
         __builtin_amdgcn_s_barrier();                    // ... everyone's is, and the tiles that are loaded over have been read
         asm volatile("" ::: "memory");
@@ -315,7 +320,7 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
         if (more && !whole) load_end(t + 1, nk, nv);
         const size_t j1 = (size_t)next * BN;
         const int vread = STEP == kRowsLag || STEP == kRowsLast ? after(vslot, S::VSLOTS - 1, S::VSLOTS) : vslot;
-        rows_tile<D, NW, KG, STEP>(w, ldsK + kslot * TILE, ldsV + vread * TILE, nk, nv,
+        rows_tile<D, NW, KG, STEP, NB>(w, ldsK + kslot * TILE, ldsV + vread * TILE, nk, nv,
                                       (const char *)((const u16 *)k.k + j1 * k.k_rs) + koff, (const char *)((const u16 *)k.v + j1 * k.v_rs) + voff,
                                       step_k, step_v, more && whole, c, mask_tile);
         kslot ^= 1;
@@ -333,7 +338,7 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
         if (t < steps) {
             step(std::integral_constant<int, kRowsLast>());
         } else {
-            rows_tile<D, NW, KG, kRowsLast>(w, ldsK, ldsV + (vslot == 0 ? S::VSLOTS - 1 : vslot - 1) * TILE, wk, wv, nullptr, nullptr, 0, 0, false,
+            rows_tile<D, NW, KG, kRowsLast, LAG_NB>(w, ldsK, ldsV + (vslot == 0 ? S::VSLOTS - 1 : vslot - 1) * TILE, wk, wv, nullptr, nullptr, 0, 0, false,
                                             c, mask_tile);
         }
     }
@@ -377,7 +382,7 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
     for (int nb = 0; nb < 2; ++nb) {
         const float l = w.l[nb];
         const int row = row0 + rstep * (16 * nb + ln);
-        if (row >= r.rows) continue;
+        if (row >= r.rows || (thin && nb == 1)) continue;
         if (pml) {
 #pragma unroll
             for (int db = 0; db < DB; ++db) *(f32x4 *)(po + (size_t)(row - r.row0) * D + db * 16 + 4 * lg) = w.o[nb][db];

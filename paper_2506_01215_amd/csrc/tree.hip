@@ -11,7 +11,8 @@
 // 37.6 us with 8 waves, 31.6 with 4; one token, 32/8 of 128, 16 caches of up to 8000 rows 49.7 with 8, 50.2 with 4.
 // 64 rows: two groups of two waves that divide the tiles, one such workgroup to a compute unit, so that there are half as many pieces to
 // put together as with two workgroups of two waves (36 batches of 33 to 64 rows over 200 to 12500 keys, mean: 0.89 of the time; four groups at
-// head_dim 64 0.92).  128 rows: two groups take as long as two workgroups (25 batches, 1.00).
+// head_dim 64 0.92).  128 rows: two groups take as long as two workgroups (25 batches, 1.00).  192 rows: a wave of 32 and one of 16 to each SIMD (48
+// nodes over 16640 rows, 32/8 of 128 32.1 -> 30.1 us against a block of 256; 32 caches of up to 4492 rows, 48 nodes, 32/8 of 64 81 -> 74).
 #include "attend_rows.h"
 #include "tree_list.h"
 
@@ -28,13 +29,13 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_attend(TreeParams p)
     });
 }
 
-template <int D, int NW, int KG>
+template <int D, int NW, int KG, bool THIN>
 __global__ __launch_bounds__(NW * KG * 64, 2) void tree_attend_rows(TreeParams p)
 {
-    using S = RowsShape<D, NW, KG>;
+    using S = RowsShape<D, NW, KG, THIN>;
     extern __shared__ __attribute__((aligned(16))) u16 lds[];
     tree_walk<u16, S::ROWS, S::BN>(p, [&](const SeqRows &r, const SeqKeys &k, int t0, int t1, long slot) {
-        rows_segment<D, NW, KG, true>(r, k, false, p.scale, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
+        rows_segment<D, NW, KG, true, THIN>(r, k, false, p.scale, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
                                   slot < 0 ? nullptr : p.part_ml + (size_t)slot * p.part_rows, lds);
     });
 }
@@ -54,7 +55,13 @@ int tree_rows(const TreeParams &p, int compute_units)
     if (few(16, narrow ? 1600 : 1300)) return 16;
     if (few(32, narrow ? 1800 : 600)) return 32;
     if (few(64, narrow ? 2000 : 1000)) return 64;
-    return rows > 128 && (rows + 127) / 128 % 2 == 0 ? 256 : 128;           // 256 where it is not half empty
+    if (rows <= 128) return 128;
+    if (rows <= 192) return 192;
+    const int by_128 = (rows + 127) / 128, by_192 = (rows + 191) / 192;
+    if (by_128 % 2 == 0) return 256;                     // none is half empty
+    // As few rows empty by 192, and K and V read less often: 371 rows of 32 x 4 caches of up to 1328 keys, 128 wide, 37.3 us against 41.3; but 64
+    // wide 74.6 against 73.0 (280 of 64 x 4 of up to 2351), and where the chip is not busy 35.2 against 28.0 (304 of 32 x 2 of up to 1035).
+    return !narrow && by_192 * 192 <= by_128 * 128 && by_192 * keys > 1500 ? 192 : 128;
 }
 
 // Keys of a tile.
@@ -72,14 +79,14 @@ hipError_t launch(const TreeParams &p, hipStream_t st)
     return hipGetLastError();
 }
 
-template <int D, int NW, int KG>
+template <int D, int NW, int KG, bool THIN = false>
 hipError_t launch_long(const TreeParams &p, hipStream_t st)
 {
-    using S = RowsShape<D, NW, KG>;
-    const hipError_t e = raise_lds<tree_attend_rows<D, NW, KG>>(S::lds_bytes);
+    using S = RowsShape<D, NW, KG, THIN>;
+    const hipError_t e = raise_lds<tree_attend_rows<D, NW, KG, THIN>>(S::lds_bytes);
     if (e != hipSuccess) return e;
     const unsigned grid = (unsigned)(p.shares ? p.shares : p.n_seq * p.Hkv) * p.row_blocks;
-    hipLaunchKernelGGL((tree_attend_rows<D, NW, KG>), dim3(grid), dim3(NW * KG * 64), S::lds_bytes, st, p);
+    hipLaunchKernelGGL((tree_attend_rows<D, NW, KG, THIN>), dim3(grid), dim3(NW * KG * 64), S::lds_bytes, st, p);
     if (p.shares) tree_merge_launch<D, S::ROWS, S::BN, true>(p, st);
     return hipGetLastError();
 }
@@ -93,6 +100,7 @@ hipError_t launch_rows(const TreeParams &p, hipStream_t st)
     if (R == 32) return launch<D, 2, NW>(p, st);
     if (R == 64) return launch_long<D, 2, 2>(p, st);
     if (R == 128) return launch_long<D, 4, 1>(p, st);
+    if (R == 192) return launch_long<D, 8, 1, true>(p, st);
     return launch_long<D, 8, 1>(p, st);
 }
 

@@ -185,7 +185,8 @@ def test_many_short_caches():
     (16, 4, 128, 8, [1, 2500], 32), (6, 2, 64, 11, [100, 0, 1000, 31], 64), (16, 4, 128, 16, [3000, 17], 64),
     (8, 2, 128, 9, [257, 2000, 3, 64], 64), (8, 8, 64, 64, [1300], 64), (8, 2, 64, 17, [600, 1, 64, 128], 128), (12, 4, 128, 40, [900, 64, 0], 128),
     (4, 2, 128, 64, [63, 1999, 0, 20], 128), (28, 4, 64, 10, [1, 300], 128), (8, 2, 128, 64, [1000, 0, 63, 65], 256),
-    (16, 4, 64, 33, [2500, 0], 256), (28, 4, 64, 50, [300, 1], 128), (32, 4, 128, 64, [700, 40], 256), (28, 4, 128, 23, [1, 3000], 256),
+    (16, 4, 64, 33, [2500, 0], 192), (16, 4, 128, 48, [3000, 64, 0], 192), (12, 4, 64, 64, [63, 1300], 192), (24, 8, 128, 43, [1, 2000], 192),
+    (28, 4, 64, 50, [300, 1], 128), (32, 4, 128, 64, [700, 40], 256), (28, 4, 128, 23, [1, 3000], 256),
 ])
 def test_every_form_shared_out(hq, hkv, d, T, lens, block):
     """Short caches in a large capacity, which is what the host chooses by: each form, with lengths where its tiles and shares end.  The
@@ -202,7 +203,7 @@ def test_every_form_shared_out(hq, hkv, d, T, lens, block):
 
 @pytest.mark.parametrize("hq,hkv,d,T,n,top", [
     (8, 8, 64, 16, 60, 300), (8, 2, 128, 8, 250, 70), (16, 8, 64, 30, 80, 90), (8, 2, 128, 28, 200, 30), (16, 4, 64, 60, 130, 64),
-    (16, 4, 128, 60, 110, 100), (21, 3, 64, 64, 100, 70),
+    (16, 4, 128, 60, 110, 100), (21, 3, 64, 64, 100, 70), (12, 4, 128, 50, 120, 90), (16, 4, 64, 48, 130, 130),
 ])
 def test_every_form_whole(hq, hkv, d, T, n, top):
     """Many short caches: one workgroup to each sequence, KV head and row block, in every form."""
