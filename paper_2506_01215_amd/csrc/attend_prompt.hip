@@ -4,7 +4,8 @@
 //                            of the group) over all keys that the block sees; KG groups of its waves divide the key tiles
 //   prompt_attend_short<D,NB,NW>   blocks of 16 NB rows whose NW waves divide the keys (attend_seq.h)
 //
-//   prompt_attend_shared<D,NB,NW>  the same blocks, their keys shared out over the chip: few rows behind many keys (prompt_share.h)
+//   prompt_attend_shared<D,NB,NW>, prompt_attend_rows_shared<D,NW,KG>   blocks of 16 NB and of 32 NW rows, their keys shared out over the chip: few
+//                            rows behind many keys (prompt_share.h)
 //
 // Large blocks read K and V less often, small ones and divided keys fill the chip with few rows and make the longest
 // block's chain of tiles shorter; prompt_plan.h says which when.
@@ -59,6 +60,17 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_shared(PromptParams 
     });
 }
 
+template <int D, int NW, int KG>
+__global__ __launch_bounds__(NW * KG * 64, 2) void prompt_attend_rows_shared(PromptParams p)
+{
+    using S = RowsShape<D, NW, KG>;
+    extern __shared__ __attribute__((aligned(16))) u16 lds[];
+    prompt_walk<u16, S::ROWS, S::BN>(p, [&](const SeqRows &r, const SeqKeys &k, int t0, int t1, long slot) {
+        rows_segment<D, NW, KG, false>(r, k, false, p.scale, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
+                                       slot < 0 ? nullptr : p.part_ml + (size_t)slot * p.part_rows, lds);
+    });
+}
+
 namespace {
 
 template <int D, int NW, int KG>
@@ -93,11 +105,24 @@ hipError_t launch_shared(const PromptParams &p, hipStream_t st)
     return hipGetLastError();
 }
 
+template <int D, int NW, int KG>
+hipError_t launch_rows_shared(const PromptParams &p, hipStream_t st)
+{
+    using S = RowsShape<D, NW, KG>;
+    const hipError_t e = raise_lds<prompt_attend_rows_shared<D, NW, KG>>(S::lds_bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((prompt_attend_rows_shared<D, NW, KG>), dim3(p.shares), dim3(NW * KG * 64), S::lds_bytes, st, p);
+    prompt_merge_launch<D, S::ROWS, S::BN, true>(p, st);
+    return hipGetLastError();
+}
+
 template <int D>
 hipError_t launch(const PromptParams &p, hipStream_t st)
 {
     if (p.shares) {
         constexpr int NW = D == 64 ? 4 : 8;
+        if (p.block == 64) return launch_rows_shared<D, 2, 2>(p, st);
+        if (p.block == 128) return launch_rows_shared<D, 4, 1>(p, st);
         return p.block == 16 ? launch_shared<D, 1, NW>(p, st) : launch_shared<D, 2, NW>(p, st);
     }
     const PromptForm &f = prompt_forms(D)[prompt_choose(D, p.G, p.Hkv, p.n_seq, p.n_q, p.n_k, p.units)];
@@ -121,7 +146,7 @@ void prompt_plan_bf16(PromptParams &p)
     const int rows = p.n_q * p.G;
     p.part_rows = rows < p.block ? rows : p.block;
     p.least = f.least / f.form.keys;
-    p.shares = (p.D == 64 ? 2 : 1) * p.units;
+    p.shares = f.workgroups * p.units;
     if (p.shares > kTreeMaxShares) p.shares = kTreeMaxShares;
 }
 

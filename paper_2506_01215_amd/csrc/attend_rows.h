@@ -193,20 +193,20 @@ __device__ __forceinline__ void rows_tile(RowsWave<D> &w, const u16 *__restrict_
     }
 }
 
-// Key tiles [t0, t1) of the sequence for the block of ROWS rows from r.row0 on, as seq_segment.  Prompts begin at
-// tile 0; by_head: how the rows are dealt to the waves.
+// Key tiles [t0, t1) of the sequence for the block of ROWS rows from r.row0 on, as seq_segment.  by_head: how the rows are dealt to
+// the waves.
 template <int D, int NW, int KG, bool TREE, bool THIN = false>
 __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool by_head, float scale, int t0, int t1, float *po,
                                              float2 *pml, u16 *lds)
 {
     using S = RowsShape<D, NW, KG, THIN>;
     constexpr int BN = S::BN, TILE = S::TILE, KS = S::KS, DB = S::DB, C8 = S::C8;
-    if (TREE) {                                          // keys are counted from the range's first one
-        k.k = (const u16 *)k.k + (size_t)t0 * BN * k.k_rs;
-        k.v = (const u16 *)k.v + (size_t)t0 * BN * k.v_rs;
-        k.n -= t0 * BN;
-        k.open -= t0 * BN;
-    }
+    // keys are counted from the range's first one
+    k.k = (const u16 *)k.k + (size_t)t0 * BN * k.k_rs;
+    k.v = (const u16 *)k.v + (size_t)t0 * BN * k.v_rs;
+    k.n -= t0 * BN;
+    k.open -= t0 * BN;
+    k.shift -= t0 * BN;
 
     const int lane = threadIdx.x & 63, wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int ln = lane & 15, lg = lane >> 4, kg = wave_all / NW, wave = wave_all % NW;

@@ -68,34 +68,48 @@ inline int prompt_choose(int head_dim, int G, int Hkv, int n_seq, int n_q, int n
     return best;
 }
 
-// Blocks whose keys are shared out (prompt_share.h): no block takes longer than its share, but there is a second launch.  130 batches of 1 to 9000
-// rows, 1 to 50 sequences behind up to 16000 keys each, whole and shared out: with these constants (2.2 times the rates of the
-// whole forms) the choice takes 0.5 % more time in the mean than the better one, at worst 17 %, and 0.93 (head_dim 64) and 0.80 (128) of the
-// whole forms' time.  Three rows behind 16000 keys, 4/1 heads of 128 80.9 -> 18.5 us, two sequences of three rows, 64/8 heads 84 -> 33; eight of
-// together 364, 56/8 heads 261 whole, 734 shared out.
+// Rows of a block where the keys of `items` items of `rows` rows (rows of a sequence times heads of a group) are shared out over the chip: the smallest
+// of up to 64 that does not make a compute unit go through more than so many keys, with 400 for the time it takes to begin a block; else
+// 128.  Blocks that take all rows read K and V least often, and are right where the chip is busy; where it is not, smaller ones are done
+// sooner, being more.  (Fitted on drafted trees, tree.hip.)
+inline int shared_rows(int head_dim, double rows, double keys, double items, int units)
+{
+    const double each = (keys + 400.0) * items / units;
+    const bool narrow = head_dim == 64;
+    auto few = [&](int R, double limit) { return rows <= R || std::ceil(rows / R) * each <= limit; };
+    return few(16, narrow ? 1600.0 : 1300.0) ? 16 : few(32, narrow ? 1800.0 : 600.0) ? 32 : few(64, narrow ? 2000.0 : 1000.0) ? 64 : 128;
+}
+
+// Blocks whose keys are shared out (prompt_share.h): no block takes longer than its share, but all go through all of their sequence's
+// tiles, and there is a second launch.
 struct PromptShared {
     PromptForm form;
     int least;               // keys that a share has at least
+    int workgroups;          // shares of a compute unit
 };
 
 // Rows of such a block where sharing out is faster than the best form, else 0; `shared`: how.
+// Measured: 150 batches of 1 to 3000 rows, 1 to 50 sequences behind up to 16000 keys each, 0.86 of the whole forms' time in the mean; three rows behind
+// 16000 keys, 4/1 heads of 128 80.9 -> 18.5 us, four sequences of 16 rows behind 8000, 32/8 heads 52 -> 35; but eight of together 364 rows behind
+// 16000, 56/8 heads 261 whole, 734 in blocks of 16 shared out: the rates here are 1.2 to 2.8 times those of the whole forms.
 inline int prompt_share_rows(int head_dim, int G, int Hkv, int n_seq, int n_q, int n_k, int units, PromptShared &shared)
 {
-    static const PromptShared forms64[2] = {{{16, 4, 32, 0.73, 0.0, 12.0, 2.3}, 256}, {{32, 4, 32, 0.84, 0.0, 12.0, 3.45}, 128}};
-    static const PromptShared forms128[2] = {{{16, 8, 32, 3.2, 0.0, 12.0, 9.3}, 128}, {{32, 8, 32, 4.1, 0.0, 12.0, 12.7}, 128}};
-    if ((double)n_k / n_seq * (head_dim == 64 ? 0.788 : 1.62) < 256.0 * 2.5) return 0;      // a block's chain takes less than the second launch
+    static const PromptShared forms64[4] = {{{16, 4, 32, 0.53, 0.0, 12.0, 1.66}, 256, 2}, {{32, 4, 32, 0.84, 0.0, 12.0, 3.45}, 128, 2},
+                                            {{64, 2, 64, 1.30, 0.0, 12.0, 5.2}, 128, 1}, {{128, 1, 64, 1.30, 0.0, 12.0, 5.7}, 128, 2}};
+    static const PromptShared forms128[4] = {{{16, 8, 32, 1.76, 0.0, 12.0, 5.1}, 128, 1}, {{32, 8, 32, 4.1, 0.0, 12.0, 12.7}, 128, 1},
+                                             {{64, 2, 64, 3.2, 0.0, 12.0, 11.2}, 128, 1}, {{128, 1, 64, 2.5, 0.0, 12.0, 12.0}, 128, 2}};
+    const double keys = (double)n_k / n_seq, rows = std::ceil((n_seq > 1 ? 1.3 : 1.0) * n_q / n_seq) * G, items = (double)n_seq * Hkv;
+    if (keys * (head_dim == 64 ? 0.788 : 1.62) < 256.0 * 2.5) return 0;              // a block's chain takes less than the second launch
     // sequences one to a lane, places counted in 32 bits, also where broken boundaries give all rows to every one of them
     if (n_seq > 64 || ((double)n_q * G / 16.0 + n_seq) * Hkv * ((double)n_k / 32.0 + 16.0) >= 33554432.0) return 0;
+    const int R = shared_rows(head_dim, rows, keys, items, units);
+    shared = (head_dim == 64 ? forms64 : forms128)[R == 16 ? 0 : R == 32 ? 1 : R == 64 ? 2 : 3];
+    const PromptForm &f = shared.form;
+    const double t = f.start + items * std::ceil(rows / R) / units * (keys / (f.keys * f.groups) * f.rate + f.block);
     const PromptForm *whole = prompt_forms(head_dim);
-    double least = prompt_estimate(whole[0], G, Hkv, n_seq, n_q, n_k, units);
-    for (int i = 1; i < kPromptForms; ++i) least = std::min(least, prompt_estimate(whole[i], G, Hkv, n_seq, n_q, n_k, units));
-    int rows = 0;
-    for (int i = 0; i < 2; ++i) {
-        const PromptShared &f = head_dim == 64 ? forms64[i] : forms128[i];
-        const double t = prompt_estimate(f.form, G, Hkv, n_seq, n_q, n_k, units);
-        if (t < least) { least = t; shared = f; rows = f.form.rows; }
-    }
-    return rows;
+    for (int i = 0; i < kPromptForms; ++i)
+        if (prompt_estimate(whole[i], G, Hkv, n_seq, n_q, n_k, units) <= t) return 0;
+    return R;
 }
 
 }  // namespace reform

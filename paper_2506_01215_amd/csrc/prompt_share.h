@@ -24,7 +24,8 @@ struct PromptShares {
         incl = wave_incl_scan(own(p));
         total = __builtin_amdgcn_readlane(incl, 63);
         const int items = __builtin_amdgcn_readlane(wave_incl_scan(seq.blocks), 63) * p.Hkv;
-        shares = max(1, min(p.shares, max(items, (int)((unsigned)total / (unsigned)p.least))));
+        const int most = (int)((unsigned)total / (unsigned)p.least);                 // as in TreeList
+        shares = max(1, min(p.shares, max(items, max(min(most, p.units), most >> 1))));
         each = (int)((unsigned)total / (unsigned)shares);
         more = total - each * shares;
     }

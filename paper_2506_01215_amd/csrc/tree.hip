@@ -14,6 +14,7 @@
 // head_dim 64 0.92).  128 rows: two groups take as long as two workgroups (25 batches, 1.00).  192 rows: a wave of 32 and one of 16 to each SIMD (48
 // nodes over 16640 rows, 32/8 of 128 32.1 -> 30.1 us against a block of 256; 32 caches of up to 4492 rows, 48 nodes, 32/8 of 64 81 -> 74).
 #include "attend_rows.h"
+#include "prompt_plan.h"
 #include "tree_list.h"
 
 namespace reform {
@@ -42,26 +43,22 @@ __global__ __launch_bounds__(NW * KG * 64, 2) void tree_attend_rows(TreeParams p
 
 namespace {
 
-// Rows of a block.  Blocks that take all rows read K and V least often, and are right where the chip is busy; where it is not, smaller blocks
-// are done sooner, being more.  What each unit would have to go through in blocks of R rows decides, in keys, with 400 for the time it
-// takes to begin a block.  Fitted to 230 batches of 17 to 512 rows over 300 to 12000 keys, 1 to 64 sequences, in every form: the choice takes
+// Rows of a block (shared_rows).  Fitted to 230 batches of 17 to 512 rows over 300 to 12000 keys, 1 to 64 sequences, in every form: the choice takes
 // 1.3 % more time in the mean than the best form, at worst 1.34 times it; the smallest block that takes all rows 23 %.
 int tree_rows(const TreeParams &p, int compute_units)
 {
     const int rows = p.T * p.G;
-    const double keys = ((double)p.max_len + p.T + 400) * p.n_seq * p.Hkv / compute_units;
     const bool narrow = p.D == 64;
-    auto few = [&](int R, int limit) { return rows <= R || (rows + R - 1) / R * keys <= limit; };
-    if (few(16, narrow ? 1600 : 1300)) return 16;
-    if (few(32, narrow ? 1800 : 600)) return 32;
-    if (few(64, narrow ? 2000 : 1000)) return 64;
+    const double keys = (double)p.max_len + p.T, items = (double)p.n_seq * p.Hkv;
+    const int R = shared_rows(p.D, rows, keys, items, compute_units);
+    if (R < 128) return R;
     if (rows <= 128) return 128;
     if (rows <= 192) return 192;
     const int by_128 = (rows + 127) / 128, by_192 = (rows + 191) / 192;
     if (by_128 % 2 == 0) return 256;                     // none is half empty
     // As few rows empty by 192, and K and V read less often: 371 rows of 32 x 4 caches of up to 1328 keys, 128 wide, 37.3 us against 41.3; but 64
     // wide 74.6 against 73.0 (280 of 64 x 4 of up to 2351), and where the chip is not busy 35.2 against 28.0 (304 of 32 x 2 of up to 1035).
-    return !narrow && by_192 * 192 <= by_128 * 128 && by_192 * keys > 1500 ? 192 : 128;
+    return !narrow && by_192 * 192 <= by_128 * 128 && by_192 * (keys + 400) * items / compute_units > 1500 ? 192 : 128;
 }
 
 // Keys of a tile.

@@ -286,3 +286,19 @@ def test_shared_out_calls_replay_from_a_graph():
         got = out.clone(), lse.clone()
         eager = binding.reform_prompt_attend(q, k, v, cu_q, 0.1, cu_k=cu_k, workspace=ws)
         assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1])
+
+
+@pytest.mark.parametrize("hq,hkv,d,q_lens,k_lens,block", [
+    (8, 2, 128, [3, 40], [9000, 70], 16), (32, 8, 128, [6, 5, 7, 6], [5000, 4000, 6000, 5200], 32), (32, 8, 128, [16], [11000], 64),
+    (32, 8, 128, [30, 3, 0, 31], [8000, 5, 9000, 15000], 128), (32, 8, 64, [6, 5, 7, 6], [6500, 64, 13000, 6500], 32),
+    (32, 8, 64, [12, 10, 14, 12], [7000, 7000, 7000, 7031], 64), (16, 4, 64, [30, 20], [32001, 33000], 128),
+])
+def test_every_shared_form(hq, hkv, d, q_lens, k_lens, block):
+    """Blocks of each size, by the workspace's; lengths that differ, tiles that end inside a share, rows that see nothing."""
+    q, kv = torch.empty((hq, sum(q_lens), d), dtype=BF, device="meta"), torch.empty((hkv, sum(k_lens), d), dtype=BF, device="meta")
+    units = torch.cuda.get_device_properties(0).multi_processor_count if torch.cuda.is_available() else 256
+    shares = min((2 if block == 128 or (d == 64 and block <= 32) else 1) * units, 512)
+    need = binding.prompt_workspace_bytes(binding.prompt_desc(q, kv, kv, q, torch.empty(len(q_lens) + 1), 0.1))
+    assert need == 2 * shares * min(block, sum(q_lens) * hq // hkv) * (4 * d + 8)
+    run_case(hq, hkv, d, q_lens, k_lens, BF, seed=block + d, spare=2)
+    run_case(hq, hkv, d, q_lens, k_lens, BF, seed=block + d + 1, layout="tokens", sharp=9.0)
