@@ -502,8 +502,8 @@ reform_status reform_prompt_attend(const reform_prompt_desc *desc, const void *q
  *     node_count [n_seq] int32 in device memory or NULL (all have n_nodes); values outside [0, n_nodes] are
  *                moved into it.  Rows of out and lse from node_count[b] on keep what they held.
  *     lse        [n_seq][n_q_heads][n_nodes] fp32, may be NULL
- * Supported: n_nodes in [1, 64]; types and head_dim as reform_prompt_attend, out and lse as there; max_cache_len + n_nodes <=
- * capacity; n_seq * n_q_heads * n_nodes at most 2^22; with B = ceil(n_nodes * G / 16), n_seq * n_kv_heads * B *
+ * Supported: n_nodes in [1, 64]; types and head_dim as reform_prompt_attend, out and lse as there; max_cache_len + n_nodes at most
+ * capacity and 2^31 - 512; n_seq * n_q_heads * n_nodes at most 2^22; with B = ceil(n_nodes * G / 16), n_seq * n_kv_heads * B *
  * ((max_cache_len + n_nodes) / 16 + 64) below 2^31.  n_seq = 0 does nothing.
  * The workspace takes partial results where long caches are shared out over workgroups.  Without it, or
  * with less than the query asks for, the call returns REFORM_ERR_WORKSPACE.  Results depend on the batch

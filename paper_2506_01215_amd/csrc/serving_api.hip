@@ -64,6 +64,9 @@ reform_status check_heads(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t dim,
 
 constexpr double kMaxGroups = 8388607.0;                 // workgroups of 512 threads in a grid
 constexpr int64_t kMaxRowStride = 1 << 24;               // offsets inside a tile of 64 rows stay within 32 bits
+// Keys of a sequence, and the row behind the tiles that a loop asks about next (two groups of waves, 64 keys a tile: up to 320 rows
+// further), are counted in 32-bit signed integers.
+constexpr int64_t kMaxTreeKeys = (1ll << 31) - 512;
 
 reform_status check_prompt(const reform_prompt_desc *d)
 {
@@ -136,7 +139,7 @@ reform_status check_tree(const reform_tree_desc *d)
     for (int64_t s : strides)
         if (s < 0 || (s * es) % 16) return REFORM_ERR_INVALID_ARG;
     if (rc != REFORM_OK) return rc;
-    if (d->n_nodes > 64) return REFORM_ERR_UNSUPPORTED;
+    if (d->n_nodes > 64 || (int64_t)d->max_cache_len + d->n_nodes > kMaxTreeKeys) return REFORM_ERR_UNSUPPORTED;
     // the list of all key tiles is counted in 32 bits (tree_list.h): 16 rows and 16 keys are the smallest blocks and tiles
     if ((double)d->n_seq * d->n_q_heads * d->n_nodes > 4194304.0) return REFORM_ERR_UNSUPPORTED;
     const double blocks = std::ceil((double)d->n_nodes * (d->n_q_heads / d->n_kv_heads) / 16.0);
