@@ -123,7 +123,7 @@ template <int D, int R, int TK, bool BF16>
 inline void prompt_merge_launch(const PromptParams &p, hipStream_t st)
 {
     int rows = 1;
-    while (2 * rows <= 1024 / D && rows < p.part_rows && p.shares * ((p.part_rows + rows - 1) / rows) > 768) rows *= 2;   // as tree_merge_launch
+    while (2 * rows <= 1024 / D && rows < p.part_rows && p.shares * ((p.part_rows + rows - 1) / rows) > 3 * p.units) rows *= 2;   // as tree_merge_launch
     hipLaunchKernelGGL((prompt_merge<D, R, TK, BF16>), dim3(p.shares * ((p.part_rows + rows - 1) / rows)), dim3(256), 0, st, p, rows);
 }
 

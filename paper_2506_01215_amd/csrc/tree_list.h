@@ -210,6 +210,7 @@ __device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
     }
 }
 
+// Two for each of this chip's 256 compute units: the most that any form keeps there at once.
 constexpr int kTreeMaxShares = 512;
 
 // Row r0 + r of an item's n pieces, piece x in slot slot(x), put together by a workgroup of 256 threads that has `rows` rows (a power of
@@ -332,14 +333,15 @@ __global__ __launch_bounds__(256) void tree_merge(TreeParams p, int rows, int by
 // 128, 30 nodes, caches of up to 2000 rows, us, by share / by item: 512 caches 556 / 690, 16 caches 44 / 36; 8 nodes,
 // 8/2 heads, 8192 caches of 1000 rows 1715 / 3225).
 // One row to a workgroup where that makes no more than three workgroups a compute unit, else two, four or more (16 ragged caches, 17 nodes, 24/8 heads
-// of 64, whole call: up to eight 28.1 us, three 25.7, one 25.6; one cache, 48 nodes, 32/8 of 128: 32.7, 32.4, 35.3).
+// of 64, whole call, two inputs in turn: up to eight 28.1 us, three 25.7, one 25.6, on another machine 28.4 and 25.3; one cache, 48 nodes, 32/8 of
+// 128: 32.7, 32.4, 35.3.  With more inputs in turn, whose caches come from memory, the first takes 28.9).
 template <int D, int R, int TK, bool BF16>
 inline void tree_merge_launch(const TreeParams &p, hipStream_t st)
 {
     const bool by_share = (long)p.n_seq * p.Hkv > p.shares;
     const long blocks = (by_share ? p.shares : (long)p.n_seq * p.Hkv) * p.row_blocks;
     int rows = 1;
-    while (2 * rows <= 1024 / D && rows < p.part_rows && blocks * ((p.part_rows + rows - 1) / rows) > 768) rows *= 2;
+    while (2 * rows <= 1024 / D && rows < p.part_rows && blocks * ((p.part_rows + rows - 1) / rows) > 3l * p.units) rows *= 2;
     const unsigned chunks = (p.part_rows + rows - 1) / rows;
     hipLaunchKernelGGL((tree_merge<D, R, TK, BF16>), dim3((unsigned)blocks * chunks), dim3(256), 0, st, p, rows, (int)by_share);
 }
