@@ -4,8 +4,12 @@
 // It computes S^T = K Q^T with v_mfma_f32_16x16x32_bf16 (operand layouts in attend_bf16.hip), so that a
 // lane owns one query column of each of its wave's two 16-row blocks, its softmax statistics are scalars, and the
 // probabilities are the B operand of O^T = V^T P^T as they stand.  K and V tiles of 64 keys go from memory
-// straight into LDS (global_load_lds, 16 bytes a lane), one tile ahead of the one that is computed
-// (two ahead: no faster, for prompts and for drafted tokens over caches in memory).
+// straight into LDS (global_load_lds, 16 bytes a lane), one tile ahead of the one that is computed (two ahead: no faster where
+// it was tried, with one group of eight waves: 52 batches of prompts and of 20 to 64 nodes, geometric mean 69.7 us against
+// 69.4; not tried with two groups of two waves).
+//
+// Addresses, strides and the list's state take more than the scalar registers there are: the compiler keeps 78 to 148 of them in
+// lanes of vector registers in the shared-out forms (8 to 32 in prompt_attend) and reads some back in every tile.
 //
 // LDS: the 64 lanes of such a load land in 1024 adjacent bytes, so rows cannot be padded one by one.  Instead a load
 // takes rows that no read takes together: rows c, c + 16, c + 32, c + 48 at head_dim 128 (at 64 rows c and c + 8 of

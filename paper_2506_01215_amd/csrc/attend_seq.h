@@ -3,8 +3,12 @@
 //
 // Rows are counted over a sequence's query rows and the G heads of a KV group together (row r is query row
 // r / G of head r % G), so K and V are read once for all of them.  Softmax in one pass with a running
-// reference maximum and sum; logits, sums and outputs in fp32, the probabilities of P.V rounded to bf16 in
-// the bf16 form (the matrix instruction takes nothing wider; 2^-9 of a probability, as in attend_bf16.hip).
+// reference maximum and sum; logits, sums and outputs in fp32.  In the bf16 form the probabilities of P.V are
+// rounded to bf16, by up to 2^-8 of each, while their sum adds them unrounded: the matrix instruction takes bf16 on both
+// sides, and a second product for what the rounding leaves would double P.V where the matrix pipe is the bound (prompts, wide
+// trees).  The forms bound by memory could hide it; they do without it too, so that all forms compute alike, and as
+// reform_chunk_attend_score does.  Outputs are off by 0.0017 to 0.0024 of their norm (up to 16640 keys), 0.0017 of it by
+// their own rounding.
 #pragma once
 #include "attend_tile.h"
 

@@ -8,7 +8,7 @@
 // 4 (l / 16) + e, which is the B operand of O^T = V^T P^T for the contraction over those four keys, and V's
 // operand is element l % 16 of row 4 (l / 16) + e: both straight from global memory, no LDS.
 //
-// Bound: the fp32 matrix pipe (0.15 PFLOP/s, of which it reaches 0.4 to 0.47: 2048 rows, 32/8 heads of 128, 550 us; 4096, 32/8 of 64, 969) and,
+// Bound: the fp32 matrix pipe (0.15 PFLOP/s, of which it reaches 0.32 to 0.48: 2048 rows, 32/8 heads of 128, 534 us; 4096, 32/8 of 64, 926; 8 x 1000, 32/8 of 128, 1341) and,
 // at the sizes of checks, latency (three prompts of up to 301 rows, 4 heads of 64: 11 us).  32 rows to a workgroup, so that K and V are read half
 // as often: the same time for large batches, twice as long for small ones (60 batches, 1.27).
 #include "attend_seq.h"
@@ -225,6 +225,7 @@ hipError_t launch_tree(const TreeParams &p, hipStream_t st)
 // A step is eight tiles of 16 keys by the waves of a workgroup, some 0.03 us for each element of a row (3.7 us at 128, 1.9 at 64), whether the chip
 // is full or not.  What sharing out saves is the longest block's chain, for some 8 us; but where a sequence's blocks are then at different keys, each
 // brings them from memory (ten rows, 12/4 heads of 96 behind 16000 keys 430 -> 48 us; 282 rows, 12/4 of 256 behind 4 x 3000 221 -> 396).
+// 80 batches of 1 to 50 sequences behind up to 16000 keys each: 0.62 of the time without sharing, at worst 1.26 (three rows behind 200, 8/4 of 256).
 void prompt_plan_f32(PromptParams &p)
 {
     const double step = 0.03 * (p.D <= 32 ? 32 : p.D <= 64 ? 64 : p.D <= 128 ? 128 : 256), keys = (double)p.n_k / p.n_seq;
@@ -251,7 +252,8 @@ hipError_t prompt_attend_f32_launch(const PromptParams &p, hipStream_t st)
 size_t tree_part_dim(bool bf16, int D) { return bf16 ? D : D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
 // Fitted as in tree.hip, to 90 batches of 1 to 40 rows over 300 to 3000 keys in heads of 32 to 256: shares of a tile for each wave and more take
-// 0.87 of the time that two tiles for each take, whole items of up to 1024 keys up to 4.8 times as much where heads are wide.
+// 0.87 of the time that two tiles for each take, whole items of up to 1024 keys up to 4.8 times as much where heads are wide.  70 other batches of 1 to 64
+// rows: 0.61 of all whole, at worst 1.21 times (37 rows of 8 x 4 caches of up to 432 keys, 128 wide, 21.7 us whole, 26.2).
 void tree_plan_f32(TreeParams &p, int compute_units)
 {
     const int whole = p.D <= 32 ? 1200 : p.D <= 64 ? 850 : p.D <= 128 ? 350 : 200;

@@ -7,7 +7,8 @@
 //
 // The constants were fitted to measurements of 370 batches (1 to 32000 rows, 1 to 50 sequences, 1 to 8 heads a group, with
 // and without keys in front) in eight forms: error 6 to 15 % (root mean square), and the one of these four that is chosen takes 2 % more time in
-// the mean than the best of the eight, at worst 47 %.  (256 rows at head_dim 128, 64 by two groups, 32 by eight and 16 by four add nothing; without the last two forms
+// the mean than the best of the eight, at worst 47 %.  300 other batches, of up to 18000 rows, against the best of the four: 2.7 % in the mean, at worst
+// 90 % (50 sequences of together 511 rows behind 3000 keys each, 28/4 heads of 128: 118 us, in blocks of 128 62).  (256 rows at head_dim 128, 64 by two groups, 32 by eight and 16 by four add nothing; without the last two forms
 // it is 4 % at head_dim 64 and 16 % at 128.)  Measured, us, blocks of 256 / 128 / 128 with two groups (head_dim 128) / 32 / 16:
 //   head_dim 64: 32 prompts of together 14586 behind 500 keys each, 8/4 heads 60 / 46 / - / 71 / -, four of 2445, 3/1 17.5 / 14.3 / - / 9.3 / 11.5, one
 //   row behind 3000 keys, 2/1 39 / 40 / - / 16 / 11.5, one of 32768, 32/8 4658 / 4799
@@ -89,8 +90,9 @@ struct PromptShared {
 };
 
 // Rows of such a block where sharing out is faster than the best form, else 0; `shared`: how.
-// Measured: 150 batches of 1 to 3000 rows, 1 to 50 sequences behind up to 16000 keys each, 0.86 of the whole forms' time in the mean; three rows behind
-// 16000 keys, 4/1 heads of 128 80.9 -> 18.5 us, four sequences of 16 rows behind 8000, 32/8 heads 52 -> 35; but eight of together 364 rows behind
+// Measured: 150 batches of 2 to 9000 rows, 1 to 50 sequences behind 500 to 16000 keys each, 0.89 of the whole forms' time in the mean, at worst 1.07 times
+// it; the best of whole and all blocks 0.84, since the rule keeps some whole that blocks of 128 rows would finish sooner (16 sequences of together 435
+// rows behind 16000 keys each, 8/1 heads of 128: 113 us, 67).  Three rows behind 16000 keys, 4/1 heads of 128 80.9 -> 18.5 us, four sequences of 16 rows behind 8000, 32/8 heads 52 -> 35; but eight of together 364 rows behind
 // 16000, 56/8 heads 261 whole, 734 in blocks of 16 shared out: the rates here are 1.2 to 2.8 times those of the whole forms.
 inline int prompt_share_rows(int head_dim, int G, int Hkv, int n_seq, int n_q, int n_k, int units, PromptShared &shared)
 {

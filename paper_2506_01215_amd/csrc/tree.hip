@@ -44,7 +44,8 @@ __global__ __launch_bounds__(NW * KG * 64, 2) void tree_attend_rows(TreeParams p
 namespace {
 
 // Rows of a block (shared_rows).  Fitted to 230 batches of 17 to 512 rows over 300 to 12000 keys, 1 to 64 sequences, in every form: the choice takes
-// 1.3 % more time in the mean than the best form, at worst 1.34 times it; the smallest block that takes all rows 23 %.
+// 1.3 % more time in the mean than the best form, at worst 1.34 times it; the smallest block that takes all rows 23 %.  146 other batches, with the form
+// of 192 rows: 2.3 %, at worst 1.47 times (504 rows of 8 caches of up to 3682 keys, 128 wide, 14.8 us in blocks of 16, 21.8).
 int tree_rows(const TreeParams &p, int compute_units)
 {
     const int rows = p.T * p.G;
@@ -110,7 +111,8 @@ void tree_plan_bf16(TreeParams &p, int compute_units)
     // Keys that one workgroup takes alone before sharing them out is faster, and that a share has at least: fitted to 360 batches of 1 to
     // 512 rows, 1 to 64 sequences of 300 to 8000 keys, each whole and shared out with 128 and 256 keys or more.  240 other ones of 300 to 25000 keys
     // against 1024 and 256 for all, means by rows: up to 16 0.96, 32 0.95, 64 0.90 (with the two groups), 128 0.97, 256 0.97, 512 0.98; at
-    // worst 1.12 (77 rows of 4 x 8 caches of up to 990 keys 14.8 -> 16.3 us).
+    // worst 1.12 (77 rows of 4 x 8 caches of up to 990 keys 14.8 -> 16.3 us).  150 others of 1 to 512 rows over 300 to 8000 keys: 0.88 of all whole, 0.86 of all
+    // shared out, at worst 1.21 times the better (224 rows of 32 x 8 caches of up to 2471 keys, 128 wide, 76.7 us whole, 93.1).
     const int whole = R == 16 ? (narrow ? 2000 : 1600) : R == 32 ? (narrow ? 2000 : 1300) : R == 64 ? (narrow ? 1600 : 1000) :
                       R == 128 ? (narrow ? 1000 : 700) : narrow ? 800 : 600;
     const int least = (R == 16 && narrow ? 256 : 128) / keys;
