@@ -17,9 +17,9 @@
  *                               selected, neighbourhood kept contiguous (Sec. 3.3, App. C.6).
  *
  * Around them stand the calls that a model's serving needs next to these: rotary positions
- * (reform_rotary_embed), whole prompts packed into one batch (reform_prompt_attend), and generation
- * from a batch of caches, by single tokens or by trees of drafted ones (reform_tree_attend,
- * reform_tree_accept).
+ * (reform_rotary_embed), whole prompts packed into one batch (reform_prompt_attend, with a sliding window
+ * reform_window_attend), and generation from a batch of caches, by single tokens or by trees of drafted ones
+ * (reform_tree_attend, reform_tree_accept), or from caches in pages (reform_paged_attend, reform_paged_evict).
  *
  * Conventions common to all calls
  *   - Every data pointer is a DEVICE pointer (HIP global memory) owned by the caller.  The
@@ -558,6 +558,124 @@ reform_status reform_tree_accept(const reform_accept_desc *desc, const int32_t *
                                  const int32_t *target, const int32_t *cache_len, const int32_t *node_count,
                                  void *k, void *v, int32_t *path, int32_t *accepted, int32_t *next_token,
                                  int32_t *new_len, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------- */
+/* reform_window_attend -- packed prompts whose rows see a sliding window and a few first keys
+ *
+ * As reform_prompt_attend, with fewer keys seen: row i of a sequence of nq query and nk key rows stands at
+ * key t = nk - nq + i and sees
+ *     j in [0, t] with j > t - window or j < n_sink
+ * A window of nk keys or more is reform_prompt_attend.  A row that sees no key (t < 0) gets out = 0 and lse = -inf.
+ *     q, out, k, v, cu_q, cu_k, lse   as in reform_prompt_attend: layouts, lengths read on the device, boundaries that are out of
+ *              place, rows of no sequence, arithmetic.  Keys and values that are not finite make rows of their sequence NaN that
+ *              see them, and may make those NaN whose block of rows goes through their tile of 64 keys
+ * Supported: as reform_prompt_attend; window >= 1, n_sink >= 0.
+ * The workspace is that of reform_prompt_attend: without it, or with less than the query asks for, REFORM_ERR_WORKSPACE.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t  dtype;
+    int32_t  n_q_heads, n_kv_heads, head_dim;
+    int32_t  n_seq, n_q_rows, n_k_rows;
+    float    scale;                          /* > 0, finite                                    */
+    int32_t  window, n_sink;
+    int32_t  reserved;                       /* 0                                              */
+    int64_t  q_head_stride, q_row_stride, k_head_stride, k_row_stride;   /* elements, multiples */
+    int64_t  v_head_stride, v_row_stride, o_head_stride, o_row_stride;   /* of 16 bytes         */
+} reform_window_desc;
+
+size_t reform_window_attend_workspace(const reform_window_desc *desc);
+
+reform_status reform_window_attend(const reform_window_desc *desc, const void *q, const void *k, const void *v,
+                                   const int32_t *cu_q, const int32_t *cu_k, void *out, float *lse,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------- */
+/* reform_paged_attend -- one new token of each of a batch of sequences over caches in pages
+ *
+ * Sequence b has L = cache_len[b] keys, the new token's own (the last one) among them.  Key j lies in row j % page_len of page
+ * page_table[b][j / page_len] of a pool that all sequences share (reform_rotary_embed writes there: slot = page * page_len +
+ * row).  Seen are
+ *     j in [0, L) with window = 0, or j >= L - window, or j < n_sink
+ * and of these the ones whose page number lies in [0, n_pages): a page that was given back, or was never there, is -1 in the
+ * table, and nothing of it is read.
+ *     s_hj  = scale * <q_bh, k_j>,   out_bh = sum_j softmax_j(s_hj) v_j,   lse_bh = log sum_j exp(s_hj)
+ *     score_bgj (+)= sum_{h in group g} softmax_j(s_hj): the attention that the key received (the eviction score of
+ *              reform_paged_evict).  accumulate = 0: entries [0, L) are written, 0 for keys that are not seen.  accumulate = 1: keys
+ *              that are seen get it added, the others keep what they have; but entry L - 1, the new token's, is written
+ * A sequence that sees no key (L = 0, as padding of a batch) gets out = 0 and lse = -inf.
+ *     q, out      [n_seq][n_q_heads][head_dim] by strides
+ *     k, v        [n_pages][n_kv_heads][page_len][head_dim] by the strides of a page, a head and a row (a pool of
+ *                 [pages][rows][heads][elements] is addressed in place), elements of a row contiguous
+ *     page_table  [n_seq][max_pages] int32 in device memory, rows table_stride apart
+ *     cache_len   [n_seq] int32 in device memory; values outside [0, max_len] are moved into it
+ *     score       [n_seq][n_kv_heads][>= max_len] fp32 by strides, entries contiguous; may be NULL
+ *     lse         [n_seq][n_q_heads] fp32, may be NULL
+ * Arithmetic as in reform_chunk_attend_score (the score sums unrounded fp32 probabilities), bitwise reproducible for the
+ * same arguments; results depend on the batch and on max_len by rounding only.  Keys and values that are not finite stay
+ * within their sequence and KV head.  Rows behind L are never looked at.
+ * Supported: types and head_dim as reform_prompt_attend; any page_len >= 1; n_pages * page_len below 2^31; max_len at most
+ * max_pages * page_len and 2^31 - 512; row stride of k and v below 2^24; n_seq * n_q_heads at most 2^22; with B = ceil(n_q_heads /
+ * n_kv_heads / 16), n_seq * n_kv_heads * B * (max_len / 16 + 64) below 2^31.  n_seq = 0 does nothing.
+ * The workspace takes partial results of caches that are shared out over workgroups, and the logits of all keys if the score is asked
+ * for (4 bytes a key that can be seen and query head); the query wants to know whether it is: want_score.  Without it, or with less than the
+ * query asks for, the call returns REFORM_ERR_WORKSPACE.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t  dtype;
+    int32_t  n_seq, n_q_heads, n_kv_heads, head_dim;
+    int32_t  page_len, n_pages, max_pages, max_len;
+    int32_t  window, n_sink;                 /* window >= 0 (0: all keys), n_sink >= 0         */
+    int32_t  want_score;                     /* 1 iff score is not NULL                        */
+    int32_t  accumulate;                     /* 0: score = ..., 1: score += ...                */
+    float    scale;                          /* > 0, finite                                    */
+    int32_t  reserved;                       /* 0                                              */
+    int64_t  q_seq_stride, q_head_stride, o_seq_stride, o_head_stride;   /* elements, multiples of 16 bytes */
+    int64_t  kv_page_stride, kv_head_stride, kv_row_stride;              /* likewise           */
+    int64_t  table_stride, score_seq_stride, score_head_stride;          /* elements           */
+} reform_paged_desc;
+
+size_t reform_paged_attend_workspace(const reform_paged_desc *desc);
+
+reform_status reform_paged_attend(const reform_paged_desc *desc, const void *q, const void *k, const void *v,
+                                  const int32_t *page_table, const int32_t *cache_len, float *score,
+                                  void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------- */
+/* reform_paged_evict -- caches in pages go back to their budget
+ *
+ * The rule of reform_evict_topk_compact for every sequence b of a batch and every KV head: of L = cache_len[b] > budget keys those
+ * `budget` are kept whose score is largest (ties: the lowest index), the first n_sink and the last n_recent always
+ * among them.  Then row r of the head becomes old row kept_idx[r], r < budget, in ascending order, for k, v, score and pos
+ * alike, in place.  A sequence of L <= budget keys stays as it is (kept_idx[r] = r).  Rows behind keep what they held.
+ * new_len[b] = min(L, budget): pages behind it can be given back.
+ *     k, v, page_table, cache_len   as in reform_paged_attend; the pages of sequences that outgrew their budget must be their
+ *              own: a page that is in the table twice holds undefined rows afterwards.  Rows whose page number lies outside
+ *              [0, n_pages) are neither read nor written: what would come from there leaves the row it would go to as it is
+ *     score    [n_seq][n_kv_heads][>= max_len] fp32 by strides, entries contiguous, in/out; must be finite (no NaN/Inf)
+ *     pos      like score, with its strides, int32 that travel with the rows, in/out; may be NULL
+ *     kept_idx [n_seq][n_kv_heads][budget] int32 out, contiguous, the first new_len entries of a head; may be NULL
+ *     new_len  [n_seq] int32 out, may be NULL; must not be cache_len itself
+ * Supported: head_dim * sizeof(element) a multiple of 16 up to 4096; strides of k and v multiples of 16 bytes; page_len, n_pages,
+ * max_pages, max_len as in reform_paged_attend; budget at least 1; n_seq * n_kv_heads * (row bytes / 32 + 4) below 2^23.  n_seq = 0 does
+ * nothing.
+ */
+typedef struct {
+    uint32_t struct_size;
+    int32_t  dtype;
+    int32_t  n_seq, n_kv_heads, head_dim;
+    int32_t  page_len, n_pages, max_pages, max_len;
+    int32_t  budget, n_sink, n_recent;       /* n_sink + n_recent <= budget                    */
+    int64_t  kv_page_stride, kv_head_stride, kv_row_stride;              /* elements           */
+    int64_t  table_stride, score_seq_stride, score_head_stride;
+} reform_paged_evict_desc;
+
+size_t reform_paged_evict_workspace(const reform_paged_evict_desc *desc);
+
+reform_status reform_paged_evict(const reform_paged_evict_desc *desc, void *k, void *v, float *score, int32_t *pos,
+                                 const int32_t *page_table, const int32_t *cache_len, int32_t *kept_idx, int32_t *new_len,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* ------------------------------------------------------------------------------------------- */
 /* Measurement aids (no step of the method): what this machine sustains on the resources the

@@ -29,6 +29,9 @@ EXPORTED = [
     "reform_rerotate_keys", "reform_gather_rows", "reform_rotary_embed",
     "reform_prompt_attend_workspace", "reform_prompt_attend",
     "reform_tree_attend_workspace", "reform_tree_attend", "reform_tree_accept",
+    "reform_window_attend_workspace", "reform_window_attend",
+    "reform_paged_attend_workspace", "reform_paged_attend",
+    "reform_paged_evict_workspace", "reform_paged_evict",
     "reform_probe_mfma_bf16", "reform_probe_stream",
     "reform_status_string", "reform_version",
 ]
@@ -136,6 +139,32 @@ class AcceptDesc(ctypes.Structure):
                 ("kv_layer_stride", ctypes.c_int64)]
 
 
+class WindowDesc(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32),
+                 ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                 ("n_seq", ctypes.c_int32), ("n_q_rows", ctypes.c_int32), ("n_k_rows", ctypes.c_int32),
+                 ("scale", ctypes.c_float), ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+                + [(f"{t}_{u}_stride", ctypes.c_int64) for t in "qkvo" for u in ("head", "row")])
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("n_seq", ctypes.c_int32),
+                 ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                 ("page_len", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                 ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("want_score", ctypes.c_int32),
+                 ("accumulate", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+                + [(f"{t}_stride", ctypes.c_int64) for t in ("q_seq", "q_head", "o_seq", "o_head", "kv_page", "kv_head", "kv_row", "table",
+                                                             "score_seq", "score_head")])
+
+
+class PagedEvictDesc(ctypes.Structure):
+    _fields_ = ([("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("n_seq", ctypes.c_int32),
+                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                 ("page_len", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                 ("budget", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("n_recent", ctypes.c_int32)]
+                + [(f"{t}_stride", ctypes.c_int64) for t in ("kv_page", "kv_head", "kv_row", "table", "score_seq", "score_head")])
+
+
 def library_path():
     return _LIB_PATH
 
@@ -190,6 +219,13 @@ def load_library():
     lib.reform_tree_attend.argtypes = [vp] * 10 + [sz, vp]
     lib.reform_tree_accept.restype = ctypes.c_int
     lib.reform_tree_accept.argtypes = [vp] * 13
+    for name in ("window_attend", "paged_attend", "paged_evict"):
+        getattr(lib, f"reform_{name}_workspace").restype = sz
+        getattr(lib, f"reform_{name}_workspace").argtypes = [vp]
+        getattr(lib, f"reform_{name}").restype = ctypes.c_int
+    lib.reform_window_attend.argtypes = [vp] * 9 + [sz, vp]
+    lib.reform_paged_attend.argtypes = [vp] * 10 + [sz, vp]
+    lib.reform_paged_evict.argtypes = [vp] * 10 + [sz, vp]
     lib.reform_probe_mfma_bf16.restype = ctypes.c_int
     lib.reform_probe_mfma_bf16.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int32, vp]
     lib.reform_probe_stream.restype = ctypes.c_int
@@ -439,6 +475,7 @@ def _packer(cls):
 
 
 _pack_rotary, _pack_prompt, _pack_tree, _pack_accept = map(_packer, (RotaryDesc, PromptDesc, TreeDesc, AcceptDesc))
+_pack_window, _pack_paged, _pack_paged_evict = map(_packer, (WindowDesc, PagedDesc, PagedEvictDesc))
 
 
 class _Codes(dict):
@@ -704,6 +741,144 @@ def reform_tree_accept(parent, drafted, target, cache_len, k=None, v=None, node_
                                 _i32(new_len, S, dev, "new_len"), _stream_of(stream, dev))
     _check(rc, "reform_tree_accept")
     return path, accepted, next_token, new_len
+
+
+def _window_fields(q, k, v, out, n_seq, scale, window, n_sink):
+    f = _prompt_fields(q, k, v, out, n_seq, scale)       # its last scalar, `reserved`, gives way to window, n_sink and this one's
+    return f[:8] + (window, n_sink, 0) + f[9:]
+
+
+def window_desc(q, k, v, out, cu_q, scale, window, n_sink=0):
+    return WindowDesc(ctypes.sizeof(WindowDesc), *_window_fields(q, k, v, out, cu_q.shape[0] - 1, scale, window, n_sink))
+
+
+def reform_window_attend(q, k, v, cu_q, scale, window, n_sink=0, cu_k=None, out=None, lse=None, workspace=None, stream=None):
+    """As reform_prompt_attend, each row seeing the last `window` keys up to its own and the first n_sink keys of its sequence.
+    Returns (out, lse [Hq, nq])."""
+    lib = load_library()
+    if out is None:
+        out = _new(torch.zeros, q.shape, q.dtype, q.device, stream)
+    if lse is None:
+        lse = _new(torch.zeros, q.shape[:2], torch.float32, q.device, stream)
+    n = cu_q.numel()
+    fields = _window_fields(q, k, v, out, n - 1, scale, window, n_sink)
+    if n < 1 or (cu_k is None and fields[6] != fields[5]):
+        raise ValueError("cu_k is needed where there are more or fewer key rows")
+    if lse.dtype is not torch.float32 or lse.numel() != fields[1] * fields[5] or not lse.is_contiguous():
+        raise ValueError("lse: [heads, rows] fp32")
+    dev = _gpu(q)
+    desc = _pack_window(*fields)
+    ws, ws_bytes = _scratch(lib.reform_window_attend_workspace, desc, dev, workspace, q, stream)
+    rc = lib.reform_window_attend(desc, q.data_ptr(), _at(k, dev), _at(v, dev), _i32(cu_q, n, dev, "cu_q"),
+                                  _i32(cu_k, n, dev, "cu_k"), _at(out, dev), _at(lse, dev), ws, ws_bytes, _stream_of(stream, dev))
+    _check(rc, "reform_window_attend")
+    return out, lse
+
+
+def _pool_fields(k, v, page_table, score, max_len, n_seq, Hkv):
+    """What the calls on caches in pages have in common: (head_dim, page_len, n_pages, max_pages, max_len), the strides of
+    k and v, and those of the table and the scores."""
+    shape, ks, ps = k.shape, k.stride(), page_table.shape
+    if len(shape) != 4 or v.shape != shape or v.stride() != ks or v.dtype is not k.dtype or shape[1] != Hkv or ks[3] != 1:
+        raise ValueError("k and v: alike, [pages, heads, rows, elements], elements contiguous")
+    if page_table.dtype is not _I32 or len(ps) != 2 or ps[0] != n_seq or (page_table.stride(1) != 1 and ps[1] != 1):
+        raise ValueError("page_table: [sequences, pages] int32, a sequence's pages contiguous")
+    most, ss = ps[1] * shape[2], (0, 0, 1)
+    if score is not None:
+        rows, ss = score.shape, score.stride()
+        if len(rows) != 3 or rows[0] != n_seq or rows[1] != Hkv or score.dtype is not torch.float32 or (ss[2] != 1 and rows[2] != 1):
+            raise ValueError("score: [sequences, KV heads, keys] fp32, a head's keys contiguous")
+        most = min(most, rows[2])
+    if max_len is None:
+        max_len = min(most, (1 << 31) - 512)
+    elif score is not None and max_len > rows[2]:
+        raise ValueError("score: max_len keys at least")
+    return (shape[3], shape[2], shape[0], ps[1], max_len), ks[:3], (page_table.stride(0), ss[0], ss[1])
+
+
+def _paged_fields(q, k, v, out, page_table, scale, window, n_sink, score, accumulate, max_len):
+    S, Hq, d = shape = q.shape
+    qs, os = q.stride(), out.stride()
+    if out.shape != shape or k.dtype is not q.dtype or out.dtype is not q.dtype or qs[2] != 1 or os[2] != 1:
+        raise ValueError("q and out: [sequences, heads, elements], of k's type, elements contiguous")
+    Hkv = k.shape[1]
+    pool, kvs, strides = _pool_fields(k, v, page_table, score, max_len, S, Hkv)
+    if pool[0] != d:
+        raise ValueError("k: as many elements as q")
+    return (_DTYPES[q.dtype], S, Hq, Hkv, *pool, window, n_sink, score is not None, bool(accumulate), scale, 0,
+            qs[0], qs[1], os[0], os[1], *kvs, *strides)
+
+
+def paged_desc(q, k, v, out, page_table, scale, window=0, n_sink=0, score=None, accumulate=False, max_len=None):
+    return PagedDesc(ctypes.sizeof(PagedDesc), *_paged_fields(q, k, v, out, page_table, scale, window, n_sink, score, accumulate, max_len))
+
+
+def reform_paged_attend(q, k, v, page_table, cache_len, scale, window=0, n_sink=0, score=None, accumulate=False, max_len=None,
+                        out=None, lse=None, workspace=None, stream=None):
+    """q [S, Hq, d]: one new token of each of S sequences; k, v [pages, Hkv, page_len, d]: a pool of pages (any strides with
+    contiguous elements), page_table [S, max_pages] i32, cache_len [S] i32 (the new token's row counts).  window > 0: the last
+    `window` keys and the first n_sink are seen.  score [S, Hkv, keys] f32: the attention that every key receives is written, or
+    added.  max_len bounds cache_len (None: what table and score have room for).  Returns (out, lse [S, Hq])."""
+    lib = load_library()
+    if out is None:
+        out = _new(torch.empty, q.shape, q.dtype, q.device, stream)
+    if lse is None:
+        lse = _new(torch.empty, q.shape[:2], torch.float32, q.device, stream)
+    fields = _paged_fields(q, k, v, out, page_table, scale, window, n_sink, score, accumulate, max_len)
+    S = fields[1]
+    if lse.dtype is not torch.float32 or lse.numel() != S * fields[2] or not lse.is_contiguous():
+        raise ValueError("lse: [sequences, heads] fp32")
+    dev = _gpu(q)
+    desc = _pack_paged(*fields)
+    ws, ws_bytes = _scratch(lib.reform_paged_attend_workspace, desc, dev, workspace, q, stream)
+    rc = lib.reform_paged_attend(desc, q.data_ptr(), _at(k, dev), _at(v, dev), _at(page_table, dev), _i32(cache_len, S, dev, "cache_len"),
+                                 _at(score, dev), _at(out, dev), _at(lse, dev), ws, ws_bytes, _stream_of(stream, dev))
+    _check(rc, "reform_paged_attend")
+    return out, lse
+
+
+def _paged_evict_fields(k, v, score, page_table, budget, n_sink, n_recent, max_len):
+    S, Hkv = score.shape[:2]
+    pool, kvs, strides = _pool_fields(k, v, page_table, score, max_len, S, Hkv)
+    return (_DTYPES[k.dtype], S, Hkv, *pool, budget, n_sink, n_recent, *kvs, *strides)
+
+
+def paged_evict_desc(k, v, score, page_table, budget, n_sink=0, n_recent=0, max_len=None):
+    return PagedEvictDesc(ctypes.sizeof(PagedEvictDesc), *_paged_evict_fields(k, v, score, page_table, budget, n_sink, n_recent, max_len))
+
+
+def reform_paged_evict(k, v, score, page_table, cache_len, budget, n_sink=0, n_recent=0, pos=None, kept_idx=None, new_len=None,
+                       max_len=None, workspace=None, stream=None):
+    """k, v [pages, Hkv, page_len, d], score (and pos, int32, with its strides) [S, Hkv, keys], page_table [S, max_pages] i32,
+    cache_len [S] i32: sequences of more than `budget` keys keep those with the largest scores, the first n_sink and the
+    last n_recent among them, moved together in place.  kept_idx [S, Hkv, budget] i32.  Returns new_len [S] i32."""
+    lib = load_library()
+    S, Hkv = score.shape[:2]
+    if new_len is None:
+        new_len = _new(torch.empty, (S,), _I32, score.device, stream)
+    fields = _paged_evict_fields(k, v, score, page_table, budget, n_sink, n_recent, max_len)
+    if pos is not None and (pos.dtype is not _I32 or pos.shape != score.shape or pos.stride() != score.stride()):
+        raise ValueError("pos: int32, shape and strides of score")
+    dev = _gpu(k)
+    desc = _pack_paged_evict(*fields)
+    ws, ws_bytes = _scratch(lib.reform_paged_evict_workspace, desc, dev, workspace, k, stream)
+    rc = lib.reform_paged_evict(desc, k.data_ptr(), _at(v, dev), _at(score, dev), _at(pos, dev), _at(page_table, dev),
+                                _i32(cache_len, S, dev, "cache_len"), _i32(kept_idx, S * Hkv * budget, dev, "kept_idx"),
+                                _i32(new_len, S, dev, "new_len"), ws, ws_bytes, _stream_of(stream, dev))
+    _check(rc, "reform_paged_evict")
+    return new_len
+
+
+def window_workspace_bytes(desc):
+    return load_library().reform_window_attend_workspace(ctypes.byref(desc))
+
+
+def paged_workspace_bytes(desc):
+    return load_library().reform_paged_attend_workspace(ctypes.byref(desc))
+
+
+def paged_evict_workspace_bytes(desc):
+    return load_library().reform_paged_evict_workspace(ctypes.byref(desc))
 
 
 def prompt_workspace_bytes(desc):

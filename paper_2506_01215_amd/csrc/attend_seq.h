@@ -12,23 +12,7 @@
 #pragma once
 #include "attend_tile.h"
 
-#include <atomic>
-
 namespace reform {
-
-// More than the default 64 KB of LDS for a kernel: once per kernel and device, not per launch.
-template <auto KERNEL>
-inline hipError_t raise_lds(size_t bytes)
-{
-    static std::atomic<bool> raised[64];
-    int dev = 0;
-    const hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return e;
-    if (dev >= 0 && dev < 64 && raised[dev].load(std::memory_order_acquire)) return hipSuccess;
-    const hipError_t f = hipFuncSetAttribute((const void *)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (f == hipSuccess && dev >= 0 && dev < 64) raised[dev].store(true, std::memory_order_release);
-    return f;
-}
 
 struct SeqRows {
     const void *q;           // first row of the group's first head

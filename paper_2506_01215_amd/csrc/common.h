@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace reform {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -175,6 +177,7 @@ struct PromptParams {
     float *lse;              // nullable
     const int32_t *cu_q, *cu_k;
     int Hq, Hkv, G, D, n_seq, n_q, n_k;
+    int window, n_sink;      // reform_window_attend: keys behind a row's own that it sees (its own among them), first keys that all see
     long q_hs, q_rs, k_hs, k_rs, v_hs, v_rs, o_hs, o_rs;     // elements
     float scale;
     int by_head;             // as in AttnParams
@@ -184,6 +187,40 @@ struct PromptParams {
     int block, part_rows;    // rows of a block then, and of one partial result
     float *part_o;           // as in TreeParams, [2 * shares][part_rows][D]
     float2 *part_ml;
+};
+
+// A pool of pages that sequences share, and how a sequence's key is found in it (pool_row).
+struct PagedPool {
+    const int32_t *table;    // [n_seq][max_pages], rows table_stride apart
+    long table_stride;
+    unsigned n_pages, page_len;
+    unsigned magic;          // key / page_len = (mulhi(key, magic) + key) >> shift for keys below 2^31
+    int shift;
+    long page_stride, head_stride, row_stride;       // elements
+};
+
+struct PagedParams {
+    const void *q, *k, *v;
+    void *out;
+    float *lse, *score;      // nullable
+    const int32_t *cache_len;
+    PagedPool pool;
+    int n_seq, Hq, Hkv, G, D, max_len, window, n_sink, accumulate;
+    long q_ss, q_hs, o_ss, o_hs, score_ss, score_hs;         // elements
+    float scale;
+};
+
+struct PagedEvictParams {
+    void *k, *v;
+    float *score;
+    int32_t *pos, *kept, *new_len;           // nullable
+    const int32_t *cache_len;
+    PagedPool pool;
+    int n_seq, Hkv, max_len, budget, n_sink, n_recent;
+    int row_bytes, elt;      // of a row of k and v, of an element
+    long score_ss, score_hs;
+    int32_t *src;            // [n_seq][Hkv][budget]: pool rows (page * page_len + row) that the kept keys come from, -1: none
+    int32_t *first;          // [n_seq][Hkv]: first row that moves
 };
 
 struct EmbedParams {
@@ -226,6 +263,28 @@ struct GatherParams {
     float eps;
     int q0, nq_grp;      // first query and number of queries of this similarity launch
 };
+
+// Element offset of key j's row inside the pool (for head 0), -1 where its page is not in the pool.  `table`: the sequence's.
+__device__ __forceinline__ unsigned pool_page(const PagedPool &p, unsigned j) { return (__umulhi(j, p.magic) + j) >> p.shift; }
+__device__ __forceinline__ long pool_row(const PagedPool &p, const int32_t *table, int j)
+{
+    const unsigned page = pool_page(p, (unsigned)j), id = (unsigned)table[page];
+    return id < p.n_pages ? (long)id * p.page_stride + (long)((unsigned)j - page * p.page_len) * p.row_stride : -1l;
+}
+
+// More than the default 64 KB of LDS for a kernel: once per kernel and device, not per launch.
+template <auto KERNEL>
+inline hipError_t raise_lds(size_t bytes)
+{
+    static std::atomic<bool> raised[64];
+    int dev = 0;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev >= 0 && dev < 64 && raised[dev].load(std::memory_order_acquire)) return hipSuccess;
+    const hipError_t f = hipFuncSetAttribute((const void *)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (f == hipSuccess && dev >= 0 && dev < 64) raised[dev].store(true, std::memory_order_release);
+    return f;
+}
 
 // Compute units of the current device (reform_api.hip; cached per device, 0 if it cannot be told).
 int device_compute_units();

@@ -2,11 +2,10 @@
 // validation and kernel launches; nothing here allocates device memory or synchronises.
 #include "../../include/reform.h"
 #include "common.h"
+#include "serving_checks.h"
 
-#include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <initializer_list>
 
 namespace reform {
 hipError_t rotary_embed_launch(const RotaryParams &p, bool bf16, bool adjacent, hipStream_t st);
@@ -26,44 +25,6 @@ using namespace reform;
 
 namespace {
 
-inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
-inline int64_t elt_size(int dtype) { return dtype == REFORM_BF16 ? 2 : 4; }
-inline bool known_dtype(int dtype) { return dtype == REFORM_F32 || dtype == REFORM_BF16; }
-
-struct Walk {
-    int64_t n, step;
-};
-
-// Strides of something that is written: its pieces of `extent` elements, at every combination of the walks' steps, must not
-// overlap.  Sorted by their steps, each walk's step has to pass over all that the ones before it cover.
-bool bad_out_strides(int64_t extent, std::initializer_list<Walk> walks)
-{
-    Walk w[4];
-    int n = 0;
-    for (const Walk &x : walks) {
-        if (x.step < 0) return true;
-        if (x.n > 1) w[n++] = x;
-    }
-    std::sort(w, w + n, [](const Walk &x, const Walk &y) { return x.step < y.step; });
-    double covered = (double)extent;
-    for (int i = 0; i < n; ++i) {
-        if ((double)w[i].step < covered) return true;
-        covered += (double)(w[i].n - 1) * (double)w[i].step;
-    }
-    return false;
-}
-
-// What the attention calls support of types and heads.
-reform_status check_heads(int32_t dtype, int32_t n_q, int32_t n_kv, int32_t dim, float scale)
-{
-    if (!known_dtype(dtype) || n_q <= 0 || n_kv <= 0 || n_q % n_kv || dim <= 0) return REFORM_ERR_INVALID_ARG;
-    if (!(scale > 0.f) || !std::isfinite(scale)) return REFORM_ERR_INVALID_ARG;
-    if (dtype == REFORM_BF16 ? dim != 64 && dim != 128 : dim % 4 || dim > 256) return REFORM_ERR_UNSUPPORTED;
-    return REFORM_OK;
-}
-
-constexpr double kMaxGroups = 8388607.0;                 // workgroups of 512 threads in a grid
-constexpr int64_t kMaxRowStride = 1 << 24;               // offsets inside a tile of 64 rows stay within 32 bits
 // Keys of a sequence, and the row behind the tiles that a loop asks about next (two groups of waves, 64 keys a tile: up to 320 rows
 // further), are counted in 32-bit signed integers.
 constexpr int64_t kMaxTreeKeys = (1ll << 31) - 512;
@@ -86,12 +47,6 @@ reform_status check_prompt(const reform_prompt_desc *d)
     if ((double)d->n_q_heads * d->n_q_rows / 16.0 + (double)d->n_kv_heads * d->n_seq > kMaxGroups) return REFORM_ERR_UNSUPPORTED;
     if (d->k_row_stride >= kMaxRowStride || d->v_row_stride >= kMaxRowStride) return REFORM_ERR_UNSUPPORTED;
     return REFORM_OK;
-}
-
-int compute_units()
-{
-    const int n = device_compute_units();
-    return n > 0 ? n : 256;
 }
 
 PromptParams prompt_sizes(const reform_prompt_desc *d)
