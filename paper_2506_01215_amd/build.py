@@ -14,7 +14,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libreform_hip.so")
 SOURCES = ["reform_api.hip", "attend_bf16.hip", "attend_f32.hip", "evict.hip", "gather.hip", "select.hip", "pool.hip", "embed.hip", "rope.hip", "rows.hip", "probe.hip",
            "serving_api.hip", "rotary.hip", "accept.hip", "attend_prompt.hip", "tree.hip", "attend_seq_f32.hip",
-           "paged_api.hip", "attend_window.hip", "attend_paged.hip", "evict_paged.hip"]
+           "paged_api.hip", "attend_window.hip", "attend_paged.hip", "attend_paged_f32.hip", "evict_paged.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]
 

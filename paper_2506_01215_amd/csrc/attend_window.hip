@@ -4,7 +4,7 @@
 namespace reform {
 
 template <class T>
-__global__ __launch_bounds__(64) void window_attend_simple(PromptParams p)
+__global__ __launch_bounds__(64) void window_attend_simple(WindowParams p)
 {
     const int row = blockIdx.x, head = blockIdx.y, g = head / p.G;
     const int32_t *cu_k = p.cu_k ? p.cu_k : p.cu_q;
@@ -29,7 +29,7 @@ __global__ __launch_bounds__(64) void window_attend_simple(PromptParams p)
     r.end((T *)p.out + (size_t)head * p.o_hs + (size_t)row * p.o_rs, p.lse ? p.lse + (size_t)head * p.n_q + row : nullptr, p.D);
 }
 
-hipError_t window_attend_launch(const PromptParams &p, bool bf16, hipStream_t st)
+hipError_t window_attend_launch(const WindowParams &p, bool bf16, hipStream_t st)
 {
     if (bf16) hipLaunchKernelGGL((window_attend_simple<u16>), dim3(p.n_q, p.Hq), dim3(64), 0, st, p);
     else hipLaunchKernelGGL((window_attend_simple<float>), dim3(p.n_q, p.Hq), dim3(64), 0, st, p);

@@ -177,7 +177,6 @@ struct PromptParams {
     float *lse;              // nullable
     const int32_t *cu_q, *cu_k;
     int Hq, Hkv, G, D, n_seq, n_q, n_k;
-    int window, n_sink;      // reform_window_attend: keys behind a row's own that it sees (its own among them), first keys that all see
     long q_hs, q_rs, k_hs, k_rs, v_hs, v_rs, o_hs, o_rs;     // elements
     float scale;
     int by_head;             // as in AttnParams
@@ -187,6 +186,10 @@ struct PromptParams {
     int block, part_rows;    // rows of a block then, and of one partial result
     float *part_o;           // as in TreeParams, [2 * shares][part_rows][D]
     float2 *part_ml;
+};
+
+struct WindowParams : PromptParams {
+    int window, n_sink;      // keys up to a row's own that it sees, and first keys that all rows see: both at most n_k
 };
 
 // A pool of pages that sequences share, and how a sequence's key is found in it (pool_row).
@@ -208,6 +211,12 @@ struct PagedParams {
     int n_seq, Hq, Hkv, G, D, max_len, window, n_sink, accumulate;
     long q_ss, q_hs, o_ss, o_hs, score_ss, score_hs;         // elements
     float scale;
+    int shares, least, units, block, row_blocks, part_rows;  // as in TreeParams
+    float *part_o;
+    float2 *part_ml;
+    float *logits;           // [n_seq][Hq][logit_keys], with a score: q.k of the tiles that are gone through, -inf where not seen
+    float2 *row_ml;          // [n_seq][Hq], with a score and a second launch: as part_ml, of items that one workgroup finished
+    int logit_keys;
 };
 
 struct PagedEvictParams {

@@ -8,8 +8,12 @@
 #include <cstring>
 
 namespace reform {
-hipError_t window_attend_launch(const PromptParams &p, bool bf16, hipStream_t st);
-hipError_t paged_attend_launch(const PagedParams &p, bool bf16, hipStream_t st);
+hipError_t window_attend_launch(const WindowParams &p, bool bf16, hipStream_t st);
+void paged_plan_bf16(PagedParams &p);
+void paged_plan_f32(PagedParams &p);
+hipError_t paged_attend_bf16(const PagedParams &p, hipStream_t st);
+hipError_t paged_attend_f32_launch(const PagedParams &p, hipStream_t st);
+size_t tree_part_dim(bool bf16, int D);
 hipError_t paged_evict_launch(const PagedEvictParams &p, hipStream_t st);
 }  // namespace reform
 
@@ -40,9 +44,9 @@ reform_status check_window(const reform_window_desc *d)
     return REFORM_OK;
 }
 
-PromptParams window_sizes(const reform_window_desc *d)
+WindowParams window_sizes(const reform_window_desc *d)
 {
-    PromptParams p;
+    WindowParams p;
     std::memset(&p, 0, sizeof(p));
     p.Hq = d->n_q_heads; p.Hkv = d->n_kv_heads; p.G = p.Hq / p.Hkv; p.D = d->head_dim;
     p.n_seq = d->n_seq; p.n_q = d->n_q_rows; p.n_k = d->n_k_rows;
@@ -124,7 +128,26 @@ PagedParams paged_sizes(const reform_paged_desc *d, const int32_t *page_table)
     p.q_ss = d->q_seq_stride; p.q_hs = d->q_head_stride; p.o_ss = d->o_seq_stride; p.o_hs = d->o_head_stride;
     p.score_ss = d->score_seq_stride; p.score_hs = d->score_head_stride;
     p.scale = d->scale;
+    p.units = compute_units();
+    if (d->dtype == REFORM_BF16) paged_plan_bf16(p);
+    else paged_plan_f32(p);
     return p;
+}
+
+// The workspace's parts, in this order: pieces and their sums, then with a score the logits and the rows' sums.
+struct PagedRoom {
+    size_t part_o, part_ml, logits, row_ml;
+    size_t all() const { return part_o + part_ml + logits + row_ml; }
+};
+PagedRoom paged_room(const reform_paged_desc *d, const PagedParams &p)
+{
+    const size_t rows = (size_t)2 * p.shares * p.row_blocks * p.part_rows, heads = (size_t)p.n_seq * p.Hq;
+    PagedRoom r;
+    r.part_o = align_up(rows * tree_part_dim(d->dtype == REFORM_BF16, p.D) * sizeof(float));
+    r.part_ml = align_up(rows * sizeof(float2));
+    r.logits = d->want_score ? align_up(heads * p.logit_keys * sizeof(float)) : 0;
+    r.row_ml = d->want_score ? align_up(heads * sizeof(float2)) : 0;
+    return r;
 }
 
 reform_status check_paged_evict(const reform_paged_evict_desc *d)
@@ -167,7 +190,7 @@ reform_status reform_window_attend(const reform_window_desc *d, const void *q, c
     if (d->n_q_rows == 0 || d->n_seq == 0) return REFORM_OK;
     if (!q || !out || !cu_q || (d->n_k_rows > 0 && (!k || !v))) return REFORM_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return REFORM_ERR_INVALID_ARG;
-    PromptParams p = window_sizes(d);
+    WindowParams p = window_sizes(d);
     p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse; p.cu_q = cu_q; p.cu_k = cu_k;
     return window_attend_launch(p, d->dtype == REFORM_BF16, (hipStream_t)hip_stream) == hipSuccess ? REFORM_OK : REFORM_ERR_RUNTIME;
 }
@@ -175,7 +198,8 @@ reform_status reform_window_attend(const reform_window_desc *d, const void *q, c
 // ---------------------------------------------------------------------------------------
 size_t reform_paged_attend_workspace(const reform_paged_desc *d)
 {
-    return 0;
+    if (check_paged(d) != REFORM_OK || d->n_seq == 0) return 0;
+    return paged_room(d, paged_sizes(d, nullptr)).all();
 }
 
 reform_status reform_paged_attend(const reform_paged_desc *d, const void *q, const void *k, const void *v, const int32_t *page_table,
@@ -190,7 +214,18 @@ reform_status reform_paged_attend(const reform_paged_desc *d, const void *q, con
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return REFORM_ERR_INVALID_ARG;
     PagedParams p = paged_sizes(d, page_table);
     p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse; p.score = score; p.cache_len = cache_len;
-    return paged_attend_launch(p, d->dtype == REFORM_BF16, (hipStream_t)hip_stream) == hipSuccess ? REFORM_OK : REFORM_ERR_RUNTIME;
+    const PagedRoom room = paged_room(d, p);
+    if (room.all()) {
+        if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < room.all()) return REFORM_ERR_WORKSPACE;
+        char *at = (char *)workspace;
+        p.part_o = (float *)at;
+        p.part_ml = (float2 *)(at + room.part_o);
+        p.logits = room.logits ? (float *)(at + room.part_o + room.part_ml) : nullptr;
+        p.row_ml = room.row_ml ? (float2 *)(at + room.part_o + room.part_ml + room.logits) : nullptr;
+    }
+    hipStream_t st = (hipStream_t)hip_stream;
+    const hipError_t e = d->dtype == REFORM_BF16 ? paged_attend_bf16(p, st) : paged_attend_f32_launch(p, st);
+    return e == hipSuccess ? REFORM_OK : REFORM_ERR_RUNTIME;
 }
 
 // ---------------------------------------------------------------------------------------

@@ -1,0 +1,217 @@
+// How single tokens' attention over caches in pages is dealt to workgroups (see reform_paged_attend in reform.h).
+//
+// The list of tree_list.h: every (sequence, KV head) is an item with a place for each key tile that it goes through, and the list is
+// cut into equal shares.  With a window these tiles are two runs, those of the first keys and those of the window, which are
+// counted through (PagedSpan): "virtual" tiles and keys are the ones counted so.
+//
+// With a score the logits q.k of all virtual keys are kept, [sequence][head][virtual key], since a key's probability needs the sum
+// over all keys: 4 bytes a key and head that are read once more, against d elements of K.  An item that one workgroup takes whole is
+// scored by it at once; the others in a second launch, which puts the pieces together as well (paged_join).
+#pragma once
+#include "tree_list.h"
+
+namespace reform {
+
+// The key tiles that a sequence of n keys goes through.
+template <int TK>
+struct PagedSpan {
+    int n, lo, sinks;        // keys; j >= lo or j < sinks is seen
+    int front, skip, tiles;  // tiles of the first keys; tiles between them and the window's; all that are gone through
+    __device__ __forceinline__ PagedSpan(const PagedParams &p, int len)
+    {
+        n = len;
+        lo = p.window ? max(n - p.window, 0) : 0;
+        sinks = min(p.n_sink, lo);
+        front = (sinks + TK - 1) / TK;
+        skip = max(lo / TK - front, 0);
+        tiles = max((n + TK - 1) / TK - skip, 1);        // one where there is no key: the result has to be written
+    }
+    __device__ __forceinline__ int tile(int u) const { return u < front ? u : u + skip; }
+    __device__ __forceinline__ bool seen(int j) const { return j < n && (j >= lo || j < sinks); }
+};
+
+template <int R, int TK>
+__device__ __forceinline__ TreeSeq tree_seq(const PagedParams &p, int b)
+{
+    TreeSeq s;
+    s.len = min(max(p.cache_len[b], 0), p.max_len);
+    s.nodes = 1;
+    s.blocks = p.row_blocks;
+    s.tiles = PagedSpan<TK>(p, s.len).tiles;
+    return s;
+}
+
+// The score of an item's virtual keys [32 * TK-tiles t0, t1), and of its part of the keys between the runs: by all threads of the
+// workgroup.  ml(r): reference (log2 units) and sum of the group's row r, from LDS.
+template <int TK, class ML>
+__device__ __forceinline__ void paged_score(const PagedParams &p, int b, int kvh, int len, int t0, int t1, int row0, int rows, ML ml)
+{
+    const PagedSpan<TK> s(p, len);
+    const float c = p.scale * kLog2e;
+    float *score = p.score + (size_t)b * p.score_ss + (size_t)kvh * p.score_hs;
+    const float *x = p.logits + ((size_t)b * p.Hq + (size_t)kvh * p.G + row0) * p.logit_keys;
+    const bool add = p.accumulate || row0 > 0;           // later rows of a group join what the first ones left
+    for (int v = t0 * TK + (int)threadIdx.x; v < t1 * TK; v += (int)blockDim.x) {
+        const int j = v < s.front * TK ? v : v + s.skip * TK;
+        if (j >= len) break;                             // virtual keys ascend
+        const float before = add && (row0 > 0 || j != len - 1) ? score[j] : 0.f;
+        float sum = 0.f;
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r) {
+            const float2 y = ml(r);                      // y.y: 1 / sum
+            sum += __builtin_amdgcn_exp2f(fmaf(x[(size_t)r * p.logit_keys + v], c, -y.x)) * y.y;
+        }
+        score[j] = before + sum;
+    }
+    if (p.accumulate || row0 > 0 || s.skip == 0) return;
+    const long gap = (long)s.skip * TK;
+    const int g0 = s.front * TK + (int)(gap * t0 / s.tiles), g1 = s.front * TK + (int)(gap * t1 / s.tiles);
+    for (int j = g0 + (int)threadIdx.x; j < g1; j += (int)blockDim.x) score[j] = 0.f;
+}
+
+// What paged_score wants of a row: reference 0 where it saw no key, so that -inf stays a weight of 0, and 1 / sum.
+__device__ __forceinline__ float2 score_row(float m, float l)
+{
+    return make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.0f / l);
+}
+
+constexpr int kScoreRows = 64;               // rows of a group that are scored at once
+
+// The second launch: its first `merges` workgroups put pieces together as tree_merge does, the others score the keys of a share each.
+template <int D, int R, int TK, bool BF16>
+__global__ __launch_bounds__(256) void paged_join(PagedParams p, int merges, int rows, int by_share)
+{
+    using List = TreeList<R, TK, PagedParams>;
+    if ((int)blockIdx.x >= merges) {
+        __shared__ float2 sml[kScoreRows];
+        const int block = (int)blockIdx.x - merges;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        auto item = [&](int b, int len, int kvh, int t0, int t1, int w0, int n) {      // n pieces from share w0 on, or 0: finished already
+            for (int row0 = 0; row0 < p.G; row0 += kScoreRows) {
+                const int here = min(kScoreRows, p.G - row0);
+                __syncthreads();                         // the rows before have been used
+                for (int r = wave; r < here; r += 4) {
+                    const int row = row0 + r, rb = row / R;
+                    float m = -INFINITY, l = 0.f;
+                    if (n == 0) {
+                        const float2 y = p.row_ml[(size_t)b * p.Hq + (size_t)kvh * p.G + row];
+                        m = y.x;
+                        l = y.y;
+                    } else {
+                        for (int x = lane; x < n; x += 64) {
+                            const float2 y = p.part_ml[tree_slot(p, w0 + x, x, rb) * p.part_rows + row - rb * R];
+                            const float top = fmaxf(m, y.x), ref = top == -INFINITY ? 0.f : top;
+                            l = l * __builtin_amdgcn_exp2f(m - ref) + y.y * __builtin_amdgcn_exp2f(y.x - ref);
+                            m = top;
+                        }
+                        const float top = wave_max(m), ref = top == -INFINITY ? 0.f : top;
+                        l = wave_sum(l * __builtin_amdgcn_exp2f(m - ref));
+                        m = top;
+                    }
+                    if (lane == 0) sml[r] = score_row(m, l);
+                }
+                __syncthreads();
+                paged_score<TK>(p, b, kvh, len, t0, t1, row0, here, [&](int r) { return sml[r]; });
+            }
+        };
+        if (p.shares == 0) {
+            const int b = block / p.Hkv, kvh = block - b * p.Hkv;
+            const TreeSeq seq = tree_seq<R, TK>(p, b);
+            item(b, seq.len, kvh, 0, seq.tiles, 0, 0);
+            return;
+        }
+        List list;
+        list.read(p);
+        if (block >= list.shares) return;
+        int which, first;
+        const int share = tree_share(block, list.shares, 1, which), begin = list.begin(share), end = list.begin(share + 1);
+        int b = list.find(p, begin, first);
+        TreeSeq seq = list.seq(p, b);
+        int kvh = (begin - first) / tree_places(seq);
+        int pos = first + kvh * tree_places(seq);
+        while (pos < end) {
+            const int t0 = max(begin - pos - kTreeStart, 0), t1 = min(end - pos - kTreeStart, seq.tiles);
+            if (t0 < t1) {
+                const int w0 = list.share_of(pos + kTreeStart), n = list.share_of(pos + kTreeStart + seq.tiles - 1) - w0 + 1;
+                item(b, seq.len, kvh, t0, t1, w0, n == 1 ? 0 : n);
+            }
+            pos += tree_places(seq);
+            if (++kvh == p.Hkv) {
+                kvh = 0;
+                if (++b >= p.n_seq) return;
+                seq = list.seq(p, b);
+            }
+        }
+        return;
+    }
+    List list;
+    list.read(p);
+    const int chunks = (p.part_rows + rows - 1) / rows * p.row_blocks;
+    int b, kvh, pos, rb, own = -1;
+    TreeSeq seq;
+    if (by_share) {                                      // the item that the share's end cuts
+        if ((int)blockIdx.x >= list.shares * chunks) return;
+        own = tree_share(blockIdx.x, list.shares, chunks, rb);
+        const int x = list.begin(own + 1) - 1;
+        b = list.find(p, x, pos);
+        seq = list.seq(p, b);
+        kvh = (x - pos) / tree_places(seq);
+    } else {                                             // an item's workgroups on the XCD that most of its shares ran on
+        const int item = tree_share(blockIdx.x, p.n_seq * p.Hkv, chunks, rb);
+        b = item / p.Hkv;
+        kvh = item - b * p.Hkv;
+        seq = list.seq(p, b);
+        pos = list.before(p, b);
+    }
+    const int chunk = rb / p.row_blocks;
+    rb -= chunk * p.row_blocks;
+    pos += kvh * tree_places(seq) + kTreeStart;
+    const int w0 = list.share_of(pos);
+    if (by_share && w0 != own) return;
+    const int n = list.share_of(pos + seq.tiles - 1) - w0 + 1;
+    const int r0 = chunk * rows, here = min(rows, p.G - rb * R - r0);
+    if (n == 1 || here <= 0) return;
+    int r, c4;
+    f32x4 y;
+    float m, l;
+    if (!merge_pieces<D>(p.part_o, p.part_ml, p.part_rows, n, r0, here, rows, [&](int x) { return tree_slot(p, w0 + x, x, rb); }, r, c4, y, m, l))
+        return;
+    const int head = kvh * p.G + rb * R + r0 + r;
+    const size_t dst = (size_t)b * p.o_ss + (size_t)head * p.o_hs + c4;
+    y *= l == 0.f ? 0.f : 1.0f / l;
+    if (c4 < p.D) {
+        if (BF16) *(v2u *)((u16 *)p.out + dst) = (v2u){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+        else *(f32x4 *)((float *)p.out + dst) = y;
+    }
+    if (c4 == 0 && p.lse) p.lse[(size_t)b * p.Hq + head] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Whether an item's workgroup scores it by itself: it has all of the item's keys and rows.
+__device__ __forceinline__ bool paged_scores_alone(const PagedParams &p) { return p.logits && p.shares == 0 && p.row_blocks == 1; }
+
+template <int D, int R, int TK, bool BF16>
+inline void paged_join_launch(const PagedParams &p, hipStream_t st)
+{
+    const bool by_share = (long)p.n_seq * p.Hkv > p.shares;
+    const long blocks = (by_share ? p.shares : (long)p.n_seq * p.Hkv) * p.row_blocks;
+    int rows = 1;                                        // as in tree_merge_launch
+    while (2 * rows <= 1024 / D && rows < p.part_rows && blocks * ((p.part_rows + rows - 1) / rows) > 3l * p.units) rows *= 2;
+    const long merges = p.shares ? blocks * ((p.part_rows + rows - 1) / rows) : 0;
+    const long scores = !p.logits || (p.shares == 0 && p.row_blocks == 1) ? 0 : p.shares ? p.shares : (long)p.n_seq * p.Hkv;
+    if (merges + scores)
+        hipLaunchKernelGGL((paged_join<D, R, TK, BF16>), dim3((unsigned)(merges + scores)), dim3(256), 0, st, p, (int)merges, rows, (int)by_share);
+}
+
+// Keys that the longest sequence may go through, in whole tiles of 32, and the list for blocks of R rows and tiles of TK keys (list_plan).
+inline void paged_plan(PagedParams &p, int R, int TK, int whole, int least, int workgroups)
+{
+    auto up = [](long x) { return (x + 31) / 32 * 32; };
+    long keys = up(p.max_len);
+    // a window of w keys lies in up to w / 32 + 2 tiles
+    if (p.window && up(p.n_sink) + up(p.window) + 32 < keys) keys = up(p.n_sink) + up(p.window) + 32;
+    if (keys < 32) keys = 32;
+    p.logit_keys = (int)keys;
+    list_plan(p, p.G, (double)keys, R, TK, whole, least, p.units, workgroups);
+}
+
+}  // namespace reform

@@ -31,28 +31,30 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams &p, int b)
     return s;
 }
 
-// Places of one of a sequence's items, and of all of them.
+// Places of one of a sequence's items, and of all of them.  P: the parameters of a call that has such a list (paged_list.h has another).
 __device__ __forceinline__ int tree_places(const TreeSeq &s) { return s.tiles + kTreeStart; }
-__device__ __forceinline__ int tree_items(const TreeParams &p, const TreeSeq &s) { return s.blocks ? p.Hkv : 0; }
-__device__ __forceinline__ int tree_all_places(const TreeParams &p, const TreeSeq &s) { return tree_items(p, s) * tree_places(s); }
+template <class P>
+__device__ __forceinline__ int tree_items(const P &p, const TreeSeq &s) { return s.blocks ? p.Hkv : 0; }
+template <class P>
+__device__ __forceinline__ int tree_all_places(const P &p, const TreeSeq &s) { return tree_items(p, s) * tree_places(s); }
 
 // The list as all lanes of a wave see it.  The first 64 sequences stay in the lanes' registers: with no more
 // than these the lengths are read once.
-template <int R, int TK>
+template <int R, int TK, class P = TreeParams>
 struct TreeList {
     int total, shares;                   // places, shares that are not empty
     int each, more;                      // places of a share; the first `more` shares have one place more
     TreeSeq lane;                        // sequence `lane`
     int lane_places;                     // and its places
 
-    __device__ __forceinline__ int load(const TreeParams &p, int b, TreeSeq &s) const
+    __device__ __forceinline__ int load(const P &p, int b, TreeSeq &s) const
     {
         s = {0, 0, 0, 0};
         if (b >= p.n_seq) return 0;
         s = tree_seq<R, TK>(p, b);
         return tree_all_places(p, s);
     }
-    __device__ __forceinline__ void read(const TreeParams &p)
+    __device__ __forceinline__ void read(const P &p)
     {
         const int l = threadIdx.x & 63;
         lane_places = load(p, l, lane);
@@ -78,14 +80,14 @@ struct TreeList {
         return y < 0 ? (int)((unsigned)x / (unsigned)(each + 1)) : more + (int)((unsigned)y / (unsigned)each);
     }
     // sequence b (the same in all lanes)
-    __device__ __forceinline__ TreeSeq seq(const TreeParams &p, int b) const
+    __device__ __forceinline__ TreeSeq seq(const P &p, int b) const
     {
         if (b >= 64) return tree_seq<R, TK>(p, b);
         return {__builtin_amdgcn_readlane(lane.len, b), __builtin_amdgcn_readlane(lane.nodes, b),
                 __builtin_amdgcn_readlane(lane.blocks, b), __builtin_amdgcn_readlane(lane.tiles, b)};
     }
     // places in front of sequence b
-    __device__ __forceinline__ int before(const TreeParams &p, int b) const
+    __device__ __forceinline__ int before(const P &p, int b) const
     {
         const int l = threadIdx.x & 63;
         int places = l < b ? lane_places : 0;
@@ -97,7 +99,7 @@ struct TreeList {
         return __builtin_amdgcn_readlane(wave_incl_scan(places), 63);
     }
     // the sequence that place x (< total) lies in, and its first place
-    __device__ __forceinline__ int find(const TreeParams &p, int x, int &first) const
+    __device__ __forceinline__ int find(const P &p, int x, int &first) const
     {
         const int l = threadIdx.x & 63;
         int sum = 0, mine[4] = {lane_places, 0, 0, 0};
@@ -140,34 +142,20 @@ __device__ __forceinline__ int tree_share(int block, int shares, int side, int &
 }
 
 // Where a share's piece of an item that it does not cover alone goes.
-__device__ __forceinline__ long tree_slot(const TreeParams &p, int share, int t0, int rb)
+template <class P>
+__device__ __forceinline__ long tree_slot(const P &p, int share, int t0, int rb)
 {
     return (2l * share + (t0 > 0 ? 0 : 1)) * p.row_blocks + rb;
 }
 
-// The items of one workgroup, in the list's order: f(rows, keys, first tile, last tile + 1, slot of a piece or -1).
-template <class T, int R, int TK, class F>
-__device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
+// The items of one workgroup, in the list's order: f(sequence, what it is, KV head, row block, first tile, last tile + 1, slot of a
+// piece or -1).
+template <int R, int TK, class P, class F>
+__device__ __forceinline__ void list_walk(const P &p, F f)
 {
     int rb;
-    auto segment = [&](int b, const TreeSeq &seq, int kvh, int t0, int t1, long slot) {
-        SeqRows r;
-        r.q = (const T *)p.q + (size_t)b * p.q_ss + (size_t)kvh * p.G * p.q_hs;
-        r.out = (T *)p.out + (size_t)b * p.o_ss + (size_t)kvh * p.G * p.o_hs;
-        r.lse = p.lse ? p.lse + ((size_t)b * p.Hq + (size_t)kvh * p.G) * p.T : nullptr;
-        r.q_hs = p.q_hs; r.q_rs = p.q_rs; r.o_hs = p.o_hs; r.o_rs = p.o_rs; r.lse_hs = p.T;
-        r.G = p.G; r.row0 = rb * R; r.rows = seq.nodes * p.G;
-        SeqKeys k;
-        k.k = (const T *)p.k + (size_t)b * p.kv_ss + (size_t)kvh * p.kv_hs;
-        k.v = (const T *)p.v + (size_t)b * p.kv_ss + (size_t)kvh * p.kv_hs;
-        k.k_rs = k.v_rs = p.D;
-        k.n = seq.len + seq.nodes; k.open = seq.len; k.shift = 0;
-        k.parent = p.parent ? p.parent + (size_t)b * p.T : nullptr;
-        k.nodes = seq.nodes;
-        f(r, k, t0, t1, slot);
-    };
     const bool whole = p.shares == 0;                    // one item to a workgroup
-    TreeList<R, TK> list;
+    TreeList<R, TK, P> list;
     int b, kvh, pos = 0, begin = 0, end, share = 0;
     TreeSeq seq;
     if (whole) {
@@ -196,7 +184,7 @@ __device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
         if (t0 < t1 && rb < seq.blocks) {
             if (again) __syncthreads();                  // the sums of the item before are still read
             again = true;
-            segment(b, seq, kvh, t0, t1, t0 > 0 || t1 < seq.tiles ? tree_slot(p, share, t0, rb) : -1);
+            f(b, seq, kvh, rb, t0, t1, t0 > 0 || t1 < seq.tiles ? tree_slot(p, share, t0, rb) : -1l);
         }
         pos += tree_places(seq);
         if (whole) return;
@@ -208,6 +196,28 @@ __device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
             } while (seq.blocks == 0);
         }
     }
+}
+
+// The drafted tokens' items: f(rows, keys, first tile, last tile + 1, slot of a piece or -1).
+template <class T, int R, int TK, class F>
+__device__ __forceinline__ void tree_walk(const TreeParams &p, F f)
+{
+    list_walk<R, TK>(p, [&](int b, const TreeSeq &seq, int kvh, int rb, int t0, int t1, long slot) {
+        SeqRows r;
+        r.q = (const T *)p.q + (size_t)b * p.q_ss + (size_t)kvh * p.G * p.q_hs;
+        r.out = (T *)p.out + (size_t)b * p.o_ss + (size_t)kvh * p.G * p.o_hs;
+        r.lse = p.lse ? p.lse + ((size_t)b * p.Hq + (size_t)kvh * p.G) * p.T : nullptr;
+        r.q_hs = p.q_hs; r.q_rs = p.q_rs; r.o_hs = p.o_hs; r.o_rs = p.o_rs; r.lse_hs = p.T;
+        r.G = p.G; r.row0 = rb * R; r.rows = seq.nodes * p.G;
+        SeqKeys k;
+        k.k = (const T *)p.k + (size_t)b * p.kv_ss + (size_t)kvh * p.kv_hs;
+        k.v = (const T *)p.v + (size_t)b * p.kv_ss + (size_t)kvh * p.kv_hs;
+        k.k_rs = k.v_rs = p.D;
+        k.n = seq.len + seq.nodes; k.open = seq.len; k.shift = 0;
+        k.parent = p.parent ? p.parent + (size_t)b * p.T : nullptr;
+        k.nodes = seq.nodes;
+        f(r, k, t0, t1, slot);
+    });
 }
 
 // Two for each of this chip's 256 compute units: the most that any form keeps there at once.
@@ -350,22 +360,27 @@ inline void tree_merge_launch(const TreeParams &p, hipStream_t st)
 // No shares where every item is short: then one workgroup takes an item whole, and there is nothing to merge.  Short is up to
 // `whole` keys where one item is alone on the chip, and up to 2.5 times as many where there are as many items as compute
 // units, since sharing these out gains only what their lengths differ by.
-inline void tree_plan(TreeParams &p, int R, int TK, int whole, int least, int compute_units, int workgroups)
+// `rows`: rows of an item, `keys`: keys of the longest.
+template <class P>
+inline void list_plan(P &p, int rows, double keys, int R, int TK, int whole, int least, int compute_units, int workgroups)
 {
-    const int rows = p.T * p.G;
     p.block = R;
     p.row_blocks = (rows + R - 1) / R;
     p.part_rows = rows < R ? rows : R;
     p.least = least;
     p.units = compute_units;
     const double items = (double)p.n_seq * p.Hkv, taken = items * p.row_blocks < compute_units ? items * p.row_blocks / compute_units : 1.0;
-    const double keys = (double)p.max_len + p.T;
     if (keys * (1.0 - 0.6 * taken) <= whole) return;
     const double most = items * (std::ceil(keys / TK) + kTreeStart) / least;
     const double want = items > most ? items : most;
     int room = workgroups / p.row_blocks;
     room = room < 1 ? 1 : room > kTreeMaxShares ? kTreeMaxShares : room;
     p.shares = want < room ? (int)want : room;
+}
+
+inline void tree_plan(TreeParams &p, int R, int TK, int whole, int least, int compute_units, int workgroups)
+{
+    list_plan(p, p.T * p.G, (double)p.max_len + p.T, R, TK, whole, least, compute_units, workgroups);
 }
 
 }  // namespace reform

@@ -92,6 +92,17 @@ def test_paged_rejects_pointers_scores_and_sizes():
     assert call_paged(paged(n_seq=0), None, None, None, None, None, None, None) == 0
 
 
+def test_paged_workspace_follows_what_is_asked_for():
+    need = lib().reform_paged_attend_workspace
+    plain, score = (need(ctypes.byref(paged(want_score=x))) for x in (0, 1))
+    assert score >= plain + 3 * 8 * 6400 * 4                            # the logits
+    assert need(ctypes.byref(paged(want_score=1, window=64, n_sink=4))) < score / 20      # of what the window shows
+    d = paged(want_score=1)
+    assert call_paged(d, score=FAKE) == 3
+    assert call_paged(d, score=FAKE, ws=FAKE, nbytes=score - 1) == 3
+    assert call_paged(d, score=FAKE, ws=FAKE + 16, nbytes=score) == 3
+
+
 def evict(**kw):
     base = dict(struct_size=size(binding.PagedEvictDesc), dtype=1, n_seq=3, n_kv_heads=2, head_dim=128, page_len=16, n_pages=500,
                 max_pages=400, max_len=6400, budget=4096, n_sink=4, n_recent=64, kv_page_stride=2 * 16 * 128, kv_head_stride=16 * 128,
