@@ -19,8 +19,6 @@
 #pragma once
 #include "attend_seq.h"
 
-#include <type_traits>
-
 namespace reform {
 
 constexpr int kRowsKeys = 64;
@@ -199,18 +197,20 @@ __device__ __forceinline__ void rows_tile(RowsWave<D> &w, const u16 *__restrict_
 
 // Key tiles [t0, t1) of the sequence for the block of ROWS rows from r.row0 on, as seq_segment.  by_head: how the rows are dealt to
 // the waves.
-template <int D, int NW, int KG, bool TREE, bool THIN = false>
-__device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool by_head, float scale, int t0, int t1, float *po,
+template <int D, int NW, int KG, bool TREE, bool THIN = false, class KEYS>
+__device__ __forceinline__ void rows_segment(const SeqRows &r, KEYS k, bool by_head, float scale, int t0, int t1, float *po,
                                              float2 *pml, u16 *lds)
 {
     using S = RowsShape<D, NW, KG, THIN>;
     constexpr int BN = S::BN, TILE = S::TILE, KS = S::KS, DB = S::DB, C8 = S::C8;
-    // keys are counted from the range's first one
-    k.k = (const u16 *)k.k + (size_t)t0 * BN * k.k_rs;
-    k.v = (const u16 *)k.v + (size_t)t0 * BN * k.v_rs;
-    k.n -= t0 * BN;
-    k.open -= t0 * BN;
-    k.shift -= t0 * BN;
+    constexpr bool WINDOW = std::is_same<KEYS, WindowKeys>::value;
+    if constexpr (!WINDOW) {                             // keys are counted from the range's first one (windows: a range is all tiles)
+        k.k = (const u16 *)k.k + (size_t)t0 * BN * k.k_rs;
+        k.v = (const u16 *)k.v + (size_t)t0 * BN * k.v_rs;
+        k.n -= t0 * BN;
+        k.open -= t0 * BN;
+        k.shift -= t0 * BN;
+    }
 
     const int lane = threadIdx.x & 63, wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int ln = lane & 15, lg = lane >> 4, kg = wave_all / NW, wave = wave_all % NW;
@@ -249,7 +249,14 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
     int tl = -1;                                         // last tile of the group that the wave needs
     if (row0 < r.rows) {
         const int last = TREE ? k.n - 1 : M + min(row0 + 31 * rstep, r.rows - 1) / r.G;       // prompts have no thin waves
-        if (last >= kg * BN && kg < ntiles) tl = (min(last / BN, ntiles - 1) - kg) / KG;       // a range may have fewer tiles than groups
+        if constexpr (WINDOW) {                          // the last key lies behind the first keys' run, or there is one run
+            if (last >= 0 && last / BN - k.skip >= kg && kg < ntiles) tl = (min(last / BN - k.skip, ntiles - 1) - kg) / KG;
+        } else if (last >= kg * BN && kg < ntiles) tl = (min(last / BN, ntiles - 1) - kg) / KG;       // a range may have fewer tiles than groups
+    }
+    int behind = -1, stay = 0;                           // as in seq_segment, of the wave's rows
+    if constexpr (WINDOW) {
+        behind = M + min(row0 + 31 * rstep, r.rows - 1) / r.G - k.window;
+        stay = k.sinks;
     }
     const int open = TREE ? k.open : M + row0 / r.G + 1; // keys below it are seen by all of the wave's rows
     unsigned long long *lines = (unsigned long long *)((char *)lds + S::line_at);
@@ -267,7 +274,7 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
         asm volatile("" : "+v"(l));                      // as in locate
 #pragma unroll
         for (int i = 0; i < S::LOADS; ++i) {
-            const int row = min((t * KG + kg) * BN + wave + S::lane_row(l) + i * NW, k.n - 1);
+            const int row = min(key_tile(k, t * KG + kg) * BN + wave + S::lane_row(l) + i * NW, k.n - 1);
             load_to_lds((const char *)((const u16 *)k.k + (size_t)row * k.k_rs + l % C8 * 8), to_k + i * NW * S::PITCH);
             load_to_lds((const char *)((const u16 *)k.v + (size_t)row * k.v_rs + l % C8 * 8), to_v + i * NW * S::PITCH);
         }
@@ -281,8 +288,8 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
     int t = 0, kslot = 0, vslot = 0;                     // the slots of tile t: t mod KSLOTS, t mod VSLOTS
     auto mask_tile = [&](auto &s) {
         constexpr int NB = sizeof(s) / sizeof(s[0]);
-        const int j0 = (t * KG + kg) * BN;
-        if (j0 + BN > open) {
+        const int j0 = key_tile(k, t * KG + kg) * BN;
+        if (j0 + BN > open || (WINDOW && j0 <= behind && j0 + BN > stay)) {
             asm volatile("; mask path" ::: "memory");
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
@@ -300,6 +307,7 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
                 } else {
                     const int more = M + at - j0 - 4 * (l >> 4);         // keys behind the lane's first that are seen
                     seen = more >= 63 ? ~0ull : more < 0 ? 0ull : (2ull << more) - 1ull;
+                    if constexpr (WINDOW) seen &= window_seen(k, M + at, j0 + 4 * (l >> 4));
                 }
                 const unsigned half[2] = {(unsigned)seen, (unsigned)(seen >> 32)};
 #pragma unroll
@@ -319,10 +327,10 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, SeqKeys k, bool b
         asm volatile("" ::: "memory");
         auto after = [](int slot, int by, int slots) { const int x = slot + by; return x >= slots ? x - slots : x; };
         const int next = (t + 1) * KG + kg;
-        const bool more = next < ntiles, whole = (next + 1) * BN <= k.n;
+        const bool more = next < ntiles, whole = (key_tile(k, next) + 1) * BN <= k.n;
         u16 *const nk = wk + (kslot ^ 1) * TILE, *const nv = wv + after(vslot, 1, S::VSLOTS) * TILE;
         if (more && !whole) load_end(t + 1, nk, nv);
-        const size_t j1 = (size_t)next * BN;
+        const size_t j1 = (size_t)key_tile(k, next) * BN;
         const int vread = STEP == kRowsLag || STEP == kRowsLast ? after(vslot, S::VSLOTS - 1, S::VSLOTS) : vslot;
         rows_tile<D, NW, KG, STEP, NB>(w, ldsK + kslot * TILE, ldsV + vread * TILE, nk, nv,
                                       (const char *)((const u16 *)k.k + j1 * k.k_rs) + koff, (const char *)((const u16 *)k.v + j1 * k.v_rs) + voff,

@@ -12,6 +12,8 @@
 #pragma once
 #include "attend_tile.h"
 
+#include <type_traits>
+
 namespace reform {
 
 struct SeqRows {
@@ -31,6 +33,29 @@ struct SeqKeys {
     const int *parent;       // trees (open = first drafted key): parents of the nodes, null: a chain
     int nodes;
 };
+
+// Prompts with a sliding window: query row i, at key t = i + shift, sees j <= t with j > t - window or j < sinks.  A block goes through
+// two runs of tiles, those of the first keys and those of its rows' windows, counted through: tile number u is tile u below `front`,
+// u + skip from there on.
+struct WindowKeys : SeqKeys {
+    int window, sinks, front, skip;
+};
+
+// Tile number u of a range of keys.
+template <class KEYS>
+__device__ __forceinline__ int key_tile(const KEYS &k, int u)
+{
+    if constexpr (std::is_same<KEYS, WindowKeys>::value) return u < k.front ? u : u + k.skip;
+    else return u;
+}
+
+// Bit x: key `first` + x is seen by the row at key t, of the windows' lower ends alone.
+__device__ __forceinline__ unsigned long long window_seen(const WindowKeys &k, int t, int first)
+{
+    const int gone = t - k.window - first, stay = k.sinks - first;       // keys first + x are behind the window for x <= gone, but stay for x < stay
+    const unsigned long long inside = gone < 0 ? ~0ull : gone >= 63 ? 0ull : ~0ull << (gone + 1);
+    return inside | (stay <= 0 ? 0ull : stay >= 64 ? ~0ull : (1ull << stay) - 1ull);
+}
 
 // Drafted nodes that node `lane` sees: itself and its ancestors, one bit each, one node per lane of a wave.
 // Six doublings: after step m the word holds the 2^m nearest of the line and `up` points 2^m nodes up.
@@ -73,11 +98,12 @@ struct SeqShape {
 // Key tiles [t0, t1) of the sequence (may be empty).  po, pml: null for a final result, else this block's
 // unnormalised sums [rows][D] and (reference maximum in log2 units, sum) [rows].
 // On entry nothing in `smem` may be in use by any wave.
-template <int D, int NB, int NW, bool TREE>
-__device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, float scale, int t0, int t1, float *po,
+template <int D, int NB, int NW, bool TREE, class KEYS>
+__device__ __forceinline__ void seq_segment(const SeqRows &r, const KEYS &s, float scale, int t0, int t1, float *po,
                                             float2 *pml, char *smem)
 {
     using S = SeqShape<D, NB, NW>;
+    constexpr bool WINDOW = std::is_same<KEYS, WindowKeys>::value;
     constexpr int KS = D / 32, DB = D / 16, C8 = S::C8, ROW = S::ROW, TILE = S::TILE, TK = S::TK;
     float *sm = (float *)(smem + S::base_bytes), *sl = sm + NW * S::R;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -87,7 +113,8 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, 
     v4u kreg[S::PIECES], vreg[S::PIECES];
     const uint32_t koff = (uint32_t)((lane / C8) * (int)s.k_rs + lane % C8 * 8) * 2u;
     const uint32_t voff = (uint32_t)((lane / C8) * (int)s.v_rs + lane % C8 * 8) * 2u;
-    auto load = [&](int t) {
+    auto load = [&](int u) {
+        const int t = key_tile(s, u);
         const char *kt = (const char *)((const u16 *)s.k + (size_t)t * TK * s.k_rs);
         const char *vt = (const char *)((const u16 *)s.v + (size_t)t * TK * s.v_rs);
         const int last = s.n - 1 - t * TK;
@@ -145,10 +172,15 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, 
         for (int db = 0; db < DB; ++db) o[nb][db] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     const float c = scale * kLog2e;
+    int behind = -1, stay = 0;                           // windows: some row does not see keys up to here, all rows see those below `stay`
+    if constexpr (WINDOW) {
+        behind = s.shift + min(r.row0 + S::R, r.rows) / r.G - s.window;
+        stay = s.sinks;
+    }
 
     for (; t < t1; t += NW) {
         store();
-        const int j0 = t * TK;
+        const int j0 = key_tile(s, t) * TK;
         if (t + NW < t1) load(t + NW);
         const u16 *sk = mine, *sv = mine + TILE;
         f32x4 x[NB][2];
@@ -162,7 +194,7 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, 
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) x[nb][kb] = mfma16(a, qreg[nb][ks], x[nb][kb]);
             }
-        if (j0 + 31 >= s.open) {
+        if (j0 + 31 >= s.open || (WINDOW && j0 <= behind && j0 + TK > stay)) {
             asm volatile("; mask path" ::: "memory");
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
@@ -180,6 +212,7 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const SeqKeys &s, 
                 } else {
                     const int more = s.shift + at - j0 - first;    // keys behind the lane's first that are seen
                     seen = more >= 31 ? ~0u : more < 0 ? 0u : (2u << more) - 1u;
+                    if constexpr (WINDOW) seen &= (unsigned)window_seen(s, s.shift + at, j0 + first);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e)

@@ -1,39 +1,131 @@
 // Attention over packed prompts whose rows see a sliding window and a few first keys (see reform_window_attend in reform.h).
-#include "attend_simple.h"
+//
+// The blocks of rows of attend_prompt.hip, each of which goes through two runs of key tiles: those of the first keys, and those from
+// the first key that its first row's window shows to the last that its last row sees (WindowKeys).  Only tiles at the
+// ends of the runs are masked.
+//
+//   window_attend<D,NW,KG>         blocks of 32 NW rows, all waves through the same tiles, KG groups of them (attend_rows.h)
+//   window_attend_short<D,NB,NW>   blocks of 16 NB rows whose NW waves divide the tiles (attend_seq.h)
+//   window_attend_f32<DP>          blocks of 16 rows, fp32 (attend_seq_f32.h)
+#include "attend_rows.h"
+#include "attend_seq_f32.h"
+#include "prompt_blocks.h"
+#include "window_plan.h"
 
 namespace reform {
 
-template <class T>
-__global__ __launch_bounds__(64) void window_attend_simple(WindowParams p)
+namespace {
+
+// The block's operands; returns the number of its tiles.
+template <class T, int ROWS, int TK>
+__device__ __forceinline__ int window_operands(const WindowParams &p, const PromptBlock &blk, int kvh, SeqRows &r, WindowKeys &k)
 {
-    const int row = blockIdx.x, head = blockIdx.y, g = head / p.G;
-    const int32_t *cu_k = p.cu_k ? p.cu_k : p.cu_q;
-    int q0 = 0, nq = 0, k0 = 0, nk = 0;
-    for (int s = 0; s < p.n_seq; ++s) {
-        const int a = min(max(p.cu_q[s], 0), p.n_q), b = min(max(p.cu_q[s + 1], 0), p.n_q);
-        if (row < a || row >= b) continue;
-        q0 = a;
-        nq = b - a;
-        k0 = min(max(cu_k[s], 0), p.n_k);
-        nk = max(min(max(cu_k[s + 1], 0), p.n_k) - k0, 0);
-        break;
-    }
-    if (nq == 0) return;
-    const int t = nk - nq + row - q0;                    // the row's own key
-    const int lo = max(t - p.window + 1, 0), sinks = min(p.n_sink, min(lo, t + 1));
-    SimpleRow<T> r;
-    r.begin((const T *)p.q + (size_t)head * p.q_hs + (size_t)row * p.q_rs, p.D);
-    const T *k = (const T *)p.k + (size_t)g * p.k_hs + (size_t)k0 * p.k_rs, *v = (const T *)p.v + (size_t)g * p.v_hs + (size_t)k0 * p.v_rs;
-    for (int j = 0; j < sinks; ++j) r.key(r.logit(k + (size_t)j * p.k_rs, p.D, p.scale), v + (size_t)j * p.v_rs, p.D);
-    for (int j = lo; j <= t; ++j) r.key(r.logit(k + (size_t)j * p.k_rs, p.D, p.scale), v + (size_t)j * p.v_rs, p.D);
-    r.end((T *)p.out + (size_t)head * p.o_hs + (size_t)row * p.o_rs, p.lse ? p.lse + (size_t)head * p.n_q + row : nullptr, p.D);
+    prompt_block_operands<T>(p, blk, kvh, blk.rb * ROWS, r, k);
+    k.window = p.window;
+    k.sinks = p.n_sink;
+    const int lo = max(k.shift + r.row0 / r.G - p.window + 1, 0);        // first key of the first row's window
+    k.front = (min(p.n_sink, lo) + TK - 1) / TK;
+    k.skip = max(lo / TK - k.front, 0);
+    return max(blk.tiles - k.skip, 0);
 }
+
+template <int D, int NW, int KG>
+__global__ __launch_bounds__(NW * KG * 64, 2) void window_attend(WindowParams p)
+{
+    using S = RowsShape<D, NW, KG>;
+    extern __shared__ __attribute__((aligned(16))) u16 lds[];
+    const int kvh = blockIdx.x % p.Hkv;
+    const PromptBlock blk = prompt_block<S::ROWS, S::BN>(p, blockIdx.x / p.Hkv);
+    if (blk.rb < 0) return;
+    SeqRows r;
+    WindowKeys k;
+    const int tiles = window_operands<u16, S::ROWS, S::BN>(p, blk, kvh, r, k);
+    rows_segment<D, NW, KG, false>(r, k, p.by_head, p.scale, 0, tiles, nullptr, nullptr, lds);
+}
+
+template <int D, int NB, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void window_attend_short(WindowParams p)
+{
+    using S = SeqShape<D, NB, NW>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int kvh = blockIdx.x % p.Hkv;
+    const PromptBlock blk = prompt_block<S::R, S::TK>(p, blockIdx.x / p.Hkv);
+    if (blk.rb < 0) return;
+    SeqRows r;
+    WindowKeys k;
+    const int tiles = window_operands<u16, S::R, S::TK>(p, blk, kvh, r, k);
+    seq_segment<D, NB, NW, false>(r, k, p.scale, 0, tiles, nullptr, nullptr, smem);
+}
+
+template <int DP>
+__global__ __launch_bounds__(kF32Waves * 64, 2) void window_attend_f32(WindowParams p)
+{
+    __shared__ F32Sums<DP> sh;
+    const int kvh = blockIdx.x % p.Hkv;
+    const PromptBlock blk = prompt_block<kF32Rows, kF32Keys>(p, blockIdx.x / p.Hkv);
+    if (blk.rb < 0) return;
+    SeqRows r;
+    WindowKeys k;
+    const int tiles = window_operands<float, kF32Rows, kF32Keys>(p, blk, kvh, r, k);
+    f32_segment<DP, false>(r, k, p.D, p.scale, 0, tiles, nullptr, nullptr, sh);
+}
+
+template <int D, int NW, int KG>
+hipError_t launch_long(WindowParams p, hipStream_t st)
+{
+    using S = RowsShape<D, NW, KG>;
+    const hipError_t e = raise_lds<window_attend<D, NW, KG>>(S::lds_bytes);
+    if (e != hipSuccess) return e;
+    p.by_head = NW % p.G == 0;
+    hipLaunchKernelGGL((window_attend<D, NW, KG>), dim3(prompt_grid(p, S::ROWS)), dim3(NW * KG * 64), S::lds_bytes, st, p);
+    return hipGetLastError();
+}
+
+template <int D, int NB, int NW>
+hipError_t launch_short(const WindowParams &p, hipStream_t st)
+{
+    using S = SeqShape<D, NB, NW>;
+    const hipError_t e = raise_lds<window_attend_short<D, NB, NW>>(S::lds_bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((window_attend_short<D, NB, NW>), dim3(prompt_grid(p, S::R)), dim3(NW * 64), S::lds_bytes, st, p);
+    return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_bf16(const WindowParams &p, hipStream_t st)
+{
+#ifdef FORCE_FORM
+    const int form = FORCE_FORM;
+#else
+    const int form = window_choose(D, p.G, p.Hkv, p.n_seq, p.n_q, p.n_k, p.window, p.n_sink, p.units);
+#endif
+    const PromptForm &f = prompt_forms(D)[form];
+    if (f.rows == 32) return launch_short<D, 2, 4>(p, st);
+    if (f.rows == 16) return launch_short<D, 1, 8>(p, st);
+    if constexpr (D == 64) {
+        if (f.rows == 256) return launch_long<D, 8, 1>(p, st);
+    } else {
+        if (f.groups == 2) return launch_long<D, 4, 2>(p, st);
+    }
+    return launch_long<D, 4, 1>(p, st);
+}
+
+template <int DP>
+hipError_t launch_f32(const WindowParams &p, hipStream_t st)
+{
+    hipLaunchKernelGGL((window_attend_f32<DP>), dim3(prompt_grid(p, kF32Rows)), dim3(kF32Waves * 64), 0, st, p);
+    return hipGetLastError();
+}
+
+}  // namespace
 
 hipError_t window_attend_launch(const WindowParams &p, bool bf16, hipStream_t st)
 {
-    if (bf16) hipLaunchKernelGGL((window_attend_simple<u16>), dim3(p.n_q, p.Hq), dim3(64), 0, st, p);
-    else hipLaunchKernelGGL((window_attend_simple<float>), dim3(p.n_q, p.Hq), dim3(64), 0, st, p);
-    return hipGetLastError();
+    if (bf16) return p.D == 64 ? launch_bf16<64>(p, st) : launch_bf16<128>(p, st);
+    if (p.D <= 32) return launch_f32<32>(p, st);
+    if (p.D <= 64) return launch_f32<64>(p, st);
+    if (p.D <= 128) return launch_f32<128>(p, st);
+    return launch_f32<256>(p, st);
 }
 
 }  // namespace reform
