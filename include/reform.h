@@ -615,7 +615,7 @@ reform_status reform_window_attend(const reform_window_desc *desc, const void *q
  * same arguments; results depend on the batch and on max_len by rounding only.  Keys and values that are not finite stay
  * within their sequence and KV head.  Rows behind L are never looked at.
  * Supported: types and head_dim as reform_prompt_attend; any page_len >= 1; n_pages * page_len below 2^31; max_len at most
- * max_pages * page_len and 2^31 - 512; row stride of k and v below 2^24; n_seq * n_q_heads at most 2^22; with B = ceil(n_q_heads /
+ * max_pages * page_len and 2^31 - 65536; row stride of k and v below 2^24; n_seq * n_q_heads at most 2^22; with B = ceil(n_q_heads /
  * n_kv_heads / 16), n_seq * n_kv_heads * B * (max_len / 16 + 64) below 2^31.  n_seq = 0 does nothing.
  * The workspace takes partial results of caches that are shared out over workgroups, and the logits of all keys if the score is asked
  * for (4 bytes a key that can be seen and query head); the query wants to know whether it is: want_score.  Without it, or with less than the
@@ -658,7 +658,7 @@ reform_status reform_paged_attend(const reform_paged_desc *desc, const void *q, 
  *     kept_idx [n_seq][n_kv_heads][budget] int32 out, contiguous, the first new_len entries of a head; may be NULL
  *     new_len  [n_seq] int32 out, may be NULL; must not be cache_len itself
  * Supported: head_dim * sizeof(element) a multiple of 16 up to 4096; strides of k and v multiples of 16 bytes; page_len, n_pages,
- * max_pages, max_len as in reform_paged_attend; budget at least 1; n_seq * n_kv_heads * (row bytes / 32 + 4) below 2^23.  n_seq = 0 does
+ * max_pages, max_len as in reform_paged_attend; budget at least 1; n_seq * n_kv_heads * (row bytes / 64 + 4) below 2^22.  n_seq = 0 does
  * nothing.
  */
 typedef struct {

@@ -790,7 +790,7 @@ def _pool_fields(k, v, page_table, score, max_len, n_seq, Hkv):
             raise ValueError("score: [sequences, KV heads, keys] fp32, a head's keys contiguous")
         most = min(most, rows[2])
     if max_len is None:
-        max_len = min(most, (1 << 31) - 512)
+        max_len = min(most, (1 << 31) - 65536)
     elif score is not None and max_len > rows[2]:
         raise ValueError("score: max_len keys at least")
     return (shape[3], shape[2], shape[0], ps[1], max_len), ks[:3], (page_table.stride(0), ss[0], ss[1])

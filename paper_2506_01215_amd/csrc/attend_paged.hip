@@ -34,6 +34,10 @@ __device__ __forceinline__ long lane_value(long x, int lane)
     return (long)(((unsigned long)hi << 32) | lo);
 }
 
+// K and V are read once: past the caches' usual order of replacement (one token over 131072 keys, 32/8 heads of 128: 96 us without
+// the hint, 85 with it; 32 caches of up to 8192 139, 123).
+__device__ __forceinline__ v4u stream_load(const void *p) { return __builtin_nontemporal_load((const v4u *)p); }
+
 // Virtual tiles [t0, t1) of sequence b's KV head for the heads from row0 on.  po, pml: as in seq_segment.
 template <int D, int NW, bool HALVES>
 __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int kvh, int len, int row0, int t0, int t1, float *po, float2 *pml, char *smem)
@@ -79,8 +83,8 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
                 for (int i = 0; i < S::PIECES; ++i) {
                     const long half = i < S::PIECES / 2 ? a : b1;
                     const uint32_t off = lane_off + (uint32_t)((i % (S::PIECES / 2)) * STEP * (int)p.pool.row_stride) * 2u;
-                    kreg[i] = *(const v4u *)((const char *)(K + half) + off);
-                    vreg[i] = *(const v4u *)((const char *)(V + half) + off);
+                    kreg[i] = stream_load((const char *)(K + half) + off);
+                    vreg[i] = stream_load((const char *)(V + half) + off);
                 }
             } else {
 #pragma unroll
@@ -89,8 +93,8 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
                     const uint32_t off = lane_off + (uint32_t)((i % (S::PIECES / 2)) * STEP * (int)p.pool.row_stride) * 2u;
                     kreg[i] = vreg[i] = (v4u){0u, 0u, 0u, 0u};           // weights of 0 meet zeros, whatever lies there
                     if ((mask >> (lane / C8 + i * STEP)) & 1u) {
-                        kreg[i] = *(const v4u *)((const char *)(K + half) + off);
-                        vreg[i] = *(const v4u *)((const char *)(V + half) + off);
+                        kreg[i] = stream_load((const char *)(K + half) + off);
+                        vreg[i] = stream_load((const char *)(V + half) + off);
                     }
                 }
             }
@@ -102,8 +106,8 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
                 const long at = ((long)__shfl((int)(ahead >> 32), row) << 32) | (unsigned)__shfl((int)ahead, row);
                 kreg[i] = vreg[i] = (v4u){0u, 0u, 0u, 0u};
                 if (at >= 0) {
-                    kreg[i] = *(const v4u *)(K + at + lane % C8 * 8);
-                    vreg[i] = *(const v4u *)(V + at + lane % C8 * 8);
+                    kreg[i] = stream_load(K + at + lane % C8 * 8);
+                    vreg[i] = stream_load(V + at + lane % C8 * 8);
                 }
             }
             look(u + NW);
@@ -249,7 +253,8 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
     }
     if (paged_scores_alone(p)) {
         __syncthreads();                                 // rows and logits are there
-        paged_score<TK>(p, b, kvh, len, t0, t1, 0, rows, [&](int r) { return row_ml[r]; });
+        int counter = 0;
+        paged_score<TK>(p, b, kvh, len, t0, t1, counter, wave, NW, [&](int) { return row_ml[min(lane, rows - 1)]; });
     }
 }
 

@@ -222,14 +222,17 @@ struct PagedParams {
 struct PagedEvictParams {
     void *k, *v;
     float *score;
-    int32_t *pos, *kept, *new_len;           // nullable
+    int32_t *pos, *new_len;  // nullable
+    int32_t *kept;           // [n_seq][Hkv][budget]; nullable where no sequence can outgrow its budget
     const int32_t *cache_len;
     PagedPool pool;
     int n_seq, Hkv, max_len, budget, n_sink, n_recent;
     int row_bytes, elt;      // of a row of k and v, of an element
+    int units;               // compute units
     long score_ss, score_hs;
-    int32_t *src;            // [n_seq][Hkv][budget]: pool rows (page * page_len + row) that the kept keys come from, -1: none
     int32_t *first;          // [n_seq][Hkv]: first row that moves
+    int segs, seg_rows, stage_rows;          // segments that an item's rows are moved in, ranks of one, staged rows of one at most
+    char *stage;             // [n_seq][Hkv][k, v][segs - 1][stage_rows] rows
 };
 
 struct EmbedParams {

@@ -1,13 +1,20 @@
-// Caches in pages go back to their budget (see reform_paged_evict in reform.h), in two launches.
+// Caches in pages go back to their budget (see reform_paged_evict in reform.h).
 //
 //   paged_select   a workgroup has one sequence's KV head: finds the budget-th score between the first and the last keys
-//                  that are always kept, and lists the kept keys and the pool rows that hold them
+//                  that are always kept, and lists the kept keys
 //   paged_move     row r becomes row kept[r]: a workgroup has one head's rows, of K or of V and of those a slice of
-//                  64 bytes each, and goes through them in ascending order
+//                  128 bytes each, and goes through them in ascending order
 //
 // In place without flags: rank r comes from row kept[r] >= r, so what a chunk of ranks [r0, r1) overwrites is read by
 // ranks below r1 only.  A workgroup that has loaded all of a chunk may store it, and the next chunk's rows can be on their way
-// meanwhile.  Slices do not touch each other's bytes.
+// meanwhile.  Slices do not touch each other's bytes.  Few items of many rows are cut into segments of ranks that move at once; the rows
+// that a segment needs of the next one's are set aside first (paged_stage, a launch between the two).
+//
+// Bound: reading and writing the rows that move.  Cold caches, all rows moving: 112 heads from 4352 to 4096 rows of 128 elements bf16
+// 440 MB in 102 us, 4.3 TB/s (a large copy: 4.9), and 10 for the selection; 8 heads from 33024 to 32768 266 MB in 66 us, 28 for the selection, which
+// has one compute unit for each head.  Rows pass the caches' usual order of replacement (114 -> 103 us).  Chunks of 1024 threads x 4 x 16 bytes
+// against 512 x 8: 95 against 103; twice as deep 150; with the next chunk's loads before this one's stores 109; 64 bytes of a row to a
+// workgroup 142, 256 more than twice as slow for few items.
 #include "common.h"
 
 #include <climits>
@@ -16,188 +23,226 @@ namespace reform {
 
 namespace {
 
-constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kSelBins = 2048;
-constexpr int kSelCached = 36864;            // candidates that stay in LDS (144 of the 160 KB)
-constexpr int kMoveThreads = 512, kMoveSlice = 64, kMoveDeep = 8;
+constexpr int kSelBins = 2048;
+constexpr int kMoveThreads = 1024, kMoveLanes = 8, kMoveDeep = 4;        // a chunk: 512 rows of 128 bytes, 64 bytes a thread
+constexpr int kStageThreads = 512;
 
 __device__ __forceinline__ int clamped_len(const PagedEvictParams &p, int b) { return min(max(p.cache_len[b], 0), p.max_len); }
 
-// The keys are compared as ordered integers (ordered_key).  Each pass counts the candidates inside [lo, hi] in 2048 bins of
-// equal width and goes on with the bin that holds the need-th largest, so three passes decide 32 bits, two where the
-// scores spread over less than 22.
-__global__ __launch_bounds__(kSelThreads) void paged_select(PagedEvictParams p, int cached)
+// The scores are compared as ordered integers (ordered_key).  Each pass counts the candidates inside [lo, hi] in 2048 bins of equal
+// width and goes on with the bin that holds the need-th largest, so three passes decide 32 bits, two where the scores spread
+// over less than 22.
+//
+// A wave has a run of candidates, K times 64 of which stay in its lanes' registers (K = 0: every pass reads them again, eight loads
+// on their way at once), so that a pass is its additions to LDS and the workgroup's barriers.
+template <int NT, int K>
+__global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
 {
-    extern __shared__ uint32_t row[];        // [cached] candidates as ordered keys
+    constexpr int NW = NT / 64, PER = kSelBins / NT;     // waves; bins of a thread
     __shared__ int bins[kSelBins];
-    __shared__ int wave_sum_[kSelWaves], wave_tie[kSelWaves], wave_out[kSelWaves];
-    __shared__ uint32_t sh_lo, sh_hi;
+    __shared__ int sh_a[NW], sh_b[NW], sh_first[NW];
+    __shared__ uint32_t sh_lo[NW], sh_hi[NW], sh_from, sh_to;
     __shared__ int sh_need, sh_all;
     const int item = blockIdx.x, b = item / p.Hkv, g = item - b * p.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = clamped_len(p, b);
     if (p.new_len && g == 0 && tid == 0) p.new_len[b] = min(n, p.budget);
-    int32_t *kept = p.kept ? p.kept + (size_t)item * p.budget : nullptr;
+    int32_t *kept = p.kept ? p.kept + (size_t)item * p.budget : nullptr;      // null only where no sequence can outgrow its budget
     if (n <= p.budget) {
-        for (int r = tid; kept && r < n; r += kSelThreads) kept[r] = r;
+        for (int r = tid; kept && r < n; r += NT) kept[r] = r;
         return;
     }
-    int32_t *src = p.src + (size_t)item * p.budget;
-    const int32_t *table = p.pool.table + (size_t)b * p.pool.table_stride;
-    auto list = [&](int r, int j) {          // rank r is key j
-        const unsigned page = pool_page(p.pool, (unsigned)j), id = (unsigned)table[page];
-        if (kept) kept[r] = j;
-        src[r] = id < p.pool.n_pages ? (int)(id * p.pool.page_len + ((unsigned)j - page * p.pool.page_len)) : -1;
-    };
     const float *score = p.score + (size_t)b * p.score_ss + (size_t)g * p.score_hs + p.n_sink;
     const int m = n - p.n_sink - p.n_recent, want = p.budget - p.n_sink - p.n_recent;      // candidates, and how many stay
-    const bool in_lds = m <= cached;
-    auto key = [&](int i) { return in_lds ? row[i] : ordered_key(score[i]); };
-    if (tid == 0) { sh_lo = ~0u; sh_hi = 0u; sh_need = want; sh_all = 0; }
-    __syncthreads();
+    const int each = ((m + NW - 1) / NW + 63) / 64 * 64, i0 = min(wave * each, m), i1 = min(i0 + each, m);
+    uint32_t mine[K > 0 ? K : 1];
+    {
+        float s[K > 0 ? K : 1];                          // all on their way before the first is looked at
+#pragma unroll
+        for (int x = 0; x < K; ++x) s[x] = score[min(i0 + 64 * x + lane, m - 1)];
+#pragma unroll
+        for (int x = 0; x < K; ++x) mine[x] = ordered_key(s[x]);
+    }
+    // f(first candidate of 64, the lane's key): the wave's candidates in order
+    auto keys = [&](auto f) {
+        if constexpr (K > 0) {
+#pragma unroll
+            for (int x = 0; x < K; ++x)
+                if (i0 + 64 * x < i1) f(i0 + 64 * x, mine[x]);
+        } else {
+            for (int i = i0; i < i1; i += 512) {
+                float s[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) s[x] = score[min(i + 64 * x + lane, m - 1)];
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    if (i + 64 * x < i1) f(i + 64 * x, ordered_key(s[x]));
+            }
+        }
+    };
     uint32_t lo = ~0u, hi = 0u;
-    for (int i = tid; i < m; i += kSelThreads) {
-        const uint32_t u = ordered_key(score[i]);
-        if (in_lds) row[i] = u;
+    keys([&](int, uint32_t u) {                          // others' keys among them do no harm
         lo = min(lo, u);
         hi = max(hi, u);
-    }
+    });
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
         lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
         hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
     }
-    if (lane == 0) { atomicMin(&sh_lo, lo); atomicMax(&sh_hi, hi); }
+    if (lane == 0) { sh_lo[wave] = lo; sh_hi[wave] = hi; }
+    for (int i = tid; i < kSelBins; i += NT) bins[i] = 0;
     __syncthreads();
-    lo = sh_lo;
-    hi = sh_hi;
-    int need = want;                         // of the candidates inside [lo, hi]; all above hi stay
-    bool all = false;                        // all inside [lo, hi] stay
-    while (want > 0 && !all && lo < hi) {
+    for (int w = 0; w < NW; ++w) {
+        lo = min(lo, sh_lo[w]);
+        hi = max(hi, sh_hi[w]);
+    }
+    int need = want;                                     // of the candidates inside [lo, hi]; all above hi stay
+    bool all = false;                                    // all inside [lo, hi] stay
+    while (want > 0 && !all && lo < hi) {                // the bins are 0
         const uint32_t range = hi - lo;
         const int shift = max(21 - __clz((int)range), 0);                    // range >> shift < 2048
-        for (int i = tid; i < kSelBins; i += kSelThreads) bins[i] = 0;
+        keys([&](int i, uint32_t u) {
+            const bool is = i + lane < i1 && u - lo <= range;
+            // scores that many keys share (0 above all) would queue for one bin: the lanes of the first one's bin add up first
+            const int bin = is ? (int)((u - lo) >> shift) : -1;
+            const unsigned long long any = __builtin_amdgcn_ballot_w64(is);
+            if (any == 0ull) return;
+            const int leader = __builtin_ctzll(any), common = __builtin_amdgcn_readlane(bin, leader);
+            const unsigned long long same = __builtin_amdgcn_ballot_w64(bin == common);
+            if (lane == leader || (is && bin != common)) atomicAdd(&bins[bin], lane == leader ? (int)__builtin_popcountll(same) : 1);
+        });
         __syncthreads();
-        for (int i = tid; i < m; i += kSelThreads) {
-            const uint32_t u = key(i) - lo;
-            if (u <= range) atomicAdd(&bins[u >> shift], 1);
+        // bins from the largest down, PER to a thread
+        int count[PER], own = 0;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+            count[x] = bins[kSelBins - 1 - (PER * tid + x)];
+            bins[kSelBins - 1 - (PER * tid + x)] = 0;
+            own += count[x];
         }
-        __syncthreads();
-        // bins from the largest down, two to a thread
-        const int hi_bin = bins[kSelBins - 1 - 2 * tid], lo_bin = bins[kSelBins - 2 - 2 * tid], own = hi_bin + lo_bin;
         const int incl = wave_incl_scan(own);
-        if (lane == 63) wave_sum_[wave] = incl;
+        if (lane == 63) sh_a[wave] = incl;
         __syncthreads();
         int above = incl - own;
-        for (int w = 0; w < wave; ++w) above += wave_sum_[w];
+        for (int w = 0; w < wave; ++w) above += sh_a[w];
         if (above < need && need <= above + own) {
-            const bool first = need <= above + hi_bin;
-            const uint32_t bin = kSelBins - (first ? 1 : 2) - 2 * tid;
-            const int over = first ? above : above + hi_bin;
-            const uint32_t from = lo + (bin << shift), wide = (1u << shift) - 1u;
-            sh_lo = from;
-            sh_hi = hi - from > wide ? from + wide : hi;
-            sh_need = need - over;
-            sh_all = need - over == (first ? hi_bin : lo_bin);
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+                if (above < need && need <= above + count[x]) {
+                    const uint32_t from = lo + ((uint32_t)(kSelBins - 1 - (PER * tid + x)) << shift), wide = (1u << shift) - 1u;
+                    sh_from = from;
+                    sh_to = hi - from > wide ? from + wide : hi;
+                    sh_need = need - above;
+                    sh_all = need - above == count[x];
+                }
+                above += count[x];
+            }
         }
         __syncthreads();
-        lo = sh_lo;
-        hi = sh_hi;
+        lo = sh_from;
+        hi = sh_to;
         need = sh_need;
         all = sh_all != 0;
     }
     // stay: above hi; inside [lo, hi] (one value, or all of them stay) the first `need`
     if (want == 0) { lo = 1u; hi = ~0u; need = 0; }
-    const int each = ((m + kSelWaves - 1) / kSelWaves + 63) / 64 * 64, i0 = min(wave * each, m), i1 = min(i0 + each, m);
     int stay = 0, tie = 0;
-    for (int i = i0 + lane; i < i1; i += 64) {
-        const uint32_t u = key(i);
-        stay += u > hi;
-        tie += u >= lo && u <= hi;
-    }
+    keys([&](int i, uint32_t u) {
+        stay += i + lane < i1 && u > hi;
+        tie += i + lane < i1 && u >= lo && u <= hi;
+    });
     stay = __builtin_amdgcn_readlane(wave_incl_scan(stay), 63);
     tie = __builtin_amdgcn_readlane(wave_incl_scan(tie), 63);
-    if (lane == 0) { wave_sum_[wave] = stay; wave_tie[wave] = tie; }
+    __syncthreads();                                     // sh_a has been read
+    if (lane == 0) { sh_a[wave] = stay; sh_b[wave] = tie; }
     __syncthreads();
     int rank = p.n_sink, ties = 0;
     for (int w = 0; w < wave; ++w) {
-        rank += wave_sum_[w];
-        ties += wave_tie[w];
+        rank += sh_a[w];
+        ties += sh_b[w];
     }
     rank += min(ties, need);
-    int first = INT_MAX;                     // first key that goes
-    for (int i = i0; i < i1; i += 64) {
-        const bool is = i + lane < i1;
-        const uint32_t u = is ? key(i + lane) : 0u;
-        const bool over = is && u > hi, same = is && u >= lo && u <= hi;
+    int first = INT_MAX;                                 // first key that goes
+    keys([&](int i, uint32_t u) {
+        const bool is = i + lane < i1, over = is && u > hi, same = is && u >= lo && u <= hi;
         const unsigned long long below = (1ull << lane) - 1ull, tied = __builtin_amdgcn_ballot_w64(same);
         const bool stays = over || (same && ties + __builtin_popcountll(tied & below) < need);
         const unsigned long long mask = __builtin_amdgcn_ballot_w64(stays), gone = __builtin_amdgcn_ballot_w64(is && !stays);
-        if (stays) list(rank + __builtin_popcountll(mask & below), p.n_sink + i + lane);
+        if (stays) kept[rank + __builtin_popcountll(mask & below)] = p.n_sink + i + lane;
         if (gone && first == INT_MAX) first = p.n_sink + i + __builtin_ctzll(gone);
         rank += __builtin_popcountll(mask);
         ties += __builtin_popcountll(tied);
-    }
-    for (int r = tid; r < p.n_sink; r += kSelThreads) list(r, r);
-    for (int r = tid; r < p.n_recent; r += kSelThreads) list(p.budget - p.n_recent + r, n - p.n_recent + r);
-    if (lane == 0) wave_out[wave] = first;
+    });
+    for (int r = tid; r < p.n_sink; r += NT) kept[r] = r;
+    for (int r = tid; r < p.n_recent; r += NT) kept[p.budget - p.n_recent + r] = n - p.n_recent + r;
+    if (lane == 0) sh_first[wave] = first;
     __syncthreads();
     if (tid == 0) {
-        for (int w = 0; w < kSelWaves; ++w) first = min(first, wave_out[w]);
+        for (int w = 0; w < NW; ++w) first = min(first, sh_first[w]);
         p.first[item] = first;
     }
 }
 
-// Rows [first, budget) of one head, LANES threads of 16 bytes to a row.
-template <int LANES>
-__device__ __forceinline__ void move_rows(const PagedEvictParams &p, int item, int first, char *base, const int32_t *table, int col)
+// Ranks [r0, r1) of one segment's rows, LANES threads of 16 bytes to a row.  Three things of a row follow from each other: which key it
+// comes from, where that key's row is, and what is in it.  They are fetched two chunks, one chunk and no chunk ahead.  Rows from
+// key `bound` on are the next segment's to overwrite: they come from `stage`, where rank bound - 1 - x has row x.
+__device__ __forceinline__ void move_rows(const PagedEvictParams &p, const int32_t *kept, int r0, int r1, int bound, char *base, const char *stage,
+                                          const int32_t *table, int col)
 {
-    constexpr int ROWS = kMoveThreads / LANES;
-    const int tr = threadIdx.x / LANES, tc = threadIdx.x % LANES;
-    const int32_t *src = p.src + (size_t)item * p.budget;
-    const bool in = col + tc * 16 < p.row_bytes;
+    constexpr int ROWS = kMoveThreads / kMoveLanes, CHUNK = kMoveDeep * ROWS;
+    const int tr = threadIdx.x / kMoveLanes, tc = threadIdx.x % kMoveLanes;
     char *const at = base + col + tc * 16;
-    auto address = [&](unsigned x) {         // of a pool row
-        const unsigned page = pool_page(p.pool, x);
-        return at + ((long)page * p.pool.page_stride + (long)(x - page * p.pool.page_len) * p.pool.row_stride) * p.elt;
-    };
-    int from[kMoveDeep];
+    const char *const staged = stage + col + tc * 16;
+    const int end = col + tc * 16 < p.row_bytes ? r1 : 0;                // lanes behind a row's last bytes move nothing
+    int key[kMoveDeep];
+    const char *from[kMoveDeep];
+    char *to[kMoveDeep];
     v4u data[kMoveDeep];
-    auto look = [&](int r0) {
+    auto place = [&](int j) {
+        const long off = pool_row(p.pool, table, j);
+        return off >= 0 ? at + off * p.elt : nullptr;
+    };
+    auto keys = [&](int r) {
+#pragma unroll
+        for (int i = 0; i < kMoveDeep; ++i) key[i] = r + i * ROWS + tr < end ? kept[r + i * ROWS + tr] : -1;
+    };
+    auto places = [&](int r) {
 #pragma unroll
         for (int i = 0; i < kMoveDeep; ++i) {
-            const int r = r0 + i * ROWS + tr;
-            from[i] = in && r < p.budget ? src[r] : -1;
+            from[i] = nullptr;
+            if (key[i] >= bound) from[i] = pool_row(p.pool, table, key[i]) >= 0 ? staged + (size_t)(bound - 1 - (r + i * ROWS + tr)) * p.row_bytes : nullptr;
+            else if (key[i] >= 0) from[i] = place(key[i]);
         }
     };
-    auto load = [&] {
+    auto fetch = [&](int r) {
 #pragma unroll
-        for (int i = 0; i < kMoveDeep; ++i)
-            if (from[i] >= 0) data[i] = *(const v4u *)address((unsigned)from[i]);
+        for (int i = 0; i < kMoveDeep; ++i) {
+            to[i] = from[i] ? place(r + i * ROWS + tr) : nullptr;
+            if (from[i]) data[i] = __builtin_nontemporal_load((const v4u *)from[i]);
+        }
     };
-    look(first);
-    for (int r0 = first; r0 < p.budget; r0 += kMoveDeep * ROWS) {
-        load();
+    keys(r0);
+    places(r0);
+    keys(r0 + CHUNK);
+    fetch(r0);
+    places(r0 + CHUNK);
+    keys(r0 + 2 * CHUNK);
+    for (; r0 < r1; r0 += CHUNK) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // what this wave moves has left its place ...
         __syncthreads();                                 // ... and what the others move
-        char *to[kMoveDeep];
-#pragma unroll
-        for (int i = 0; i < kMoveDeep; ++i) {
-            const int r = r0 + i * ROWS + tr;
-            const long off = from[i] >= 0 ? pool_row(p.pool, table, r) : -1l;
-            to[i] = off >= 0 ? at + off * p.elt : nullptr;
-        }
-        look(r0 + kMoveDeep * ROWS);
 #pragma unroll
         for (int i = 0; i < kMoveDeep; ++i)
-            if (to[i]) *(v4u *)to[i] = data[i];
+            if (to[i]) __builtin_nontemporal_store(data[i], (v4u *)to[i]);
+        fetch(r0 + CHUNK);                               // none of its rows lies where this chunk goes
+        places(r0 + 2 * CHUNK);
+        keys(r0 + 3 * CHUNK);
     }
 }
 
 // The same for four bytes a row in one piece of memory (score, pos).
-__device__ __forceinline__ void move_words(const PagedEvictParams &p, int item, int first, uint32_t *base)
+__device__ __forceinline__ void move_words(const PagedEvictParams &p, const int32_t *kept, int first, int n, uint32_t *base)
 {
-    const int b = item / p.Hkv, n = clamped_len(p, b);
-    const int32_t *kept = p.kept + (size_t)item * p.budget;
     uint32_t data[kMoveDeep];
     for (int r0 = first; r0 < p.budget; r0 += kMoveDeep * kMoveThreads) {
 #pragma unroll
@@ -215,35 +260,103 @@ __device__ __forceinline__ void move_words(const PagedEvictParams &p, int item, 
     }
 }
 
-template <int LANES>
+// An item's segments, one where more keys go than a segment's staged rows can hold.
+__device__ __forceinline__ int segments(const PagedEvictParams &p, int n) { return n - p.budget <= p.stage_rows ? p.segs : 1; }
+
+__device__ __forceinline__ char *stage_of(const PagedEvictParams &p, int item, int what, int seg)
+{
+    return p.stage + (((size_t)item * 2 + what) * (p.segs - 1) + seg) * p.stage_rows * p.row_bytes;
+}
+
+// Before segments move at once: rows that a segment's last ranks need and the next segment overwrites, 16 bytes a thread.
+__global__ __launch_bounds__(kStageThreads) void paged_stage(PagedEvictParams p, int groups)
+{
+    const int bounds = p.segs - 1, item = blockIdx.x / (2 * bounds * groups), rest = blockIdx.x - item * 2 * bounds * groups;
+    const int what = rest / (bounds * groups), seg = (rest - what * bounds * groups) / groups, group = rest % groups;
+    const int b = item / p.Hkv, g = item - b * p.Hkv, n = clamped_len(p, b);
+    if (n <= p.budget || segments(p, n) == 1) return;
+    const int pieces = p.row_bytes / 16, i = group * kStageThreads + threadIdx.x;
+    const int bound = (seg + 1) * p.seg_rows, x = i / pieces, c = (i - x * pieces) * 16, r = bound - 1 - x;
+    if (x >= min(p.stage_rows, n - p.budget) || r >= p.budget) return;   // no more rows than go come from behind the bound
+    const int j = p.kept[(size_t)item * p.budget + r];
+    if (j < bound) return;
+    const long off = pool_row(p.pool, p.pool.table + (size_t)b * p.pool.table_stride, j);
+    const char *base = (const char *)(what ? p.v : p.k) + (size_t)g * p.pool.head_stride * p.elt;
+    if (off >= 0) *(v4u *)(stage_of(p, item, what, seg) + (size_t)x * p.row_bytes + c) = __builtin_nontemporal_load((const v4u *)(base + off * p.elt + c));
+}
+
+// XCDs take workgroups in turn: those of one item are eight apart, so that a row's slices meet in one L2.
+__device__ __forceinline__ int item_of(int block, int items, int parts, int &part)
+{
+    const int each = items >> 3, even = 8 * each * parts;                // items of an XCD
+    const int j = block < even ? block >> 3 : block - even, i = j / parts;
+    part = j - i * parts;
+    return block < even ? (block & 7) * each + i : 8 * each + i;
+}
+
 __global__ __launch_bounds__(kMoveThreads) void paged_move(PagedEvictParams p, int slices, int parts)
 {
-    const int item = blockIdx.x / parts, part = blockIdx.x - item * parts;
-    const int b = item / p.Hkv, g = item - b * p.Hkv;
-    if (clamped_len(p, b) <= p.budget) return;
+    int part;
+    const int item = item_of(blockIdx.x, p.n_seq * p.Hkv, parts, part);
+    const int b = item / p.Hkv, g = item - b * p.Hkv, n = clamped_len(p, b);
+    if (n <= p.budget) return;
     const int first = p.first[item];
-    if (part < 2 * slices) {
-        char *base = (char *)(part < slices ? p.k : p.v) + (size_t)g * p.pool.head_stride * p.elt;
-        move_rows<LANES>(p, item, first, base, p.pool.table + (size_t)b * p.pool.table_stride, part % slices * LANES * 16);
-    } else {
+    const int32_t *kept = p.kept + (size_t)item * p.budget;
+    if (part >= 2 * slices * p.segs) {
         const size_t at = (size_t)b * p.score_ss + (size_t)g * p.score_hs;
-        move_words(p, item, first, part == 2 * slices ? (uint32_t *)p.score + at : (uint32_t *)p.pos + at);
+        move_words(p, kept, first, n, part == 2 * slices * p.segs ? (uint32_t *)p.score + at : (uint32_t *)p.pos + at);
+        return;
     }
+    const int seg = part / (2 * slices), rest = part - seg * 2 * slices, what = rest / slices, segs = segments(p, n);
+    const bool last = segs == 1 || seg == segs - 1;
+    const int r0 = max(first, seg * p.seg_rows), r1 = last ? p.budget : (seg + 1) * p.seg_rows;
+    if (seg >= segs || r0 >= r1) return;
+    move_rows(p, kept, r0, r1, last ? INT_MAX : r1, (char *)(what ? p.v : p.k) + (size_t)g * p.pool.head_stride * p.elt,
+              last ? nullptr : stage_of(p, item, what, seg), p.pool.table + (size_t)b * p.pool.table_stride, rest % slices * kMoveLanes * 16);
 }
 
 }  // namespace
 
+// How many segments an item's rows are moved in: as many as there are compute units for.  A segment's chunks follow each other, some
+// 4 us each whatever else runs, so one workgroup for few items of many rows leaves the chip idle: 8 heads of 32768 rows, 128 wide,
+// whole 323 us, in 8 segments 66, in 16 69 (and 5 to 10 for the staging); 112 heads of 4096 rows, of which two would make the best of
+// the chip, 102 whole and 106 in two.  Segments of 1024 rows at least, and where it is known how many keys may go, so large
+// that a quarter of their rows has room for that many; an item that more keys leave moves in one.
+void paged_evict_plan(PagedEvictParams &p)
+{
+    const double items = (double)p.n_seq * p.Hkv;
+    const int slices = (p.row_bytes + kMoveLanes * 16 - 1) / (kMoveLanes * 16), most_gone = p.max_len - p.budget;
+    p.segs = 1;
+    if (most_gone > 0) {
+        const double want = p.units / (items * 2.0 * slices), fit = p.budget / (4.0 * most_gone);
+        int segs = want < 32.0 ? (int)want : 32;
+        if (fit >= 2.0 && segs > fit) segs = (int)fit;
+        if (segs > p.budget / 1024) segs = p.budget / 1024;
+        if (segs > 1 && items * p.budget * p.row_bytes / 32.0 < 2147483648.0) p.segs = segs;      // threads of the staging
+    }
+    p.seg_rows = (p.budget + p.segs - 1) / p.segs;
+    p.stage_rows = p.segs == 1 ? 0 : most_gone < p.seg_rows / 4 ? most_gone : p.seg_rows / 4;
+}
+
+size_t paged_evict_stage_bytes(const PagedEvictParams &p)
+{
+    return (size_t)p.n_seq * p.Hkv * 2 * (p.segs - 1) * p.stage_rows * p.row_bytes;
+}
+
 hipError_t paged_evict_launch(const PagedEvictParams &p, hipStream_t st)
 {
-    const int items = p.n_seq * p.Hkv;
-    const int most = p.max_len - p.n_sink - p.n_recent, cached = most < kSelCached ? (most > 0 ? most : 0) : kSelCached;
-    const hipError_t e = raise_lds<paged_select>(4 * kSelCached);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(paged_select, dim3(items), dim3(kSelThreads), 4 * (size_t)cached, st, p, cached);
+    const int items = p.n_seq * p.Hkv, most = p.max_len - p.n_sink - p.n_recent;
+    if (most <= 2048) hipLaunchKernelGGL((paged_select<256, 8>), dim3(items), dim3(256), 0, st, p);
+    else if (most <= 8192) hipLaunchKernelGGL((paged_select<1024, 8>), dim3(items), dim3(1024), 0, st, p);
+    else if (most <= 32768) hipLaunchKernelGGL((paged_select<1024, 32>), dim3(items), dim3(1024), 0, st, p);
+    else hipLaunchKernelGGL((paged_select<1024, 0>), dim3(items), dim3(1024), 0, st, p);
     if (p.max_len <= p.budget) return hipGetLastError();
-    constexpr int LANES = kMoveSlice / 16;
-    const int slices = (p.row_bytes + kMoveSlice - 1) / kMoveSlice, parts = 2 * slices + (p.pos ? 2 : 1);
-    hipLaunchKernelGGL((paged_move<LANES>), dim3((unsigned)items * parts), dim3(kMoveThreads), 0, st, p, slices, parts);
+    const int slices = (p.row_bytes + kMoveLanes * 16 - 1) / (kMoveLanes * 16), parts = 2 * slices * p.segs + (p.pos ? 2 : 1);
+    if (p.segs > 1) {
+        const int groups = (p.stage_rows * (p.row_bytes / 16) + kStageThreads - 1) / kStageThreads;
+        hipLaunchKernelGGL(paged_stage, dim3(items * 2 * (p.segs - 1) * groups), dim3(kStageThreads), 0, st, p, groups);
+    }
+    hipLaunchKernelGGL(paged_move, dim3((unsigned)items * parts), dim3(kMoveThreads), 0, st, p, slices, parts);
     return hipGetLastError();
 }
 

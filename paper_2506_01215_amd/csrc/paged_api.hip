@@ -14,6 +14,8 @@ void paged_plan_f32(PagedParams &p);
 hipError_t paged_attend_bf16(const PagedParams &p, hipStream_t st);
 hipError_t paged_attend_f32_launch(const PagedParams &p, hipStream_t st);
 size_t tree_part_dim(bool bf16, int D);
+void paged_evict_plan(PagedEvictParams &p);
+size_t paged_evict_stage_bytes(const PagedEvictParams &p);
 hipError_t paged_evict_launch(const PagedEvictParams &p, hipStream_t st);
 }  // namespace reform
 
@@ -21,7 +23,7 @@ using namespace reform;
 
 namespace {
 
-constexpr int64_t kMaxPagedKeys = (1ll << 31) - 512;     // keys are counted in 32-bit signed integers, some tiles past the last one
+constexpr int64_t kMaxPagedKeys = (1ll << 31) - 65536;   // keys are counted in 32-bit signed integers, some tiles or chunks past the last one
 inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // ---------------------------------------------------------------------------------------
@@ -161,14 +163,36 @@ reform_status check_paged_evict(const reform_paged_evict_desc *d)
     const int64_t es = elt_size(d->dtype);
     if ((d->head_dim * es) % 16 || d->head_dim * es > 4096) return REFORM_ERR_UNSUPPORTED;
     if ((d->kv_page_stride * es) % 16 || (d->kv_head_stride * es) % 16 || (d->kv_row_stride * es) % 16) return REFORM_ERR_UNSUPPORTED;
-    // workgroups of up to 512 threads, two and more for each 64 bytes of a row (evict_paged.hip)
-    if (pool_too_large(d) || (double)d->n_seq * d->n_kv_heads * (d->head_dim * es / 32.0 + 4.0) > kMaxGroups) return REFORM_ERR_UNSUPPORTED;
+    // workgroups of 1024 threads, two for each 128 bytes of a row and two more (evict_paged.hip)
+    if (pool_too_large(d) || (double)d->n_seq * d->n_kv_heads * (d->head_dim * es / 64.0 + 4.0) > kMaxGroups / 2) return REFORM_ERR_UNSUPPORTED;
     return REFORM_OK;
 }
 
-size_t evict_list_bytes(const reform_paged_evict_desc *d)
+PagedEvictParams evict_sizes(const reform_paged_evict_desc *d, const int32_t *page_table)
 {
-    return align_up((size_t)d->n_seq * d->n_kv_heads * d->budget * sizeof(int32_t));
+    PagedEvictParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.pool = pool_of(d, page_table);
+    p.n_seq = d->n_seq; p.Hkv = d->n_kv_heads; p.max_len = d->max_len;
+    p.budget = d->budget; p.n_sink = d->n_sink; p.n_recent = d->n_recent;
+    p.units = compute_units();
+    p.elt = (int)elt_size(d->dtype);
+    p.row_bytes = d->head_dim * p.elt;
+    p.score_ss = d->score_seq_stride; p.score_hs = d->score_head_stride;
+    paged_evict_plan(p);
+    return p;
+}
+
+// The workspace's parts: kept keys, first rows that move, staged rows.
+struct EvictRoom {
+    size_t list, first, stage;
+    size_t all() const { return list + first + stage; }
+};
+EvictRoom evict_room(const PagedEvictParams &p)
+{
+    if (p.max_len <= p.budget) return {0, 0, 0};         // nobody outgrows the budget
+    const size_t items = (size_t)p.n_seq * p.Hkv;
+    return {align_up(items * p.budget * sizeof(int32_t)), align_up(items * sizeof(int32_t)), align_up(paged_evict_stage_bytes(p))};
 }
 
 }  // namespace
@@ -231,8 +255,8 @@ reform_status reform_paged_attend(const reform_paged_desc *d, const void *q, con
 // ---------------------------------------------------------------------------------------
 size_t reform_paged_evict_workspace(const reform_paged_evict_desc *d)
 {
-    if (check_paged_evict(d) != REFORM_OK || d->n_seq == 0 || d->max_len <= d->budget) return 0;
-    return 2 * evict_list_bytes(d) + align_up((size_t)d->n_seq * d->n_kv_heads * sizeof(int32_t));
+    if (check_paged_evict(d) != REFORM_OK || d->n_seq == 0) return 0;
+    return evict_room(evict_sizes(d, nullptr)).all();
 }
 
 reform_status reform_paged_evict(const reform_paged_evict_desc *d, void *k, void *v, float *score, int32_t *pos,
@@ -245,21 +269,15 @@ reform_status reform_paged_evict(const reform_paged_evict_desc *d, void *k, void
     if (!cache_len || new_len == cache_len || (d->max_len > 0 && !score)) return REFORM_ERR_INVALID_ARG;
     if ((d->n_pages > 0 && (!k || !v || k == v)) || (d->max_pages > 0 && !page_table)) return REFORM_ERR_INVALID_ARG;
     if (!aligned16(k) || !aligned16(v)) return REFORM_ERR_UNSUPPORTED;
-    PagedEvictParams p;
-    std::memset(&p, 0, sizeof(p));
+    PagedEvictParams p = evict_sizes(d, page_table);
     p.k = k; p.v = v; p.score = score; p.pos = pos; p.kept = kept_idx; p.new_len = new_len; p.cache_len = cache_len;
-    p.pool = pool_of(d, page_table);
-    p.n_seq = d->n_seq; p.Hkv = d->n_kv_heads; p.max_len = d->max_len;
-    p.budget = d->budget; p.n_sink = d->n_sink; p.n_recent = d->n_recent;
-    p.elt = (int)elt_size(d->dtype);
-    p.row_bytes = d->head_dim * p.elt;
-    p.score_ss = d->score_seq_stride; p.score_hs = d->score_head_stride;
-    if (d->max_len > d->budget) {
-        const size_t need = reform_paged_evict_workspace(d), list = evict_list_bytes(d);
-        if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return REFORM_ERR_WORKSPACE;
-        p.src = (int32_t *)workspace;
-        p.first = (int32_t *)((char *)workspace + 2 * list);
-        if (!p.kept) p.kept = (int32_t *)((char *)workspace + list);
+    const EvictRoom room = evict_room(p);
+    if (room.all()) {
+        if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < room.all()) return REFORM_ERR_WORKSPACE;
+        char *at = (char *)workspace;
+        if (!p.kept) p.kept = (int32_t *)at;
+        p.first = (int32_t *)(at + room.list);
+        p.stage = at + room.list + room.first;
     }
     return paged_evict_launch(p, (hipStream_t)hip_stream) == hipSuccess ? REFORM_OK : REFORM_ERR_RUNTIME;
 }

@@ -41,41 +41,67 @@ __device__ __forceinline__ TreeSeq tree_seq(const PagedParams &p, int b)
     return s;
 }
 
-// The score of an item's virtual keys [32 * TK-tiles t0, t1), and of its part of the keys between the runs: by all threads of the
-// workgroup.  ml(r): reference (log2 units) and sum of the group's row r, from LDS.
-template <int TK, class ML>
-__device__ __forceinline__ void paged_score(const PagedParams &p, int b, int kvh, int len, int t0, int t1, int row0, int rows, ML ml)
-{
-    const PagedSpan<TK> s(p, len);
-    const float c = p.scale * kLog2e;
-    float *score = p.score + (size_t)b * p.score_ss + (size_t)kvh * p.score_hs;
-    const float *x = p.logits + ((size_t)b * p.Hq + (size_t)kvh * p.G + row0) * p.logit_keys;
-    const bool add = p.accumulate || row0 > 0;           // later rows of a group join what the first ones left
-    for (int v = t0 * TK + (int)threadIdx.x; v < t1 * TK; v += (int)blockDim.x) {
-        const int j = v < s.front * TK ? v : v + s.skip * TK;
-        if (j >= len) break;                             // virtual keys ascend
-        const float before = add && (row0 > 0 || j != len - 1) ? score[j] : 0.f;
-        float sum = 0.f;
-#pragma unroll 4
-        for (int r = 0; r < rows; ++r) {
-            const float2 y = ml(r);                      // y.y: 1 / sum
-            sum += __builtin_amdgcn_exp2f(fmaf(x[(size_t)r * p.logit_keys + v], c, -y.x)) * y.y;
-        }
-        score[j] = before + sum;
-    }
-    if (p.accumulate || row0 > 0 || s.skip == 0) return;
-    const long gap = (long)s.skip * TK;
-    const int g0 = s.front * TK + (int)(gap * t0 / s.tiles), g1 = s.front * TK + (int)(gap * t1 / s.tiles);
-    for (int j = g0 + (int)threadIdx.x; j < g1; j += (int)blockDim.x) score[j] = 0.f;
-}
-
-// What paged_score wants of a row: reference 0 where it saw no key, so that -inf stays a weight of 0, and 1 / sum.
+// What the score wants of a row: its reference (log2 units), 0 where it saw no key so that -inf stays a weight of 0, and 1 / sum.
 __device__ __forceinline__ float2 score_row(float m, float l)
 {
     return make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.0f / l);
 }
 
-constexpr int kScoreRows = 64;               // rows of a group that are scored at once
+constexpr int kScoreChunk = 256;             // virtual keys that a wave scores at once, four to a lane
+
+// The score of an item's virtual tiles [t0, t1) and of its part of the keys between the two runs, by waves that share out the
+// chunks: this one takes those whose number, counted on from `counter` (which goes up by the item's chunks), is `mine` modulo `waves`.
+// rows(r0): score_row of the group's row r0 + lane, asked for where the wave has a chunk.
+template <int TK, class ROWS>
+__device__ __forceinline__ void paged_score(const PagedParams &p, int b, int kvh, int len, int t0, int t1, int &counter, int mine, int waves, ROWS rows)
+{
+    const PagedSpan<TK> s(p, len);
+    const int lane = threadIdx.x & 63, chunks = ((t1 - t0) * TK + kScoreChunk - 1) / kScoreChunk;
+    int at = mine - counter % waves;
+    if (at < 0) at += waves;
+    counter += chunks;
+    if (at >= chunks) return;
+    const float c = p.scale * kLog2e;
+    float *score = p.score + (size_t)b * p.score_ss + (size_t)kvh * p.score_hs;
+    const float *logits = p.logits + ((size_t)b * p.Hq + (size_t)kvh * p.G) * p.logit_keys;
+    float2 y = rows(0);
+    for (; at < chunks; at += waves) {
+        const int v0 = t0 * TK + at * kScoreChunk, v = min(v0 + 4 * lane, t1 * TK - 4);          // four keys lie in one tile
+        const int j = v < s.front * TK ? v : v + s.skip * TK, here = v0 + 4 * lane < t1 * TK ? min(4, len - j) : 0;
+        f32x4 before = {0.f, 0.f, 0.f, 0.f}, sum = {0.f, 0.f, 0.f, 0.f};
+        if (p.accumulate && here > 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) before[e] = score[min(j + e, len - 1)];
+        }
+        for (int r0 = 0; r0 < p.G; r0 += 64) {
+            if (p.G > 64) y = rows(r0);
+            const float *x = logits + (size_t)r0 * p.logit_keys + v;
+            const int n = min(64, p.G - r0);
+            for (int r = 0; r < n; r += 4) {             // four rows' logits on their way at once; rows behind the last weigh nothing
+                f32x4 l[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) l[i] = *(const f32x4 *)(x + (size_t)min(r + i, n - 1) * p.logit_keys);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float ref = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y.x), r + i));
+                    const float inv = r + i < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y.y), r + i)) : 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(fmaf(l[i][e], c, -ref)) * inv;
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < here) score[j + e] = (j + e == len - 1 ? 0.f : before[e]) + sum[e];          // the new token has no score yet
+        if (p.accumulate || s.skip == 0) continue;
+        const long gap = (long)s.skip * TK;              // between the runs: as large a part as of the item's chunks
+        const int a = v0 / TK, z = min(a + kScoreChunk / TK, t1);
+        const int g0 = s.front * TK + (int)(gap * a / s.tiles), g1 = s.front * TK + (int)(gap * z / s.tiles);
+        for (int g = g0 + lane; g < g1; g += 64) score[g] = 0.f;
+    }
+}
+
+constexpr int kScoreParts = 4;               // workgroups that score a share, or an item
 
 // The second launch: its first `merges` workgroups put pieces together as tree_merge does, the others score the keys of a share each.
 template <int D, int R, int TK, bool BF16>
@@ -83,36 +109,34 @@ __global__ __launch_bounds__(256) void paged_join(PagedParams p, int merges, int
 {
     using List = TreeList<R, TK, PagedParams>;
     if ((int)blockIdx.x >= merges) {
-        __shared__ float2 sml[kScoreRows];
-        const int block = (int)blockIdx.x - merges;
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int block = ((int)blockIdx.x - merges) / kScoreParts, part = ((int)blockIdx.x - merges) % kScoreParts;
+        const int lane = threadIdx.x & 63, mine = 4 * part + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        int counter = 0;
         auto item = [&](int b, int len, int kvh, int t0, int t1, int w0, int n) {      // n pieces from share w0 on, or 0: finished already
-            for (int row0 = 0; row0 < p.G; row0 += kScoreRows) {
-                const int here = min(kScoreRows, p.G - row0);
-                __syncthreads();                         // the rows before have been used
-                for (int r = wave; r < here; r += 4) {
-                    const int row = row0 + r, rb = row / R;
-                    float m = -INFINITY, l = 0.f;
-                    if (n == 0) {
-                        const float2 y = p.row_ml[(size_t)b * p.Hq + (size_t)kvh * p.G + row];
-                        m = y.x;
-                        l = y.y;
-                    } else {
-                        for (int x = lane; x < n; x += 64) {
-                            const float2 y = p.part_ml[tree_slot(p, w0 + x, x, rb) * p.part_rows + row - rb * R];
-                            const float top = fmaxf(m, y.x), ref = top == -INFINITY ? 0.f : top;
-                            l = l * __builtin_amdgcn_exp2f(m - ref) + y.y * __builtin_amdgcn_exp2f(y.x - ref);
-                            m = top;
-                        }
-                        const float top = wave_max(m), ref = top == -INFINITY ? 0.f : top;
-                        l = wave_sum(l * __builtin_amdgcn_exp2f(m - ref));
+            paged_score<TK>(p, b, kvh, len, t0, t1, counter, mine, 4 * kScoreParts, [&](int r0) {
+                const int row = min(r0 + lane, p.G - 1), rb = row / R;
+                if (n == 0) {
+                    const float2 y = p.row_ml[(size_t)b * p.Hq + (size_t)kvh * p.G + row];
+                    return score_row(y.x, y.y);
+                }
+                float m = -INFINITY, l = 0.f;
+                for (int x = 0; x < n; x += 4) {         // pieces past the last repeat it, without weight
+                    float2 y[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int piece = min(x + i, n - 1);
+                        y[i] = p.part_ml[tree_slot(p, w0 + piece, piece, rb) * p.part_rows + row - rb * R];
+                        if (x + i >= n) y[i] = make_float2(-INFINITY, 0.f);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float top = fmaxf(m, y[i].x), ref = top == -INFINITY ? 0.f : top;
+                        l = l * __builtin_amdgcn_exp2f(m - ref) + y[i].y * __builtin_amdgcn_exp2f(y[i].x - ref);
                         m = top;
                     }
-                    if (lane == 0) sml[r] = score_row(m, l);
                 }
-                __syncthreads();
-                paged_score<TK>(p, b, kvh, len, t0, t1, row0, here, [&](int r) { return sml[r]; });
-            }
+                return score_row(m, l);
+            });
         };
         if (p.shares == 0) {
             const int b = block / p.Hkv, kvh = block - b * p.Hkv;
@@ -197,7 +221,7 @@ inline void paged_join_launch(const PagedParams &p, hipStream_t st)
     int rows = 1;                                        // as in tree_merge_launch
     while (2 * rows <= 1024 / D && rows < p.part_rows && blocks * ((p.part_rows + rows - 1) / rows) > 3l * p.units) rows *= 2;
     const long merges = p.shares ? blocks * ((p.part_rows + rows - 1) / rows) : 0;
-    const long scores = !p.logits || (p.shares == 0 && p.row_blocks == 1) ? 0 : p.shares ? p.shares : (long)p.n_seq * p.Hkv;
+    const long scores = !p.logits || (p.shares == 0 && p.row_blocks == 1) ? 0 : kScoreParts * (p.shares ? p.shares : (long)p.n_seq * p.Hkv);
     if (merges + scores)
         hipLaunchKernelGGL((paged_join<D, R, TK, BF16>), dim3((unsigned)(merges + scores)), dim3(256), 0, st, p, (int)merges, rows, (int)by_share);
 }

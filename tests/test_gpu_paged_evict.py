@@ -196,3 +196,34 @@ def test_graph_follows_lengths_and_scores():
         torch.cuda.synchronize()
         want_len = call(*eager, torch.zeros_like(new_len))
         assert torch.equal(k, eager[0]) and torch.equal(v, eager[1]) and torch.equal(score, eager[2]) and torch.equal(new_len, want_len)
+
+
+@pytest.mark.parametrize("lens,budget,n_sink,n_recent", [
+    ([4300], 4096, 4, 64),                  # few rows go: segments move at once
+    ([9000, 4200, 100], 4096, 0, 0),        # more go than is staged, beside one where few do
+    ([16500, 16385], 16384, 300, 200), ([8193], 8192, 8000, 0), ([8193], 8192, 0, 8000),
+])
+@pytest.mark.parametrize("kind", ["spread", "ties", "equal"])
+@pytest.mark.parametrize("page_len", [16, 50])
+def test_rows_in_segments(lens, budget, n_sink, n_recent, kind, page_len):
+    run_case(1, 64, lens, page_len, budget, n_sink, n_recent, BF, seed=budget, kind=kind)
+    run_case(2, 4, lens, page_len, budget, n_sink, n_recent, F, seed=budget, kind=kind, columns=max(lens) // page_len + 9)
+
+
+def test_segments_and_pages_that_are_not_there():
+    run_case(1, 64, [4300], 64, 4096, 4, 64, BF, seed=1, holes=[(0, 31), (0, 32), (0, 16), (0, 48), (0, 66)])
+
+
+def test_the_first_rows_go():
+    """Every segment's last rows come from the next one's."""
+    rnd, g = random.Random(1), torch.Generator().manual_seed(1)
+    n, budget, page_len = 4500, 4096, 32
+    table, pages = ref.make_table(rnd, [n], page_len)
+    k, v = (torch.randn(pages, 1, page_len, 64, generator=g).to(BF) for _ in range(2))
+    score = torch.arange(len(table[0]) * page_len).float()[None, None].clone()
+    pos = torch.arange(score.shape[2], dtype=torch.int32)[None, None].clone()
+    want = expected(k, v, score, pos, table, [n], budget, 0, 0)
+    dk, dv, ds, dp = (x.to(DEV) for x in (k, v, score, pos))
+    binding.reform_paged_evict(dk, dv, ds, i32(table), i32([n]), budget, pos=dp)
+    for x, y in zip((dk, dv, ds, dp), want):
+        assert torch.equal(x.cpu(), y)
