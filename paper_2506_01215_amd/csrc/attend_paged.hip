@@ -34,12 +34,15 @@ __device__ __forceinline__ long lane_value(long x, int lane)
     return (long)(((unsigned long)hi << 32) | lo);
 }
 
-// K and V are read once: past the caches' usual order of replacement (one token over 131072 keys, 32/8 heads of 128: 96 us without
-// the hint, 85 with it; 32 caches of up to 8192 139, 123).
-__device__ __forceinline__ v4u stream_load(const void *p) { return __builtin_nontemporal_load((const v4u *)p); }
+// K and V that are read once go past the caches' usual order of replacement (paged_plan).
+template <bool STREAM>
+__device__ __forceinline__ v4u load16(const void *p)
+{
+    return STREAM ? __builtin_nontemporal_load((const v4u *)p) : *(const v4u *)p;
+}
 
 // Virtual tiles [t0, t1) of sequence b's KV head for the heads from row0 on.  po, pml: as in seq_segment.
-template <int D, int NW, bool HALVES>
+template <int D, int NW, bool HALVES, bool STREAM>
 __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int kvh, int len, int row0, int t0, int t1, float *po, float2 *pml, char *smem)
 {
     using S = PagedShape<D, NW>;
@@ -83,8 +86,8 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
                 for (int i = 0; i < S::PIECES; ++i) {
                     const long half = i < S::PIECES / 2 ? a : b1;
                     const uint32_t off = lane_off + (uint32_t)((i % (S::PIECES / 2)) * STEP * (int)p.pool.row_stride) * 2u;
-                    kreg[i] = stream_load((const char *)(K + half) + off);
-                    vreg[i] = stream_load((const char *)(V + half) + off);
+                    kreg[i] = load16<STREAM>((const char *)(K + half) + off);
+                    vreg[i] = load16<STREAM>((const char *)(V + half) + off);
                 }
             } else {
 #pragma unroll
@@ -93,8 +96,8 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
                     const uint32_t off = lane_off + (uint32_t)((i % (S::PIECES / 2)) * STEP * (int)p.pool.row_stride) * 2u;
                     kreg[i] = vreg[i] = (v4u){0u, 0u, 0u, 0u};           // weights of 0 meet zeros, whatever lies there
                     if ((mask >> (lane / C8 + i * STEP)) & 1u) {
-                        kreg[i] = stream_load((const char *)(K + half) + off);
-                        vreg[i] = stream_load((const char *)(V + half) + off);
+                        kreg[i] = load16<STREAM>((const char *)(K + half) + off);
+                        vreg[i] = load16<STREAM>((const char *)(V + half) + off);
                     }
                 }
             }
@@ -106,8 +109,8 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
                 const long at = ((long)__shfl((int)(ahead >> 32), row) << 32) | (unsigned)__shfl((int)ahead, row);
                 kreg[i] = vreg[i] = (v4u){0u, 0u, 0u, 0u};
                 if (at >= 0) {
-                    kreg[i] = stream_load(K + at + lane % C8 * 8);
-                    vreg[i] = stream_load(V + at + lane % C8 * 8);
+                    kreg[i] = load16<STREAM>(K + at + lane % C8 * 8);
+                    vreg[i] = load16<STREAM>(V + at + lane % C8 * 8);
                 }
             }
             look(u + NW);
@@ -258,25 +261,25 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
     }
 }
 
-template <int D, int NW, bool HALVES>
+template <int D, int NW, bool HALVES, bool STREAM>
 __global__ __launch_bounds__(NW * 64, 2) void paged_attend(PagedParams p)
 {
     using S = PagedShape<D, NW>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     list_walk<S::R, S::TK>(p, [&](int b, const TreeSeq &seq, int kvh, int rb, int t0, int t1, long slot) {
-        paged_segment<D, NW, HALVES>(p, b, kvh, seq.len, rb * S::R, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
+        paged_segment<D, NW, HALVES, STREAM>(p, b, kvh, seq.len, rb * S::R, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * D,
                                      slot < 0 ? nullptr : p.part_ml + (size_t)slot * p.part_rows, smem);
     });
 }
 
-template <int D, int NW, bool HALVES>
+template <int D, int NW, bool HALVES, bool STREAM>
 hipError_t launch(const PagedParams &p, hipStream_t st)
 {
     using S = PagedShape<D, NW>;
-    const hipError_t e = raise_lds<paged_attend<D, NW, HALVES>>(S::lds_bytes);
+    const hipError_t e = raise_lds<paged_attend<D, NW, HALVES, STREAM>>(S::lds_bytes);
     if (e != hipSuccess) return e;
     const unsigned grid = (unsigned)(p.shares ? p.shares : p.n_seq * p.Hkv) * p.row_blocks;
-    hipLaunchKernelGGL((paged_attend<D, NW, HALVES>), dim3(grid), dim3(NW * 64), S::lds_bytes, st, p);
+    hipLaunchKernelGGL((paged_attend<D, NW, HALVES, STREAM>), dim3(grid), dim3(NW * 64), S::lds_bytes, st, p);
     paged_join_launch<D, S::R, S::TK, true>(p, st);
     return hipGetLastError();
 }
@@ -290,11 +293,20 @@ void paged_plan_bf16(PagedParams &p)
     paged_plan(p, 16, 32, narrow ? 2000 : 1600, (narrow ? 256 : 128) / 32, (narrow ? 2 : 1) * p.units);
 }
 
+namespace {
+
+template <int D, int NW>
+hipError_t launch_form(const PagedParams &p, hipStream_t st)
+{
+    if (p.pool.page_len % 16) return p.stream ? launch<D, NW, false, true>(p, st) : launch<D, NW, false, false>(p, st);
+    return p.stream ? launch<D, NW, true, true>(p, st) : launch<D, NW, true, false>(p, st);
+}
+
+}  // namespace
+
 hipError_t paged_attend_bf16(const PagedParams &p, hipStream_t st)
 {
-    const bool halves = p.pool.page_len % 16 == 0;
-    if (p.D == 64) return halves ? launch<64, 4, true>(p, st) : launch<64, 4, false>(p, st);
-    return halves ? launch<128, 8, true>(p, st) : launch<128, 8, false>(p, st);
+    return p.D == 64 ? launch_form<64, 4>(p, st) : launch_form<128, 8>(p, st);
 }
 
 }  // namespace reform

@@ -59,7 +59,7 @@ __device__ __forceinline__ void paged_segment_f32(const PagedParams &p, int b, i
         for (int a = 0; a < NA; ++a) k[a] = zero;
         if (at < 0) return;
 #pragma unroll
-        for (int a = 0; a < NA; ++a) k[a] = 16 * a + 4 * lg < D ? __builtin_nontemporal_load((const f32x4 *)(K + at + 16 * a + 4 * lg)) : zero;
+        for (int a = 0; a < NA; ++a) k[a] = quad(K + at, a);
     };
     int u = t0 + wave;
     long here = look(u), next = look(u + kWaves);
@@ -74,7 +74,7 @@ __device__ __forceinline__ void paged_segment_f32(const PagedParams &p, int b, i
             const int from = 4 * lg + e;                 // lane of the key's place
             const long at = ((long)__shfl((int)(here >> 32), from) << 32) | (unsigned)__shfl((int)here, from);
 #pragma unroll
-            for (int a = 0; a < NA; ++a) v[e][a] = at >= 0 && 16 * a + ln < D ? __builtin_nontemporal_load(V + at + 16 * a + ln) : 0.f;
+            for (int a = 0; a < NA; ++a) v[e][a] = at >= 0 && 16 * a + ln < D ? V[at + 16 * a + ln] : 0.f;
         };
         if (AHEAD) {
 #pragma unroll

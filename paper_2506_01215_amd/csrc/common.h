@@ -211,6 +211,7 @@ struct PagedParams {
     int n_seq, Hq, Hkv, G, D, max_len, window, n_sink, accumulate;
     long q_ss, q_hs, o_ss, o_hs, score_ss, score_hs;         // elements
     float scale;
+    int stream;              // K and V are read past the caches' usual order of replacement
     int shares, least, units, block, row_blocks, part_rows;  // as in TreeParams
     float *part_o;
     float2 *part_ml;
