@@ -94,12 +94,7 @@ hipError_t launch_short(const WindowParams &p, hipStream_t st)
 template <int D>
 hipError_t launch_bf16(const WindowParams &p, hipStream_t st)
 {
-#ifdef FORCE_FORM
-    const int form = FORCE_FORM;
-#else
-    const int form = window_choose(D, p.G, p.Hkv, p.n_seq, p.n_q, p.n_k, p.window, p.n_sink, p.units);
-#endif
-    const PromptForm &f = prompt_forms(D)[form];
+    const PromptForm &f = window_forms(D)[window_choose(D, p.G, p.Hkv, p.n_seq, p.n_q, p.n_k, p.window, p.n_sink, p.units)];
     if (f.rows == 32) return launch_short<D, 2, 4>(p, st);
     if (f.rows == 16) return launch_short<D, 1, 8>(p, st);
     if constexpr (D == 64) {
