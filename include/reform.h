@@ -567,8 +567,8 @@ reform_status reform_tree_accept(const reform_accept_desc *desc, const int32_t *
  *     j in [0, t] with j > t - window or j < n_sink
  * A window of nk keys or more is reform_prompt_attend.  A row that sees no key (t < 0) gets out = 0 and lse = -inf.
  *     q, out, k, v, cu_q, cu_k, lse   as in reform_prompt_attend: layouts, lengths read on the device, boundaries that are out of
- *              place, rows of no sequence, arithmetic.  Keys and values that are not finite make rows of their sequence NaN that
- *              see them, and may make those NaN whose block of rows goes through their tile of 64 keys
+ *              place, rows of no sequence, arithmetic.  Keys and values that are not finite stay within their sequence; there, rows
+ *              whose block goes through their tile of 64 keys may become NaN as well as those that see them
  * Supported: as reform_prompt_attend; window >= 1, n_sink >= 0.
  * The workspace is that of reform_prompt_attend: without it, or with less than the query asks for, REFORM_ERR_WORKSPACE.
  */
@@ -611,9 +611,11 @@ reform_status reform_window_attend(const reform_window_desc *desc, const void *q
  *     cache_len   [n_seq] int32 in device memory; values outside [0, max_len] are moved into it
  *     score       [n_seq][n_kv_heads][>= max_len] fp32 by strides, entries contiguous; may be NULL
  *     lse         [n_seq][n_q_heads] fp32, may be NULL
- * Arithmetic as in reform_chunk_attend_score (the score sums unrounded fp32 probabilities), bitwise reproducible for the
- * same arguments; results depend on the batch and on max_len by rounding only.  Keys and values that are not finite stay
- * within their sequence and KV head.  Rows behind L are never looked at.
+ * out, lse and score lie apart from the inputs and one another.
+ * Arithmetic: products and sums in fp32; for bf16 the probabilities of the P.V product are taken in two bf16 parts (16 bits), the score sums the
+ * unrounded fp32 ones.  Bitwise reproducible for the same arguments; results depend on the batch and on max_len by rounding only.
+ * Keys and values that are not finite matter where they are seen only, and there stay within their sequence and KV head (an infinite
+ * value may give NaN).  Rows behind L are never looked at.
  * Supported: types and head_dim as reform_prompt_attend; any page_len >= 1; n_pages * page_len below 2^31; max_len at most
  * max_pages * page_len and 2^31 - 65536; row stride of k and v below 2^24; n_seq * n_q_heads at most 2^22; with B = ceil(n_q_heads /
  * n_kv_heads / 16), n_seq * n_kv_heads * B * (max_len / 16 + 64) below 2^31.  n_seq = 0 does nothing.
@@ -656,7 +658,10 @@ reform_status reform_paged_attend(const reform_paged_desc *desc, const void *q, 
  *     score    [n_seq][n_kv_heads][>= max_len] fp32 by strides, entries contiguous, in/out; must be finite (no NaN/Inf)
  *     pos      like score, with its strides, int32 that travel with the rows, in/out; may be NULL
  *     kept_idx [n_seq][n_kv_heads][budget] int32 out, contiguous, the first new_len entries of a head; may be NULL
- *     new_len  [n_seq] int32 out, may be NULL; must not be cache_len itself
+ *     new_len  [n_seq] int32 out, may be NULL
+ * k, v, score, pos, kept_idx and new_len lie apart from one another (k and v may be parts of one pool) and from the inputs.
+ * The workspace takes the kept keys, and rows that are set aside where few heads have many; the query gives 0 where max_len is within
+ * the budget.  Without it, or with less than the query asks for, the call returns REFORM_ERR_WORKSPACE.
  * Supported: head_dim * sizeof(element) a multiple of 16 up to 4096; strides of k and v multiples of 16 bytes; page_len, n_pages,
  * max_pages, max_len as in reform_paged_attend; budget at least 1; n_seq * n_kv_heads * (row bytes / 64 + 4) below 2^22.  n_seq = 0 does
  * nothing.

@@ -2,7 +2,9 @@
 //
 // Bound: reading K and V once.  The rows of a block are up to 16 heads of a KV group; the keys are shared out over the whole chip
 // (paged_list.h), and every wave has tiles of 32 keys of its own, without a barrier before the sums meet: S^T = K Q^T, so that a
-// lane owns one head's logits, which are the B operand of O^T = V^T P^T as they stand, as in attend_seq.h.
+// lane owns one head's logits, which are the B operand of O^T = V^T P^T as they stand, as in attend_seq.h.  The matrix pipe waits for
+// memory, so P.V is done twice, with the probabilities rounded to bf16 and with what that leaves of them: together 16 bits, and
+// outputs are off by their own rounding (0.0017 of their norm; 0.0023 with one product).
 //
 // What pages add: a tile's rows lie anywhere.  Where page_len is a multiple of 16 (HALVES), each half of a tile lies in one page:
 // lane l looks up half l % 2 of the wave's tile l / 2, 32 tiles in one go, and a tile's two bases are read from the lanes into scalar
@@ -166,7 +168,7 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
             *(f32x4 *)(logits + (size_t)u * TK + 16) = x[1];
         }
         // against the reference so far, and anew with the true maximum where a row outgrew it (or has none yet)
-        v4u pb;
+        v4u pb, pl;                                      // rounded to bf16, and what that leaves, rounded
         float rs;
         auto probabilities = [&](float ref) {
             float pv[8];
@@ -176,7 +178,11 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
                 pv[e] = __builtin_amdgcn_exp2f(fmaf(x[e >> 2][e & 3], c, -ref));
                 rs += pv[e];
             }
-            pb = (v4u){pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]), pack_bf16x2(pv[4], pv[5]), pack_bf16x2(pv[6], pv[7])};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                pb[i] = pack_bf16x2(pv[2 * i], pv[2 * i + 1]);
+                pl[i] = pack_bf16x2(pv[2 * i] - __uint_as_float(pb[i] << 16), pv[2 * i + 1] - __uint_as_float(pb[i] & 0xffff0000u));
+            }
         };
         probabilities(m * c);
         if (__builtin_amdgcn_ballot_w64(!(rs < kBigSum)) != 0ull) {
@@ -200,6 +206,7 @@ __device__ __forceinline__ void paged_segment(const PagedParams &p, int b, int k
         for (int db = 0; db < DB; ++db) {
             const v2u lo = lds_read_tr16(vf + 16 * db), hi = lds_read_tr16(vf + 16 * ROW + 16 * db);
             o[db] = mfma16((v4u){lo.x, lo.y, hi.x, hi.y}, pb, o[db]);
+            o[db] = mfma16((v4u){lo.x, lo.y, hi.x, hi.y}, pl, o[db]);
         }
     }
 

@@ -35,7 +35,7 @@ __global__ __launch_bounds__(NW * KG * 64, 2) void window_attend(WindowParams p)
     using S = RowsShape<D, NW, KG>;
     extern __shared__ __attribute__((aligned(16))) u16 lds[];
     const int kvh = blockIdx.x % p.Hkv;
-    const PromptBlock blk = prompt_block<S::ROWS, S::BN>(p, blockIdx.x / p.Hkv);
+    const PromptBlock blk = prompt_block<S::ROWS, S::BN>(p, blockIdx.x / p.Hkv, p.sorted);
     if (blk.rb < 0) return;
     SeqRows r;
     WindowKeys k;
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(NW * 64, 2) void window_attend_short(WindowParams p
     using S = SeqShape<D, NB, NW>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int kvh = blockIdx.x % p.Hkv;
-    const PromptBlock blk = prompt_block<S::R, S::TK>(p, blockIdx.x / p.Hkv);
+    const PromptBlock blk = prompt_block<S::R, S::TK>(p, blockIdx.x / p.Hkv, p.sorted);
     if (blk.rb < 0) return;
     SeqRows r;
     WindowKeys k;
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kF32Waves * 64, 2) void window_attend_f32(WindowPar
 {
     __shared__ F32Sums<DP> sh;
     const int kvh = blockIdx.x % p.Hkv;
-    const PromptBlock blk = prompt_block<kF32Rows, kF32Keys>(p, blockIdx.x / p.Hkv);
+    const PromptBlock blk = prompt_block<kF32Rows, kF32Keys>(p, blockIdx.x / p.Hkv, p.sorted);
     if (blk.rb < 0) return;
     SeqRows r;
     WindowKeys k;
@@ -97,9 +97,7 @@ hipError_t launch_bf16(const WindowParams &p, hipStream_t st)
     const PromptForm &f = window_forms(D)[window_choose(D, p.G, p.Hkv, p.n_seq, p.n_q, p.n_k, p.window, p.n_sink, p.units)];
     if (f.rows == 32) return launch_short<D, 2, 4>(p, st);
     if (f.rows == 16) return launch_short<D, 1, 8>(p, st);
-    if constexpr (D == 64) {
-        if (f.rows == 256) return launch_long<D, 8, 1>(p, st);
-    } else {
+    if constexpr (D == 128) {
         if (f.groups == 2) return launch_long<D, 4, 2>(p, st);
     }
     return launch_long<D, 4, 1>(p, st);

@@ -190,6 +190,7 @@ struct PromptParams {
 
 struct WindowParams : PromptParams {
     int window, n_sink;      // keys up to a row's own that it sees, and first keys that all rows see: both at most n_k
+    int sorted;              // long blocks first (prompt_block)
 };
 
 // A pool of pages that sequences share, and how a sequence's key is found in it (pool_row).

@@ -49,8 +49,9 @@ __device__ __forceinline__ int prompt_blocks_with(const PromptParams &p, const P
     return s.blocks - p.G * x / ROWS;
 }
 
+// sorted: by length, where there are up to kPromptSorted sequences; else in their order.
 template <int ROWS, int TK>
-__device__ __forceinline__ PromptBlock prompt_block(const PromptParams &p, int idx)
+__device__ __forceinline__ PromptBlock prompt_block(const PromptParams &p, int idx, bool sorted = true)
 {
     const int lane = threadIdx.x & 63;
     PromptSeq s = {0, 0, 0, 0, 0};
@@ -59,7 +60,7 @@ __device__ __forceinline__ PromptBlock prompt_block(const PromptParams &p, int i
         s = prompt_seq<ROWS>(p, 0);
         rb = s.blocks - 1 - idx;
         if (rb < 0) return {-1, 0, 0, 0, 0, 0};
-    } else if (p.n_seq <= kPromptSorted) {
+    } else if (sorted && p.n_seq <= kPromptSorted) {
         if (lane < p.n_seq) s = prompt_seq<ROWS>(p, lane);
         auto count = [&](int tiles, int &mine) {
             mine = prompt_blocks_with<ROWS, TK>(p, s, tiles);

@@ -1,25 +1,26 @@
 // Which form of the packed prompts' attention a batch with a sliding window takes (attend_window.hip).  Host code without device types.
 //
-// The forms are prompt_plan.h's, and the time of one is estimated as there, with as many tiles as a block goes through: those up to its last
+// The forms are prompt_plan.h's (without 256 rows at head_dim 64, which no batch of those below took less time in), and the time of one is estimated as there, with as many tiles as a block goes through: those up to its last
 // row's key, but no more than the window, the block's own rows and the first keys take.  The costs are of their own: with few tiles
 // to a block more of them are masked, and more of the time is a block's beginning and end.
 //
 // Fitted to 160 batches (30 to 17000 rows, 1 to 32 sequences, windows of 1 to 6000 keys, up to 256 first ones, with and without keys in front),
-// each in all four forms: the one that is chosen takes 1.7 % more time in the mean than the best, at worst 37 %; 110 other
+// each in all forms: the one that is chosen takes 1.7 % more time in the mean than the best, at worst 37 %; 110 other
 // batches 3 %, at worst 46 % (30 sequences of together 154 rows, window 797, 24/8 heads of 128: 10.6 us, in blocks of 128 7.2).  Measured, us,
-// blocks of 256 / 128 / 32 / 16 at head_dim 64: 525 rows of two, window 2, 14/2 heads 11.8 / 9.7 / 6.7 / 9.4; blocks of 128 / 128 with two
+// blocks of 128 / 32 / 16 at head_dim 64: 525 rows of two, window 2, 14/2 heads 9.7 / 6.7 / 9.4; blocks of 128 / 128 with two
 // groups / 32 / 16 at 128: 157 rows of four, window 305, 24/8 9.5 / 11.1 / 8.5 / 6.6; 1072 rows, window 146, 8/1 15.2 / 16.2 / 11.0 / 16.1.
 #pragma once
 #include "prompt_plan.h"
 
 namespace reform {
 
+inline int window_form_count(int head_dim) { return head_dim == 64 ? 3 : 4; }
+
 inline const PromptForm *window_forms(int head_dim)
 {
-    static const PromptForm wide64[kPromptForms] = {{256, 1, 64, 1.53, 1.26, 6.0, 6.2}, {128, 1, 64, 0.77, 0.89, 5.8, 3.3},
-                                                    {32, 4, 32, 0.41, 0.64, 5.3, 1.6}, {16, 8, 32, 0.75, 1.98, 2.8, 3.2}};
-    static const PromptForm wide128[kPromptForms] = {{128, 1, 64, 1.09, 1.63, 6.1, 5.3}, {128, 2, 64, 2.52, 2.59, 6.6, 6.9},
-                                                     {32, 4, 32, 0.91, 1.33, 6.4, 2.9}, {16, 8, 32, 1.74, 3.32, 2.7, 3.6}};
+    static const PromptForm wide64[3] = {{128, 1, 64, 0.77, 0.89, 5.8, 3.3}, {32, 4, 32, 0.41, 0.64, 5.3, 1.6}, {16, 8, 32, 0.75, 1.98, 2.8, 3.2}};
+    static const PromptForm wide128[4] = {{128, 1, 64, 1.09, 1.63, 6.1, 5.3}, {128, 2, 64, 2.52, 2.59, 6.6, 6.9},
+                                          {32, 4, 32, 0.91, 1.33, 6.4, 2.9}, {16, 8, 32, 1.74, 3.32, 2.7, 3.6}};
     return head_dim == 64 ? wide64 : wide128;
 }
 
@@ -49,7 +50,7 @@ inline int window_choose(int head_dim, int G, int Hkv, int n_seq, int n_q, int n
     const PromptForm *forms = window_forms(head_dim);
     int best = 0;
     double least = 0.0;
-    for (int i = 0; i < kPromptForms; ++i) {
+    for (int i = 0; i < window_form_count(head_dim); ++i) {
         const double t = window_estimate(forms[i], G, Hkv, n_seq, n_q, n_k, window, n_sink, units);
         if (i == 0 || t < least) { best = i; least = t; }
     }

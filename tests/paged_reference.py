@@ -2,12 +2,31 @@
 serving_reference.py.  One more is needed, for the score: a probability is off by a factor of at most 1 + 2 E + (n + 8) 2^-24
 (exponent, sum), and adding those of G heads, and what was there before, rounds G + 1 times:
    |d score| <= sum_h p_h (2 E_h + (n + 8) 2^-24) + (G + 1) 2^-24 |score|
+Single tokens over pages take the probabilities of P.V in two bf16 parts, the second the rounded rest of the first: off by
+u(bf16)^2 = 2^-16 of each at most, not by u(bf16).
 """
 import math
 
 import torch
 
-from serving_reference import U24
+from serving_reference import U24, half_step
+from serving_checks import finite
+
+
+def check_single(out, lse, want_out, want_lse, a, err, keys, dtype, what=""):
+    """As serving_reference.check_attention, with the bound of probabilities in two parts, and every number required to be one."""
+    out, lse, u = out.double().cpu(), lse.double().cpu(), half_step(dtype)
+    for t, name in ((out, "outputs"), (want_out, "reference"), (a, "bound"), (err, "bound")):
+        finite(t, f"{what} {name}")
+    rel = 2 * err + (keys + 8) * U24 + (u * u if dtype == torch.bfloat16 else 0.0)
+    bound = rel[..., None] * a * 1.01 + u * want_out.abs() * 1.01 + 1e-30
+    bad = (out - want_out).abs() > bound
+    assert not bool(bad.any()), f"{what}: {int(bad.sum())} of {bad.numel()} outputs off, worst {float(((out - want_out).abs() / bound).max()):.2f} of the bound"
+    empty = want_lse == -math.inf
+    finite(lse[~empty], f"{what} lse")
+    assert bool((lse[empty] == -math.inf).all()), f"{what}: lse of rows that see nothing"
+    bad = ((lse - want_lse).abs() > err + (keys + 8) * U24 + 4 * U24 * (want_lse.abs() + 1)) & ~empty
+    assert not bool(bad.any()), f"{what}: {int(bad.sum())} lse off"
 
 
 def rows(q, k, v, scale, seen):

@@ -9,7 +9,7 @@ import torch
 import paged_reference as ref
 import serving_reference as sref
 from paper_2506_01215_amd import binding
-from serving_checks import check_attention, finite
+from serving_checks import finite
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -75,7 +75,7 @@ def run_case(hq, hkv, d, lens, page_len, dtype, seed, window=0, sinks=0, score=N
                                                score=sc, accumulate=bool(score), out=out, lse=lse, max_len=max_len)
     want, want_lse, a, err, scores = ref.paged_attend(q, k, v, table, lens, d ** -0.5, window, sinks)
     for b in range(S):
-        check_attention(got[b], got_lse[b], want[b], want_lse[b], a[b], err[b], max(1, lens[b]), dtype, f"sequence {b}")
+        ref.check_single(got[b], got_lse[b], want[b], want_lse[b], a[b], err[b], max(1, lens[b]), dtype, f"sequence {b}")
     if score is not None:
         check_score(sc, before, scores, lens, hq // hkv, score)
     return got, got_lse
@@ -141,7 +141,7 @@ def test_lengths_outside_are_moved_in(dtype):
     table = [[0, 1, 2, 3], [4, 5, 6, 7], [8, 9, 10, 11]]
     out, lse = binding.reform_paged_attend(q.to(DEV), k.to(DEV), v.to(DEV), i32(table), i32([-5, 1 << 30, 30]), 0.125, max_len=50)
     want, wl, a, err, _ = ref.paged_attend(q, k, v, table, [0, 50, 30], 0.125)
-    check_attention(out, lse, want, wl, a, err, 64, dtype)
+    ref.check_single(out, lse, want, wl, a, err, 64, dtype)
 
 
 def test_sharp_logits():
@@ -171,7 +171,7 @@ def test_strides_and_shared_pages(dtype, page_len):
     sc = before.to(DEV)
     got, lse = binding.reform_paged_attend(q.to(DEV)[:hq].transpose(0, 1), *dev, wide[:, 5:], i32(n), 0.125, score=sc[..., :80], accumulate=True, out=out)
     want, wl, a, err, scores = ref.paged_attend(q[:hq].transpose(0, 1), *pool, table, n, 0.125)
-    check_attention(got, lse, want, wl, a, err, 80, dtype)
+    ref.check_single(got, lse, want, wl, a, err, 80, dtype)
     check_score(sc, before, scores, n, hq // hkv, True)
 
 

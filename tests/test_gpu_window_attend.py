@@ -65,6 +65,15 @@ def test_one_long_prompt(hq, hkv, d, n, window, sinks):
     run_case(hq, hkv, d, [n], [n], window, sinks, BF, seed=n)
 
 
+@pytest.mark.parametrize("hq,hkv,d,lens,window,sinks", [
+    # a size of every form: 128, 32 and 16 rows at head_dim 64; 128, 128 by two groups, 32 and 16 at 128 (test_window_plan.py)
+    (32, 8, 64, [1200], 300, 0), (16, 2, 64, [900], 511, 65), (8, 2, 64, [100], 7, 2), (8, 2, 128, [2100], 300, 100), (32, 8, 128, [700], 200, 256),
+    (2, 1, 128, [6164], 12, 64), (16, 2, 128, [700, 600, 500], 833, 5), (16, 2, 128, [70, 66, 65, 65], 8, 64),
+    (8, 2, 128, [60], 33, 5)])
+def test_every_form(hq, hkv, d, lens, window, sinks):
+    run_case(hq, hkv, d, lens, lens, window, sinks, BF, seed=sum(lens))
+
+
 @pytest.mark.parametrize("d,rows,keys,window,sinks", [(128, 3, 9000, 8000, 4), (64, 1, 12000, 11000, 300), (128, 20, 5000, 4000, 64)])
 def test_few_rows_behind_many_keys(d, rows, keys, window, sinks):
     run_case(8, 2, d, [rows, 1], [keys, keys - 77], window, sinks, BF, seed=rows)

@@ -22,7 +22,7 @@ def window(**kw):
     return binding.WindowDesc(**{**base, **kw})
 
 
-def call_window(d, q=FAKE, k=FAKE, v=FAKE, cu=FAKE, out=FAKE):
+def call_window(d, q=FAKE, k=FAKE, v=FAKE, cu=FAKE, out=2 * FAKE):
     return lib().reform_window_attend(ctypes.byref(d), q, k, v, cu, None, out, None, None, 0, None)
 
 
@@ -45,7 +45,7 @@ def test_window_rejects(field, value, status):
 
 
 def test_window_rejects_pointers_and_types():
-    for kw in (dict(q=None), dict(k=None), dict(v=None), dict(cu=None), dict(out=None), dict(q=FAKE + 8), dict(out=FAKE + 2)):
+    for kw in (dict(q=None), dict(k=None), dict(v=None), dict(cu=None), dict(out=None), dict(q=FAKE + 8), dict(out=FAKE + 2), dict(out=FAKE)):
         assert call_window(window(), **kw) == 1
     assert call_window(window(dtype=0, head_dim=130, o_row_stride=132, o_head_stride=13200)) == 2
     assert call_window(window(dtype=0, head_dim=260, o_row_stride=260, o_head_stride=26000)) == 2
@@ -62,7 +62,7 @@ def paged(**kw):
     return binding.PagedDesc(**{**base, **kw})
 
 
-def call_paged(d, q=FAKE, k=FAKE, v=FAKE, table=FAKE, lens=FAKE, score=None, out=FAKE, ws=None, nbytes=0):
+def call_paged(d, q=FAKE, k=FAKE, v=FAKE, table=FAKE, lens=FAKE, score=None, out=2 * FAKE, ws=None, nbytes=0):
     return lib().reform_paged_attend(ctypes.byref(d), q, k, v, table, lens, score, out, None, ws, nbytes, None)
 
 
@@ -82,11 +82,12 @@ def test_paged_rejects(field, value, status):
 
 def test_paged_rejects_pointers_scores_and_sizes():
     for kw in (dict(q=None), dict(k=None), dict(v=None), dict(lens=None), dict(out=None), dict(table=None), dict(k=FAKE + 8), dict(out=FAKE + 4),
-               dict(score=FAKE)):
+               dict(score=3 * FAKE), dict(out=FAKE)):
         assert call_paged(paged(), **kw) == 1, kw
     assert call_paged(paged(want_score=1)) == 1                         # a score is wanted and there is none
-    assert call_paged(paged(want_score=1, score_head_stride=6399), score=FAKE) == 1       # heads overlap
-    assert call_paged(paged(want_score=1, score_seq_stride=6400), score=FAKE) == 1
+    assert call_paged(paged(want_score=1), score=2 * FAKE) == 1         # it is the output
+    assert call_paged(paged(want_score=1, score_head_stride=6399), score=3 * FAKE) == 1       # heads overlap
+    assert call_paged(paged(want_score=1, score_seq_stride=6400), score=3 * FAKE) == 1
     huge = dict(page_len=1 << 20, n_pages=2047, max_pages=2048, kv_head_stride=128 << 20, kv_page_stride=256 << 20)
     assert call_paged(paged(max_len=(1 << 31) - 65535, **huge)) == 2
     assert call_paged(paged(n_seq=0), None, None, None, None, None, None, None) == 0
@@ -98,9 +99,9 @@ def test_paged_workspace_follows_what_is_asked_for():
     assert score >= plain + 3 * 8 * 6400 * 4                            # the logits
     assert need(ctypes.byref(paged(want_score=1, window=64, n_sink=4))) < score / 20      # of what the window shows
     d = paged(want_score=1)
-    assert call_paged(d, score=FAKE) == 3
-    assert call_paged(d, score=FAKE, ws=FAKE, nbytes=score - 1) == 3
-    assert call_paged(d, score=FAKE, ws=FAKE + 16, nbytes=score) == 3
+    assert call_paged(d, score=3 * FAKE) == 3
+    assert call_paged(d, score=3 * FAKE, ws=FAKE, nbytes=score - 1) == 3
+    assert call_paged(d, score=3 * FAKE, ws=FAKE + 16, nbytes=score) == 3
 
 
 def evict(**kw):
@@ -110,7 +111,7 @@ def evict(**kw):
     return binding.PagedEvictDesc(**{**base, **kw})
 
 
-def call_evict(d, k=FAKE, v=2 * FAKE, score=FAKE, table=FAKE, lens=FAKE, new_len=None, ws=None, nbytes=0):
+def call_evict(d, k=FAKE, v=2 * FAKE, score=3 * FAKE, table=4 * FAKE, lens=5 * FAKE, new_len=None, ws=None, nbytes=0):
     return lib().reform_paged_evict(ctypes.byref(d), k, v, score, None, table, lens, None, new_len, ws, nbytes, None)
 
 
@@ -131,7 +132,7 @@ def test_evict_rejects(field, value, status):
 
 def test_evict_rejects_pointers_rows_and_workspaces():
     assert call_evict(evict(max_pages=1 << 28, table_stride=1 << 28, max_len=(1 << 31) - 65535, score_head_stride=1 << 31, score_seq_stride=1 << 32)) == 2
-    for kw in (dict(k=None), dict(v=None), dict(score=None), dict(table=None), dict(lens=None), dict(v=FAKE), dict(new_len=FAKE)):
+    for kw in (dict(k=None), dict(v=None), dict(score=None), dict(table=None), dict(lens=None), dict(v=FAKE), dict(new_len=5 * FAKE), dict(new_len=3 * FAKE), dict(score=FAKE)):
         assert call_evict(evict(), **kw) == 1, kw
     assert call_evict(evict(), k=FAKE + 8) == 2
     assert call_evict(evict(head_dim=4)) == 2                            # rows of 8 bytes
