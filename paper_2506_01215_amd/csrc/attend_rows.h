@@ -254,9 +254,16 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, KEYS k, bool by_h
         } else if (last >= kg * BN && kg < ntiles) tl = (min(last / BN, ntiles - 1) - kg) / KG;       // a range may have fewer tiles than groups
     }
     int behind = -1, stay = 0;                           // as in seq_segment, of the wave's rows
+    int own[2] = {0, 0};                                 // windows: the key of the lane's own rows, less its first key of a tile
     if constexpr (WINDOW) {
         behind = M + min(row0 + 31 * rstep, r.rows - 1) / r.G - k.window;
         stay = k.sinks;
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) {
+            int head;
+            locate(nb, own[nb], head);
+            own[nb] += M - 4 * lg;
+        }
     }
     const int open = TREE ? k.open : M + row0 / r.G + 1; // keys below it are seen by all of the wave's rows
     unsigned long long *lines = (unsigned long long *)((char *)lds + S::line_at);
@@ -289,7 +296,39 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, KEYS k, bool by_h
     auto mask_tile = [&](auto &s) {
         constexpr int NB = sizeof(s) / sizeof(s[0]);
         const int j0 = key_tile(k, t * KG + kg) * BN;
-        if (j0 + BN > open || (WINDOW && j0 <= behind && j0 + BN > stay)) {
+        if constexpr (WINDOW) {
+            // a comparison and a choice for each logit and end of the window; few tiles have both ends, or first keys beside one
+            if (j0 + BN > open) {
+                asm volatile("; mask path" ::: "memory");
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    const int last = own[nb] - j0;       // keys 16 kb + e of the lane's are seen up to here ...
+#pragma unroll
+                    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[nb][kb][e] = 16 * kb + e <= last ? s[nb][kb][e] : -INFINITY;
+                }
+            }
+            if (j0 <= behind && j0 + BN > stay) {
+                asm volatile("; mask path" ::: "memory");
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    const int gone = own[nb] - j0 - k.window, front = stay - j0 - 4 * lg;    // ... and from here on, or below the first keys' end
+                    if (j0 < stay) {
+#pragma unroll
+                        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                s[nb][kb][e] = 16 * kb + e > gone || 16 * kb + e < front ? s[nb][kb][e] : -INFINITY;
+                    } else {
+#pragma unroll
+                        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[nb][kb][e] = 16 * kb + e > gone ? s[nb][kb][e] : -INFINITY;
+                    }
+                }
+            }
+        } else if (j0 + BN > open) {
             asm volatile("; mask path" ::: "memory");
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
@@ -307,7 +346,6 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, KEYS k, bool by_h
                 } else {
                     const int more = M + at - j0 - 4 * (l >> 4);         // keys behind the lane's first that are seen
                     seen = more >= 63 ? ~0ull : more < 0 ? 0ull : (2ull << more) - 1ull;
-                    if constexpr (WINDOW) seen &= window_seen(k, M + at, j0 + 4 * (l >> 4));
                 }
                 const unsigned half[2] = {(unsigned)seen, (unsigned)(seen >> 32)};
 #pragma unroll

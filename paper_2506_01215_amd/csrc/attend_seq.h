@@ -49,14 +49,6 @@ __device__ __forceinline__ int key_tile(const KEYS &k, int u)
     else return u;
 }
 
-// Bit x: key `first` + x is seen by the row at key t, of the windows' lower ends alone.
-__device__ __forceinline__ unsigned long long window_seen(const WindowKeys &k, int t, int first)
-{
-    const int gone = t - k.window - first, stay = k.sinks - first;       // keys first + x are behind the window for x <= gone, but stay for x < stay
-    const unsigned long long inside = gone < 0 ? ~0ull : gone >= 63 ? 0ull : ~0ull << (gone + 1);
-    return inside | (stay <= 0 ? 0ull : stay >= 64 ? ~0ull : (1ull << stay) - 1ull);
-}
-
 // Drafted nodes that node `lane` sees: itself and its ancestors, one bit each, one node per lane of a wave.
 // Six doublings: after step m the word holds the 2^m nearest of the line and `up` points 2^m nodes up.
 __device__ __forceinline__ unsigned long long tree_line(const int *parent, int nodes)
@@ -173,8 +165,11 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const KEYS &s, flo
     }
     const float c = scale * kLog2e;
     int behind = -1, stay = 0;                           // windows: some row does not see keys up to here, all rows see those below `stay`
+    int own[NB];                                         // and the key of the lane's own rows, less its first key of a tile
     if constexpr (WINDOW) {
-        behind = s.shift + min(r.row0 + S::R, r.rows) / r.G - s.window;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) own[nb] = s.shift + min(r.row0 + nb * 16 + ln, r.rows - 1) / r.G - 4 * lg;
+        behind = __builtin_amdgcn_readlane(own[NB - 1], 15) - s.window;          // of the block's last row
         stay = s.sinks;
     }
 
@@ -194,7 +189,28 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const KEYS &s, flo
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) x[nb][kb] = mfma16(a, qreg[nb][ks], x[nb][kb]);
             }
-        if (j0 + 31 >= s.open || (WINDOW && j0 <= behind && j0 + TK > stay)) {
+        if constexpr (WINDOW) {
+            // of the lane's keys 16 kb + e: seen up to its rows' own, and from behind their windows' ends or below the first keys'
+            if (j0 + 31 >= s.open) {
+                asm volatile("; mask path" ::: "memory");
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if ((e >> 2) * 16 + (e & 3) > own[nb] - j0) x[nb][e >> 2][e & 3] = -INFINITY;
+            }
+            if (j0 <= behind && j0 + TK > stay) {
+                asm volatile("; mask path" ::: "memory");
+                const int front = stay - j0 - 4 * lg;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int key = (e >> 2) * 16 + (e & 3);
+                        if (key <= own[nb] - j0 - s.window && key >= front) x[nb][e >> 2][e & 3] = -INFINITY;
+                    }
+            }
+        } else if (j0 + 31 >= s.open) {
             asm volatile("; mask path" ::: "memory");
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
@@ -212,7 +228,6 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const KEYS &s, flo
                 } else {
                     const int more = s.shift + at - j0 - first;    // keys behind the lane's first that are seen
                     seen = more >= 31 ? ~0u : more < 0 ? 0u : (2u << more) - 1u;
-                    if constexpr (WINDOW) seen &= (unsigned)window_seen(s, s.shift + at, j0 + first);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e)

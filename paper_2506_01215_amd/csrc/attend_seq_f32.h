@@ -68,7 +68,7 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const KEYS &s, int
     for (int a = 0; a < NA; ++a) asm volatile("" : "+v"(q[a]));
     int behind = -1, stay = 0;                           // as in seq_segment
     if constexpr (WINDOW) {
-        behind = s.shift + min(r.row0 + kF32Rows, r.rows) / r.G - s.window;
+        behind = __builtin_amdgcn_readlane(lim, 15) - s.window;
         stay = s.sinks;
     }
     for (; t < t1; t += kF32Waves) {
