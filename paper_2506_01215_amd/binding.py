@@ -487,10 +487,14 @@ _DTYPES = _Codes({torch.float32: REFORM_F32, torch.bfloat16: REFORM_BF16})
 _I32 = torch.int32
 
 
+# The current device's index where torch has been initialised, as it has with a tensor on a GPU.
+_CURRENT = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _gpu(t):
     """The current device's index if t is there: calls launch on it, and a host tensor's address would be read by the GPU."""
     dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != _CURRENT():
         raise ValueError("all tensors have to be on the current GPU")
     return dev
 
@@ -542,7 +546,9 @@ def _scratch(query, desc, dev, workspace, first, stream):
             workspace.record_stream(stream)
     elif workspace.get_device() != dev:
         raise ValueError("all tensors have to be on the current GPU")
-    return _workspace(query, desc, None, workspace)
+    base = workspace.data_ptr()
+    off = -base % 256
+    return base + off, max(workspace.numel() - off, 0)
 
 
 ROPE_SCALING = {None: 0, "none": 0, "linear": 1, "base": 2, "parts": 3, "bands": 4}
@@ -776,37 +782,44 @@ def reform_window_attend(q, k, v, cu_q, scale, window, n_sink=0, cu_k=None, out=
 
 
 def _pool_fields(k, v, page_table, score, max_len, n_seq, Hkv):
-    """What the calls on caches in pages have in common: (head_dim, page_len, n_pages, max_pages, max_len), the strides of
-    k and v, and those of the table and the scores."""
-    shape, ks, ps = k.shape, k.stride(), page_table.shape
-    if len(shape) != 4 or v.shape != shape or v.stride() != ks or v.dtype is not k.dtype or shape[1] != Hkv or ks[3] != 1:
+    """What the calls on caches in pages have in common: (head_dim, page_len, n_pages, max_pages, max_len), and the strides of k and
+    v, of the table and of the scores."""
+    pages, heads, page_len, d = shape = k.shape
+    ks = k.stride()
+    if v.shape != shape or v.stride() != ks or v.dtype is not k.dtype or heads != Hkv or ks[3] != 1:
         raise ValueError("k and v: alike, [pages, heads, rows, elements], elements contiguous")
-    if page_table.dtype is not _I32 or len(ps) != 2 or ps[0] != n_seq or (page_table.stride(1) != 1 and ps[1] != 1):
+    seqs, columns = page_table.shape
+    ts = page_table.stride()
+    if page_table.dtype is not _I32 or seqs != n_seq or (ts[1] != 1 and columns != 1):
         raise ValueError("page_table: [sequences, pages] int32, a sequence's pages contiguous")
-    most, ss = ps[1] * shape[2], (0, 0, 1)
-    if score is not None:
-        rows, ss = score.shape, score.stride()
-        if len(rows) != 3 or rows[0] != n_seq or rows[1] != Hkv or score.dtype is not torch.float32 or (ss[2] != 1 and rows[2] != 1):
-            raise ValueError("score: [sequences, KV heads, keys] fp32, a head's keys contiguous")
-        most = min(most, rows[2])
+    if score is None:
+        if max_len is None:
+            max_len = min(columns * page_len, _MOST_KEYS)
+        return (d, page_len, pages, columns, max_len), (ks[0], ks[1], ks[2], ts[0], 0, 0)
+    seqs, heads, room = score.shape
+    ss = score.stride()
+    if seqs != n_seq or heads != Hkv or score.dtype is not torch.float32 or (ss[2] != 1 and room != 1):
+        raise ValueError("score: [sequences, KV heads, keys] fp32, a head's keys contiguous")
     if max_len is None:
-        max_len = min(most, (1 << 31) - 65536)
-    elif score is not None and max_len > rows[2]:
+        max_len = min(columns * page_len, room, _MOST_KEYS)
+    elif max_len > room:
         raise ValueError("score: max_len keys at least")
-    return (shape[3], shape[2], shape[0], ps[1], max_len), ks[:3], (page_table.stride(0), ss[0], ss[1])
+    return (d, page_len, pages, columns, max_len), (ks[0], ks[1], ks[2], ts[0], ss[0], ss[1])
+
+
+_MOST_KEYS = (1 << 31) - 65536
 
 
 def _paged_fields(q, k, v, out, page_table, scale, window, n_sink, score, accumulate, max_len):
     S, Hq, d = shape = q.shape
-    qs, os = q.stride(), out.stride()
-    if out.shape != shape or k.dtype is not q.dtype or out.dtype is not q.dtype or qs[2] != 1 or os[2] != 1:
+    qs, os, dtype, Hkv = q.stride(), out.stride(), q.dtype, k.shape[1]
+    if out.shape != shape or k.dtype is not dtype or out.dtype is not dtype or qs[2] != 1 or os[2] != 1:
         raise ValueError("q and out: [sequences, heads, elements], of k's type, elements contiguous")
-    Hkv = k.shape[1]
-    pool, kvs, strides = _pool_fields(k, v, page_table, score, max_len, S, Hkv)
+    pool, strides = _pool_fields(k, v, page_table, score, max_len, S, Hkv)
     if pool[0] != d:
         raise ValueError("k: as many elements as q")
-    return (_DTYPES[q.dtype], S, Hq, Hkv, *pool, window, n_sink, score is not None, bool(accumulate), scale, 0,
-            qs[0], qs[1], os[0], os[1], *kvs, *strides)
+    return (_DTYPES[dtype], S, Hq, Hkv, *pool, window, n_sink, score is not None, bool(accumulate), scale, 0,
+            qs[0], qs[1], os[0], os[1], *strides)
 
 
 def paged_desc(q, k, v, out, page_table, scale, window=0, n_sink=0, score=None, accumulate=False, max_len=None):
@@ -829,18 +842,20 @@ def reform_paged_attend(q, k, v, page_table, cache_len, scale, window=0, n_sink=
     if lse.dtype is not torch.float32 or lse.numel() != S * fields[2] or not lse.is_contiguous():
         raise ValueError("lse: [sequences, heads] fp32")
     dev = _gpu(q)
+    if k.get_device() != dev or v.get_device() != dev or page_table.get_device() != dev or out.get_device() != dev or lse.get_device() != dev:
+        raise ValueError("all tensors have to be on the current GPU")
     desc = _pack_paged(*fields)
     ws, ws_bytes = _scratch(lib.reform_paged_attend_workspace, desc, dev, workspace, q, stream)
-    rc = lib.reform_paged_attend(desc, q.data_ptr(), _at(k, dev), _at(v, dev), _at(page_table, dev), _i32(cache_len, S, dev, "cache_len"),
-                                 _at(score, dev), _at(out, dev), _at(lse, dev), ws, ws_bytes, _stream_of(stream, dev))
+    rc = lib.reform_paged_attend(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), page_table.data_ptr(), _i32(cache_len, S, dev, "cache_len"),
+                                 _at(score, dev), out.data_ptr(), lse.data_ptr(), ws, ws_bytes, _stream_of(stream, dev))
     _check(rc, "reform_paged_attend")
     return out, lse
 
 
 def _paged_evict_fields(k, v, score, page_table, budget, n_sink, n_recent, max_len):
-    S, Hkv = score.shape[:2]
-    pool, kvs, strides = _pool_fields(k, v, page_table, score, max_len, S, Hkv)
-    return (_DTYPES[k.dtype], S, Hkv, *pool, budget, n_sink, n_recent, *kvs, *strides)
+    S, Hkv, _ = score.shape
+    pool, strides = _pool_fields(k, v, page_table, score, max_len, S, Hkv)
+    return (_DTYPES[k.dtype], S, Hkv, *pool, budget, n_sink, n_recent, *strides)
 
 
 def paged_evict_desc(k, v, score, page_table, budget, n_sink=0, n_recent=0, max_len=None):
@@ -860,9 +875,11 @@ def reform_paged_evict(k, v, score, page_table, cache_len, budget, n_sink=0, n_r
     if pos is not None and (pos.dtype is not _I32 or pos.shape != score.shape or pos.stride() != score.stride()):
         raise ValueError("pos: int32, shape and strides of score")
     dev = _gpu(k)
+    if v.get_device() != dev or score.get_device() != dev or page_table.get_device() != dev:
+        raise ValueError("all tensors have to be on the current GPU")
     desc = _pack_paged_evict(*fields)
     ws, ws_bytes = _scratch(lib.reform_paged_evict_workspace, desc, dev, workspace, k, stream)
-    rc = lib.reform_paged_evict(desc, k.data_ptr(), _at(v, dev), _at(score, dev), _at(pos, dev), _at(page_table, dev),
+    rc = lib.reform_paged_evict(desc, k.data_ptr(), v.data_ptr(), score.data_ptr(), _at(pos, dev), page_table.data_ptr(),
                                 _i32(cache_len, S, dev, "cache_len"), _i32(kept_idx, S * Hkv * budget, dev, "kept_idx"),
                                 _i32(new_len, S, dev, "new_len"), ws, ws_bytes, _stream_of(stream, dev))
     _check(rc, "reform_paged_evict")
