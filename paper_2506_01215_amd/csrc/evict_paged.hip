@@ -29,6 +29,12 @@ constexpr int kStageThreads = 512;
 
 __device__ __forceinline__ int clamped_len(const PagedEvictParams &p, int b) { return min(max(p.cache_len[b], 0), p.max_len); }
 
+// Lanes below this one that are in the mask.
+__device__ __forceinline__ int lanes_below(unsigned long long mask)
+{
+    return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
+}
+
 // The scores are compared as ordered integers (ordered_key).  Each pass counts the candidates inside [lo, hi] in 2048 bins of equal
 // width and goes on with the bin that holds the need-th largest, so three passes decide 32 bits, two where the scores spread
 // over less than 22.
@@ -102,16 +108,15 @@ __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
     while (want > 0 && !all && lo < hi) {                // the bins are 0
         const uint32_t range = hi - lo;
         const int shift = max(21 - __clz((int)range), 0);                    // range >> shift < 2048
+        // keys that many share would queue for one bin: the smallest (of scores: 0) is the likeliest, and is counted in a register
+        int least = 0;
         keys([&](int i, uint32_t u) {
-            const bool is = i + lane < i1 && u - lo <= range;
-            // scores that many keys share (0 above all) would queue for one bin: the lanes of the first one's bin add up first
-            const int bin = is ? (int)((u - lo) >> shift) : -1;
-            const unsigned long long any = __builtin_amdgcn_ballot_w64(is);
-            if (any == 0ull) return;
-            const int leader = __builtin_ctzll(any), common = __builtin_amdgcn_readlane(bin, leader);
-            const unsigned long long same = __builtin_amdgcn_ballot_w64(bin == common);
-            if (lane == leader || (is && bin != common)) atomicAdd(&bins[bin], lane == leader ? (int)__builtin_popcountll(same) : 1);
+            const uint32_t x = u - lo;
+            const bool is = i + lane < i1 && x <= range;
+            least += (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(is && x == 0u));
+            if (is && x != 0u) atomicAdd(&bins[x >> shift], 1);
         });
+        if (lane == 0 && least > 0) atomicAdd(&bins[0], least);
         __syncthreads();
         // bins from the largest down, PER to a thread
         int count[PER], own = 0;
@@ -165,14 +170,20 @@ __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
     rank += min(ties, need);
     int first = INT_MAX;                                 // first key that goes
     keys([&](int i, uint32_t u) {
-        const bool is = i + lane < i1, over = is && u > hi, same = is && u >= lo && u <= hi;
-        const unsigned long long below = (1ull << lane) - 1ull, tied = __builtin_amdgcn_ballot_w64(same);
-        const bool stays = over || (same && ties + __builtin_popcountll(tied & below) < need);
-        const unsigned long long mask = __builtin_amdgcn_ballot_w64(stays), gone = __builtin_amdgcn_ballot_w64(is && !stays);
-        if (stays) kept[rank + __builtin_popcountll(mask & below)] = p.n_sink + i + lane;
-        if (gone && first == INT_MAX) first = p.n_sink + i + __builtin_ctzll(gone);
+        const bool is = i + lane < i1, same = is && u >= lo && u <= hi;
+        bool stays = is && u > hi;
+        const unsigned long long tied = __builtin_amdgcn_ballot_w64(same);
+        if (tied != 0ull) {
+            stays = stays || (same && ties + lanes_below(tied) < need);
+            ties += __builtin_popcountll(tied);
+        }
+        const unsigned long long mask = __builtin_amdgcn_ballot_w64(stays);
+        if (stays) kept[rank + lanes_below(mask)] = p.n_sink + i + lane;
         rank += __builtin_popcountll(mask);
-        ties += __builtin_popcountll(tied);
+        if (first == INT_MAX) {
+            const unsigned long long gone = __builtin_amdgcn_ballot_w64(is && !stays);
+            if (gone != 0ull) first = p.n_sink + i + __builtin_ctzll(gone);
+        }
     });
     for (int r = tid; r < p.n_sink; r += NT) kept[r] = r;
     for (int r = tid; r < p.n_recent; r += NT) kept[p.budget - p.n_recent + r] = n - p.n_recent + r;
