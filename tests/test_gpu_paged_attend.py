@@ -126,11 +126,31 @@ def test_long_and_ragged(dtype, d, hq, hkv):
     run_case(4, 1, d, [20000], 128, dtype, seed=5, window=15000, sinks=1000, score=True)
 
 
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F, 64)])
+def test_more_items_than_shares(dtype, d):
+    """Hundreds of sequences, a few of them long: shares hold many items, and pieces are found by the shares' ends."""
+    rnd = random.Random(9)
+    lens = [rnd.choice([0, 1, 5, rnd.randint(0, 60)]) for _ in range(290)]
+    for i in (0, 77, 78, 150, 289):
+        lens[i] = rnd.randint(2600, 3000)
+    run_case(4, 2, d, lens, 32, dtype, seed=6, score=True)
+    run_case(2, 2, d, lens, 16, dtype, seed=7)
+
+
 def test_table_wider_than_the_sequences():
     """The plan goes by what the lengths may be, the result by what they are."""
     run_case(8, 2, 128, [50, 0, 3], 16, BF, seed=1, columns=900, score=True)
     run_case(8, 2, 64, [50, 0, 300], 16, BF, seed=1, columns=900, max_len=310, score=False)
     run_case(8, 2, 64, [50, 0, 300], 16, F, seed=1, columns=900, score=True)
+
+
+@pytest.mark.parametrize("d,page_len", [(128, 16), (128, 20), (64, 16), (64, 20)])
+@pytest.mark.parametrize("window", [0, 3000])
+def test_calls_that_may_read_much(d, page_len, window):
+    """Tables that have room for 64 MB of keys and values: read past the caches' usual order."""
+    columns = 9000 // page_len * 128 // d * 4
+    run_case(8, 2, d, [6000, 1, 0, 333, 2700], page_len, BF, seed=d, columns=columns, window=window, sinks=7 if window else 0, score=True)
+    run_case(14, 2, d, [17, 4000], page_len, BF, seed=d + 1, columns=3 * columns, window=2 * window, score=None)
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
