@@ -39,8 +39,8 @@ __device__ __forceinline__ int lanes_below(unsigned long long mask)
 // width and goes on with the bin that holds the need-th largest, so three passes decide 32 bits, two where the scores spread
 // over less than 22.
 //
-// A wave has a run of candidates, K times 64 of which stay in its lanes' registers (K = 0: every pass reads them again, eight loads
-// on their way at once), so that a pass is its additions to LDS and the workgroup's barriers.
+// A wave has a run of candidates.  Up to K times 64 of them stay in its lanes' registers, so that a pass is its additions to LDS and the
+// workgroup's barriers; of longer rows every pass reads them again, eight loads on their way at once.
 template <int NT, int K>
 __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
 {
@@ -61,9 +61,10 @@ __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
     const float *score = p.score + (size_t)b * p.score_ss + (size_t)g * p.score_hs + p.n_sink;
     const int m = n - p.n_sink - p.n_recent, want = p.budget - p.n_sink - p.n_recent;      // candidates, and how many stay
     const int each = ((m + NW - 1) / NW + 63) / 64 * 64, i0 = min(wave * each, m), i1 = min(i0 + each, m);
-    uint32_t mine[K > 0 ? K : 1];
-    {
-        float s[K > 0 ? K : 1];                          // all on their way before the first is looked at
+    const bool kept_here = each <= 64 * K;
+    uint32_t mine[K];
+    if (kept_here) {
+        float s[K];                                      // all on their way before the first is looked at
 #pragma unroll
         for (int x = 0; x < K; ++x) s[x] = score[min(i0 + 64 * x + lane, m - 1)];
 #pragma unroll
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
     }
     // f(first candidate of 64, the lane's key): the wave's candidates in order
     auto keys = [&](auto f) {
-        if constexpr (K > 0) {
+        if (kept_here) {
 #pragma unroll
             for (int x = 0; x < K; ++x)
                 if (i0 + 64 * x < i1) f(i0 + 64 * x, mine[x]);
@@ -359,8 +360,7 @@ hipError_t paged_evict_launch(const PagedEvictParams &p, hipStream_t st)
     const int items = p.n_seq * p.Hkv, most = p.max_len - p.n_sink - p.n_recent;
     if (most <= 2048) hipLaunchKernelGGL((paged_select<256, 8>), dim3(items), dim3(256), 0, st, p);
     else if (most <= 8192) hipLaunchKernelGGL((paged_select<1024, 8>), dim3(items), dim3(1024), 0, st, p);
-    else if (most <= 32768) hipLaunchKernelGGL((paged_select<1024, 32>), dim3(items), dim3(1024), 0, st, p);
-    else hipLaunchKernelGGL((paged_select<1024, 0>), dim3(items), dim3(1024), 0, st, p);
+    else hipLaunchKernelGGL((paged_select<1024, 32>), dim3(items), dim3(1024), 0, st, p);
     if (p.max_len <= p.budget) return hipGetLastError();
     const int slices = (p.row_bytes + kMoveLanes * 16 - 1) / (kMoveLanes * 16), parts = 2 * slices * p.segs + (p.pos ? 2 : 1);
     if (p.segs > 1) {
