@@ -11,7 +11,7 @@
 // that a segment needs of the next one's are set aside first (paged_stage, a launch between the two).
 //
 // Bound: reading and writing the rows that move.  Cold caches, all rows moving: 112 heads from 4352 to 4096 rows of 128 elements bf16
-// 440 MB in 102 us, 4.3 TB/s (a large copy: 4.9), and 10 for the selection; 8 heads from 33024 to 32768 266 MB in 66 us, 28 for the selection, which
+// 440 MB in 102 us, 4.3 TB/s (a large copy: 4.9), and 8 for the selection; 8 heads from 33024 to 32768 266 MB in 66 us, 16 for the selection, which
 // has one compute unit for each head.  Rows pass the caches' usual order of replacement (114 -> 103 us).  Chunks of 1024 threads x 4 x 16 bytes
 // against 512 x 8: 95 against 103; twice as deep 150; with the next chunk's loads before this one's stores 109; 64 bytes of a row to a
 // workgroup 142, 256 more than twice as slow for few items.
@@ -23,7 +23,7 @@ namespace reform {
 
 namespace {
 
-constexpr int kSelBins = 2048;
+constexpr int kSelBins = 2048, kSelGroup = 4;
 constexpr int kMoveThreads = 1024, kMoveLanes = 8, kMoveDeep = 4;        // a chunk: 512 rows of 128 bytes, 64 bytes a thread
 constexpr int kStageThreads = 512;
 
@@ -35,18 +35,36 @@ __device__ __forceinline__ int lanes_below(unsigned long long mask)
     return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
 }
 
+// ordered_key in fewer instructions (-0 + 0 is 0), and 1 at least.
+__device__ __forceinline__ uint32_t candidate_key(float f)
+{
+    const int u = __float_as_int(f + 0.f);
+    return max((uint32_t)u ^ ((uint32_t)(u >> 31) | 0x80000000u), 1u);
+}
+
+// What the waves before this one counted: one read and a scan, where a loop would wait for each of up to 15 reads.
+__device__ __forceinline__ int waves_before(const int *counts, int lane, int wave)
+{
+    return __builtin_amdgcn_readlane(row_incl_scan(lane < wave ? counts[lane] : 0), 15);
+}
+
 // The scores are compared as ordered integers (ordered_key).  Each pass counts the candidates inside [lo, hi] in 2048 bins of equal
 // width and goes on with the bin that holds the need-th largest, so three passes decide 32 bits, two where the scores spread
 // over less than 22.
 //
 // A wave has a run of candidates.  Up to K times 64 of them stay in its lanes' registers, so that a pass is its additions to LDS and the
-// workgroup's barriers; of longer rows every pass reads them again, eight loads on their way at once.
+// workgroup's barriers; of longer rows every pass reads them again, the next eight loads on their way meanwhile.
+//
+// What bounds it is the instructions of 16 waves on one compute unit, scalar ones as much as vector ones, so each step over 64 keys
+// has few of both and no branch of its own: 8 heads of 33024 keys 28 -> 19 us in a trace, 128 of up to 4352 10.8 -> 8.4, 8 heads of
+// 131328 148 -> 83 (groups of kSelGroup keys: 1 21.0, 9.2; 2 19.4, 8.6; 4 18.9, 8.4; 8 18.9, 9.5).  The rest are the first reads, 4 us, and
+// barriers.
 template <int NT, int K>
 __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
 {
     constexpr int NW = NT / 64, PER = kSelBins / NT;     // waves; bins of a thread
     __shared__ int bins[kSelBins];
-    __shared__ int sh_a[NW], sh_b[NW], sh_first[NW];
+    __shared__ int sh_a[NW], sh_b[NW];
     __shared__ uint32_t sh_lo[NW], sh_hi[NW], sh_from, sh_to;
     __shared__ int sh_need, sh_all;
     const int item = blockIdx.x, b = item / p.Hkv, g = item - b * p.Hkv;
@@ -62,36 +80,59 @@ __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
     const int m = n - p.n_sink - p.n_recent, want = p.budget - p.n_sink - p.n_recent;      // candidates, and how many stay
     const int each = ((m + NW - 1) / NW + 63) / 64 * 64, i0 = min(wave * each, m), i1 = min(i0 + each, m);
     const bool kept_here = each <= 64 * K;
+    // a key is 1 at least, 0 where there is no candidate: outside every [lo, hi] and above none
+    auto key = [&](int i, float s) { return i + lane < i1 ? candidate_key(s) : 0u; };
     uint32_t mine[K];
     if (kept_here) {
         float s[K];                                      // all on their way before the first is looked at
 #pragma unroll
         for (int x = 0; x < K; ++x) s[x] = score[min(i0 + 64 * x + lane, m - 1)];
 #pragma unroll
-        for (int x = 0; x < K; ++x) mine[x] = ordered_key(s[x]);
+        for (int x = 0; x < K; ++x) mine[x] = key(i0 + 64 * x, s[x]);
     }
     // f(first candidate of 64, the lane's key): the wave's candidates in order
     auto keys = [&](auto f) {
         if (kept_here) {
 #pragma unroll
-            for (int x = 0; x < K; ++x)
-                if (i0 + 64 * x < i1) f(i0 + 64 * x, mine[x]);
+            for (int x = 0; x < K; x += kSelGroup)
+                if (i0 + 64 * x < i1) {
+#pragma unroll
+                    for (int y = 0; y < kSelGroup; ++y) f(i0 + 64 * (x + y), mine[x + y]);
+                }
         } else {
+            float next[8];
+            auto load = [&](int i) {
+                if (i + 512 <= m) {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) next[x] = (score + i)[64 * x + lane];
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) next[x] = score[min(i + 64 * x + lane, m - 1)];
+                }
+            };
+            load(i0);
             for (int i = i0; i < i1; i += 512) {
                 float s[8];
 #pragma unroll
-                for (int x = 0; x < 8; ++x) s[x] = score[min(i + 64 * x + lane, m - 1)];
+                for (int x = 0; x < 8; ++x) s[x] = next[x];
+                load(i + 512);
+                if (i + 512 <= i1) {
 #pragma unroll
-                for (int x = 0; x < 8; ++x)
-                    if (i + 64 * x < i1) f(i + 64 * x, ordered_key(s[x]));
+                    for (int x = 0; x < 8; ++x) f(i + 64 * x, candidate_key(s[x]));
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) f(i + 64 * x, key(i + 64 * x, s[x]));
+                }
             }
         }
     };
     uint32_t lo = ~0u, hi = 0u;
-    keys([&](int, uint32_t u) {                          // others' keys among them do no harm
-        lo = min(lo, u);
+    keys([&](int, uint32_t u) {
+        lo = min(lo, u - 1u);                            // 0, no candidate, is the largest then
         hi = max(hi, u);
     });
+    lo += 1u;
+    if (lo == 0u) lo = ~0u;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
         lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
@@ -111,11 +152,10 @@ __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
         const int shift = max(21 - __clz((int)range), 0);                    // range >> shift < 2048
         // keys that many share would queue for one bin: the smallest (of scores: 0) is the likeliest, and is counted in a register
         int least = 0;
-        keys([&](int i, uint32_t u) {
+        keys([&](int, uint32_t u) {
             const uint32_t x = u - lo;
-            const bool is = i + lane < i1 && x <= range;
-            least += (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(is && x == 0u));
-            if (is && x != 0u) atomicAdd(&bins[x >> shift], 1);
+            least += (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(x == 0u));
+            if (x - 1u < range) atomicAdd(&bins[x >> shift], 1);
         });
         if (lane == 0 && least > 0) atomicAdd(&bins[0], least);
         __syncthreads();
@@ -130,8 +170,7 @@ __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
         const int incl = wave_incl_scan(own);
         if (lane == 63) sh_a[wave] = incl;
         __syncthreads();
-        int above = incl - own;
-        for (int w = 0; w < wave; ++w) above += sh_a[w];
+        int above = incl - own + waves_before(sh_a, lane, wave);
         if (above < need && need <= above + own) {
 #pragma unroll
             for (int x = 0; x < PER; ++x) {
@@ -153,47 +192,48 @@ __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
     }
     // stay: above hi; inside [lo, hi] (one value, or all of them stay) the first `need`
     if (want == 0) { lo = 1u; hi = ~0u; need = 0; }
+    const uint32_t range = hi - lo;
     int stay = 0, tie = 0;
-    keys([&](int i, uint32_t u) {
-        stay += i + lane < i1 && u > hi;
-        tie += i + lane < i1 && u >= lo && u <= hi;
+    keys([&](int, uint32_t u) {
+        stay += u > hi;
+        tie += u - lo <= range;
     });
     stay = __builtin_amdgcn_readlane(wave_incl_scan(stay), 63);
     tie = __builtin_amdgcn_readlane(wave_incl_scan(tie), 63);
     __syncthreads();                                     // sh_a has been read
     if (lane == 0) { sh_a[wave] = stay; sh_b[wave] = tie; }
     __syncthreads();
-    int rank = p.n_sink, ties = 0;
-    for (int w = 0; w < wave; ++w) {
-        rank += sh_a[w];
-        ties += sh_b[w];
+    const int stay0 = waves_before(sh_a, lane, wave), tie0 = waves_before(sh_b, lane, wave), rank = stay0 + min(tie0, need);
+    int32_t *const to = kept + p.n_sink + rank;
+    unsigned at = 0u;                                    // kept keys of the wave so far
+    auto keep = [&](int i, unsigned long long stays) {
+        if (__builtin_amdgcn_inverse_ballot_w64(stays))
+            *(int32_t *)((char *)to + 4u * (at + (unsigned)lanes_below(stays))) = p.n_sink + i + lane;
+        at += (unsigned)__builtin_popcountll(stays);
+    };
+    const bool first_goes = rank == i0 && stay0 + stay + min(tie0 + tie, need) < i1;         // no key of the waves before goes
+    int first = INT_MAX;                                 // key that goes, with first_goes
+    auto goes = [&](int i, unsigned long long stays) {
+        if (first == INT_MAX && ~stays != 0ull) first = i + __builtin_ctzll(~stays);
+    };
+    if (tie0 >= need || tie0 + tie <= need) {            // the wave's ties all go, or all stay
+        const uint32_t over = tie0 < need ? lo - 1u : hi;
+        keys([&](int i, uint32_t u) { keep(i, __builtin_amdgcn_ballot_w64(u > over)); });
+        if (first_goes) keys([&](int i, uint32_t u) { goes(i, __builtin_amdgcn_ballot_w64(u > over)); });
+    } else {
+        int left = need - tie0;
+        keys([&](int i, uint32_t u) {
+            unsigned long long stays = __builtin_amdgcn_ballot_w64(u > hi);
+            const unsigned long long tied = __builtin_amdgcn_ballot_w64(u - lo <= range);
+            stays |= tied & __builtin_amdgcn_ballot_w64(lanes_below(tied) < left);
+            left -= (int)__builtin_popcountll(tied);
+            keep(i, stays);
+            goes(i, stays);
+        });
     }
-    rank += min(ties, need);
-    int first = INT_MAX;                                 // first key that goes
-    keys([&](int i, uint32_t u) {
-        const bool is = i + lane < i1, same = is && u >= lo && u <= hi;
-        bool stays = is && u > hi;
-        const unsigned long long tied = __builtin_amdgcn_ballot_w64(same);
-        if (tied != 0ull) {
-            stays = stays || (same && ties + lanes_below(tied) < need);
-            ties += __builtin_popcountll(tied);
-        }
-        const unsigned long long mask = __builtin_amdgcn_ballot_w64(stays);
-        if (stays) kept[rank + lanes_below(mask)] = p.n_sink + i + lane;
-        rank += __builtin_popcountll(mask);
-        if (first == INT_MAX) {
-            const unsigned long long gone = __builtin_amdgcn_ballot_w64(is && !stays);
-            if (gone != 0ull) first = p.n_sink + i + __builtin_ctzll(gone);
-        }
-    });
+    if (first_goes && lane == 0) p.first[item] = p.n_sink + first;
     for (int r = tid; r < p.n_sink; r += NT) kept[r] = r;
     for (int r = tid; r < p.n_recent; r += NT) kept[p.budget - p.n_recent + r] = n - p.n_recent + r;
-    if (lane == 0) sh_first[wave] = first;
-    __syncthreads();
-    if (tid == 0) {
-        for (int w = 0; w < NW; ++w) first = min(first, sh_first[w]);
-        p.first[item] = first;
-    }
 }
 
 // Ranks [r0, r1) of one segment's rows, LANES threads of 16 bytes to a row.  Three things of a row follow from each other: which key it

@@ -51,6 +51,9 @@ def scores_of(kind, g, shape):
         return torch.full(shape, 0.25)
     if kind == "signs":                                                  # both zeros are alike, negative ones come last
         return torch.randint(-3, 3, shape, generator=g).float() * torch.where(torch.rand(shape, generator=g) < 0.3, -0.0, 1.0)
+    if kind == "subnormal":                                              # zeros of both signs and numbers below the smallest normal one
+        return torch.randint(-9, 200, shape, generator=g, dtype=torch.int32).clamp_min(-1).mul(3).float() * 2.0 ** -149 \
+            * torch.where(torch.rand(shape, generator=g) < 0.3, -0.0, 1.0)
     return torch.rand(shape, generator=g) * 1e-30 + 1.0 * (torch.rand(shape, generator=g) < 0.1)      # far apart
 
 
@@ -227,3 +230,15 @@ def test_the_first_rows_go():
     binding.reform_paged_evict(dk, dv, ds, i32(table), i32([n]), budget, pos=dp)
     for x, y in zip((dk, dv, ds, dp), want):
         assert torch.equal(x.cpu(), y)
+
+
+@pytest.mark.parametrize("lens,budget", [([384, 300], 256), ([9000], 8200), ([40000], 39000), ([36000], 700)])
+def test_subnormal_scores(lens, budget):
+    run_case(1, 64, lens, 64, budget, 4, 10, BF, seed=budget, kind="subnormal")
+
+
+@pytest.mark.parametrize("kind", ["equal", "signs", "apart"])
+def test_long_rows_of_other_scores(kind):
+    """Rows that are read anew in every pass: runs of candidates that end inside 512 and inside 64."""
+    for n, budget in ((32900 + 14, 32000), (33800, 33700), (50001, 25000)):
+        run_case(1, 64, [n], 64, budget, 4, 10, BF, seed=n, kind=kind)
