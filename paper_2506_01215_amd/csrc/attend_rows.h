@@ -249,15 +249,15 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, KEYS k, bool by_h
     int tl = -1;                                         // last tile of the group that the wave needs
     if (row0 < r.rows) {
         const int last = TREE ? k.n - 1 : M + min(row0 + 31 * rstep, r.rows - 1) / r.G;       // prompts have no thin waves
-        if constexpr (WINDOW) {                          // the last key lies behind the first keys' run, or there is one run
-            if (last >= 0 && last / BN - k.skip >= kg && kg < ntiles) tl = (min(last / BN - k.skip, ntiles - 1) - kg) / KG;
+        if constexpr (WINDOW) {                          // the last key is of the second run, or there is one run
+            if (last >= 0 && (last - k.skip) / BN >= kg && kg < ntiles) tl = (min((last - k.skip) / BN, ntiles - 1) - kg) / KG;
         } else if (last >= kg * BN && kg < ntiles) tl = (min(last / BN, ntiles - 1) - kg) / KG;       // a range may have fewer tiles than groups
     }
     int behind = -1, stay = 0;                           // as in seq_segment, of the wave's rows
     int own[2] = {0, 0};                                 // windows: the key of the lane's own rows, less its first key of a tile
     if constexpr (WINDOW) {
         behind = M + min(row0 + 31 * rstep, r.rows - 1) / r.G - k.window;
-        stay = k.sinks;
+        stay = k.stay;
 #pragma unroll
         for (int nb = 0; nb < 2; ++nb) {
             int head;
@@ -281,7 +281,7 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, KEYS k, bool by_h
         asm volatile("" : "+v"(l));                      // as in locate
 #pragma unroll
         for (int i = 0; i < S::LOADS; ++i) {
-            const int row = min(key_tile(k, t * KG + kg) * BN + wave + S::lane_row(l) + i * NW, k.n - 1);
+            const int row = min(key_of(k, (t * KG + kg) * BN + wave + S::lane_row(l) + i * NW), k.n - 1);
             load_to_lds((const char *)((const u16 *)k.k + (size_t)row * k.k_rs + l % C8 * 8), to_k + i * NW * S::PITCH);
             load_to_lds((const char *)((const u16 *)k.v + (size_t)row * k.v_rs + l % C8 * 8), to_v + i * NW * S::PITCH);
         }
@@ -295,7 +295,7 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, KEYS k, bool by_h
     int t = 0, kslot = 0, vslot = 0;                     // the slots of tile t: t mod KSLOTS, t mod VSLOTS
     auto mask_tile = [&](auto &s) {
         constexpr int NB = sizeof(s) / sizeof(s[0]);
-        const int j0 = key_tile(k, t * KG + kg) * BN;
+        const int j0 = key_start<BN>(k, t * KG + kg);
         if constexpr (WINDOW) {
             // a comparison and a choice for each logit and end of the window; few tiles have both ends, or first keys beside one
             if (j0 + BN > open) {
@@ -365,13 +365,13 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, KEYS k, bool by_h
         asm volatile("" ::: "memory");
         auto after = [](int slot, int by, int slots) { const int x = slot + by; return x >= slots ? x - slots : x; };
         const int next = (t + 1) * KG + kg;
-        const bool more = next < ntiles, whole = (key_tile(k, next) + 1) * BN <= k.n;
+        const int j1 = key_start<BN>(k, next);
+        const bool more = next < ntiles, whole = j1 + BN <= k.n && !key_split<BN>(k, next);
         u16 *const nk = wk + (kslot ^ 1) * TILE, *const nv = wv + after(vslot, 1, S::VSLOTS) * TILE;
         if (more && !whole) load_end(t + 1, nk, nv);
-        const size_t j1 = (size_t)key_tile(k, next) * BN;
         const int vread = STEP == kRowsLag || STEP == kRowsLast ? after(vslot, S::VSLOTS - 1, S::VSLOTS) : vslot;
         rows_tile<D, NW, KG, STEP, NB>(w, ldsK + kslot * TILE, ldsV + vread * TILE, nk, nv,
-                                      (const char *)((const u16 *)k.k + j1 * k.k_rs) + koff, (const char *)((const u16 *)k.v + j1 * k.v_rs) + voff,
+                                      (const char *)((const u16 *)k.k + (size_t)j1 * k.k_rs) + koff, (const char *)((const u16 *)k.v + (size_t)j1 * k.v_rs) + voff,
                                       step_k, step_v, more && whole, c, mask_tile);
         kslot ^= 1;
         vslot = after(vslot, 1, S::VSLOTS);

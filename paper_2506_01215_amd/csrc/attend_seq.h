@@ -35,18 +35,33 @@ struct SeqKeys {
 };
 
 // Prompts with a sliding window: query row i, at key t = i + shift, sees j <= t with j > t - window or j < sinks.  A block goes through
-// two runs of tiles, those of the first keys and those of its rows' windows, counted through: tile number u is tile u below `front`,
-// u + skip from there on.
+// two runs of keys, the first ones and those that its rows' windows show, counted through: places below `cut` are the keys of these
+// numbers, those from there on the keys `skip` further.  Tiles are cut from the places, so that few keys of them are not seen by any row:
+// one tile may have keys of both runs, and only there rows are addressed one by one.
 struct WindowKeys : SeqKeys {
-    int window, sinks, front, skip;
+    int window, cut, skip;   // skip = 0: cut = 0
+    int stay;                // keys below it that lie in a tile are seen by all rows, unless they are behind the row's own
 };
 
-// Tile number u of a range of keys.
-template <class KEYS>
-__device__ __forceinline__ int key_tile(const KEYS &k, int u)
+// Tile u of TK places: its first key (with keys of both runs: as if all were of the second), whether it has keys of both, and the key
+// of a place.
+template <int TK, class KEYS>
+__device__ __forceinline__ int key_start(const KEYS &k, int u)
 {
-    if constexpr (std::is_same<KEYS, WindowKeys>::value) return u < k.front ? u : u + k.skip;
-    else return u;
+    if constexpr (std::is_same<KEYS, WindowKeys>::value) return u * TK + (u * TK + TK > k.cut ? k.skip : 0);
+    else return u * TK;
+}
+template <int TK, class KEYS>
+__device__ __forceinline__ bool key_split(const KEYS &k, int u)
+{
+    if constexpr (std::is_same<KEYS, WindowKeys>::value) return u * TK < k.cut && u * TK + TK > k.cut;
+    else return false;
+}
+template <class KEYS>
+__device__ __forceinline__ int key_of(const KEYS &k, int place)
+{
+    if constexpr (std::is_same<KEYS, WindowKeys>::value) return place + (place < k.cut ? 0 : k.skip);
+    else return place;
 }
 
 // Drafted nodes that node `lane` sees: itself and its ancestors, one bit each, one node per lane of a wave.
@@ -106,11 +121,18 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const KEYS &s, flo
     const uint32_t koff = (uint32_t)((lane / C8) * (int)s.k_rs + lane % C8 * 8) * 2u;
     const uint32_t voff = (uint32_t)((lane / C8) * (int)s.v_rs + lane % C8 * 8) * 2u;
     auto load = [&](int u) {
-        const int t = key_tile(s, u);
-        const char *kt = (const char *)((const u16 *)s.k + (size_t)t * TK * s.k_rs);
-        const char *vt = (const char *)((const u16 *)s.v + (size_t)t * TK * s.v_rs);
-        const int last = s.n - 1 - t * TK;
-        if (last >= TK - 1) {
+        const int j0 = key_start<TK>(s, u);
+        const char *kt = (const char *)((const u16 *)s.k + (size_t)j0 * s.k_rs);
+        const char *vt = (const char *)((const u16 *)s.v + (size_t)j0 * s.v_rs);
+        const int last = s.n - 1 - j0;
+        if (key_split<TK>(s, u)) {
+#pragma unroll
+            for (int i = 0; i < S::PIECES; ++i) {
+                const size_t row = min(key_of(s, u * TK + lane / C8 + i * (64 / C8)), s.n - 1);
+                kreg[i] = *(const v4u *)((const u16 *)s.k + row * s.k_rs + lane % C8 * 8);
+                vreg[i] = *(const v4u *)((const u16 *)s.v + row * s.v_rs + lane % C8 * 8);
+            }
+        } else if (last >= TK - 1) {
 #pragma unroll
             for (int i = 0; i < S::PIECES; ++i) {
                 kreg[i] = *(const v4u *)(kt + (koff + (uint32_t)(i * (64 / C8) * (int)s.k_rs) * 2u));
@@ -164,18 +186,18 @@ __device__ __forceinline__ void seq_segment(const SeqRows &r, const KEYS &s, flo
         for (int db = 0; db < DB; ++db) o[nb][db] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     const float c = scale * kLog2e;
-    int behind = -1, stay = 0;                           // windows: some row does not see keys up to here, all rows see those below `stay`
+    int behind = -1, stay = 0;                           // windows: some row does not see keys up to here; see WindowKeys
     int own[NB];                                         // and the key of the lane's own rows, less its first key of a tile
     if constexpr (WINDOW) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) own[nb] = s.shift + min(r.row0 + nb * 16 + ln, r.rows - 1) / r.G - 4 * lg;
         behind = __builtin_amdgcn_readlane(own[NB - 1], 15) - s.window;          // of the block's last row
-        stay = s.sinks;
+        stay = s.stay;
     }
 
     for (; t < t1; t += NW) {
         store();
-        const int j0 = key_tile(s, t) * TK;
+        const int j0 = key_start<TK>(s, t);
         if (t + NW < t1) load(t + NW);
         const u16 *sk = mine, *sv = mine + TILE;
         f32x4 x[NB][2];

@@ -57,7 +57,7 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const KEYS &s, int
     constexpr bool AHEAD = DP <= 128;
     f32x4 k[NA];
     auto load_keys = [&](int u) {
-        const float *kr = (const float *)s.k + (size_t)min(key_tile(s, u) * kF32Keys + ln, s.n - 1) * s.k_rs + 4 * lg;
+        const float *kr = (const float *)s.k + (size_t)min(key_of(s, u * kF32Keys + ln), s.n - 1) * s.k_rs + 4 * lg;
 #pragma unroll
         for (int a = 0; a < NA; ++a) k[a] = quad(kr, a);
     };
@@ -69,14 +69,14 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const KEYS &s, int
     int behind = -1, stay = 0;                           // as in seq_segment
     if constexpr (WINDOW) {
         behind = __builtin_amdgcn_readlane(lim, 15) - s.window;
-        stay = s.sinks;
+        stay = s.stay;
     }
     for (; t < t1; t += kF32Waves) {
-        const int j0 = key_tile(s, t) * kF32Keys;
+        const int j0 = key_start<kF32Keys>(s, t);
         if (!AHEAD) load_keys(t);
         float v[4][NA];
         auto load_values = [&](int e) {
-            const float *vr = (const float *)s.v + (size_t)min(j0 + 4 * lg + e, s.n - 1) * s.v_rs + ln;
+            const float *vr = (const float *)s.v + (size_t)min(key_of(s, t * kF32Keys + 4 * lg + e), s.n - 1) * s.v_rs + ln;
 #pragma unroll
             for (int a = 0; a < NA; ++a) {
                 const bool in = 16 * a + ln < D;
@@ -97,9 +97,9 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const KEYS &s, int
         if (j0 + kF32Keys - 1 >= s.open || (WINDOW && j0 <= behind && j0 + kF32Keys > stay)) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int j = j0 + 4 * lg + e, node = j - s.open;
+                const int j = key_of(s, t * kF32Keys + 4 * lg + e), node = j - s.open;
                 bool seen = TREE ? node < 0 || (node < 64 && ((line >> (node & 63)) & 1ull)) : j <= lim;
-                if constexpr (WINDOW) seen = seen && (j > lim - s.window || j < s.sinks);
+                if constexpr (WINDOW) seen = seen && (j > lim - s.window || j < stay);
                 if (!seen) x[e] = -INFINITY;
             }
         }

@@ -1,7 +1,7 @@
 // Attention over packed prompts whose rows see a sliding window and a few first keys (see reform_window_attend in reform.h).
 //
-// The blocks of rows of attend_prompt.hip, each of which goes through two runs of key tiles: those of the first keys, and those from
-// the first key that its first row's window shows to the last that its last row sees (WindowKeys).  Only tiles at the
+// The blocks of rows of attend_prompt.hip, each of which goes through two runs of keys, the first ones and those from
+// the first key that its first row's window shows to the last that its last row sees, in tiles cut from both counted through (WindowKeys).  Only tiles at the
 // ends of the runs are masked.
 //
 //   window_attend<D,NW,KG>         blocks of 32 NW rows, all waves through the same tiles, KG groups of them (attend_rows.h)
@@ -22,11 +22,12 @@ __device__ __forceinline__ int window_operands(const WindowParams &p, const Prom
 {
     prompt_block_operands<T>(p, blk, kvh, blk.rb * ROWS, r, k);
     k.window = p.window;
-    k.sinks = p.n_sink;
     const int lo = max(k.shift + r.row0 / r.G - p.window + 1, 0);        // first key of the first row's window
-    k.front = (min(p.n_sink, lo) + TK - 1) / TK;
-    k.skip = max(lo / TK - k.front, 0);
-    return max(blk.tiles - k.skip, 0);
+    const int last = k.shift + (min(r.row0 + ROWS, r.rows) - 1) / r.G;   // last key that the block sees
+    k.skip = max(lo - p.n_sink, 0);
+    k.cut = k.skip ? p.n_sink : 0;
+    k.stay = max(lo, p.n_sink);
+    return last < 0 ? 0 : (last - k.skip) / TK + 1;
 }
 
 template <int D, int NW, int KG>
