@@ -72,8 +72,8 @@ WindowParams window_sizes(const reform_window_desc *d)
     // beyond the number of keys neither says more, and the kernels' sums with them stay within 32 bits
     p.window = d->window < d->n_k_rows ? d->window : d->n_k_rows > 0 ? d->n_k_rows : 1;
     p.n_sink = d->n_sink < d->n_k_rows ? d->n_sink : d->n_k_rows;
-    // Where all blocks have as many tiles as the window shows, their order says nothing, and finding it takes 0.3 us and more (22 sequences
-    // of together 5900 rows behind 4977 keys each, window 3, 32/8 heads of 64: 32.1 us sorted, 29.2 not; 18 of together 3300 rows, window 3743, 28/4: 24.1, 27.8).
+    // Where all blocks have as many tiles as the window shows, their order says nothing, and finding it takes 0.1 us and more (15 sequences
+    // of together 4400 rows behind 4977 keys each, window 3, 32/8 heads of 64: 27.4 us sorted, 25.3 not; 17 of together 4000 rows, window 3743, 28/4: 23.2, 27.2).
     p.sorted = 2 * (int64_t)p.window * p.n_seq > p.n_k;
     return p;
 }

@@ -5,10 +5,11 @@
 // to a block more of them are masked, and more of the time is a block's beginning and end.
 //
 // Fitted to 160 batches (30 to 17000 rows, 1 to 32 sequences, windows of 1 to 6000 keys, up to 256 first ones, with and without keys in front),
-// each in all forms: the one that is chosen takes 1.7 % more time in the mean than the best, at worst 37 %; 110 other
-// batches 3 %, at worst 46 % (30 sequences of together 154 rows, window 797, 24/8 heads of 128: 10.6 us, in blocks of 128 7.2).  Measured, us,
-// blocks of 128 / 32 / 16 at head_dim 64: 525 rows of two, window 2, 14/2 heads 9.7 / 6.7 / 9.4; blocks of 128 / 128 with two
-// groups / 32 / 16 at 128: 157 rows of four, window 305, 24/8 9.5 / 11.1 / 8.5 / 6.6; 1072 rows, window 146, 8/1 15.2 / 16.2 / 11.0 / 16.1.
+// each in all forms, when a tile of the first keys held no key of the window.  Of 280 other batches, with tiles as they are, the form that is
+// chosen takes 0.9 % more time in the mean than the best, at worst 36 % (222 rows of four, window 2, 16/2 heads of 128: blocks of 128 9.1 us, of
+// 16 6.6); costs fitted to 170 of them anew, and without the tile that first keys add, chose no better.  Measured, us,
+// blocks of 128 / 32 / 16 at head_dim 64: 525 rows of two, window 2, 14/2 heads 7.2 / 6.2 / 8.7; blocks of 128 / 128 with two
+// groups / 32 / 16 at 128: 157 rows of four, window 305, 24/8 8.5 / 10.1 / 8.3 / 6.7; 1072 rows, window 146, 8/1 11.3 / 12.4 / 9.8 / 15.1.
 #pragma once
 #include "prompt_plan.h"
 
