@@ -195,3 +195,18 @@ def test_another_stream():
     got = binding.reform_window_attend(q, k, v, cu, 0.125, 64, stream=st)
     st.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("hq,hkv,d,lens,dtype", [(8, 2, 64, [700, 650], BF), (8, 2, 64, [230], BF), (8, 1, 64, [60, 100], BF), (8, 2, 128, [720, 500], BF),
+                                                 (2, 1, 128, [2300], BF), (4, 4, 128, [190], BF), (4, 2, 64, [170], F), (2, 1, 200, [150], F)])
+@pytest.mark.parametrize("window", [1, 30, 64, 70])
+def test_tiles_of_first_keys_and_window(hq, hkv, d, lens, dtype, window):
+    """The first keys end anywhere inside a tile, whose other keys are the window's: next to them, a tile away, or further."""
+    for sinks in (1, 15, 16, 17, 31, 33, 63, 65, 100):
+        run_case(hq, hkv, d, lens, [n + (0 if sinks % 2 else 37) for n in lens], window, sinks, dtype, seed=sinks)
+
+
+def test_two_groups_of_waves_and_first_keys_inside_a_tile():
+    for sinks in (1, 33, 63, 70, 130):
+        run_case(2, 1, 128, [6164], [6164], 12, sinks, BF, seed=sinks)
+        run_case(16, 2, 128, [700, 600, 500], [700, 600, 500], 833, sinks, BF, seed=sinks)
