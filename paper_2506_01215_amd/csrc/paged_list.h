@@ -101,19 +101,18 @@ __device__ __forceinline__ void paged_score(const PagedParams &p, int b, int kvh
     }
 }
 
-constexpr int kScoreParts = 4;               // workgroups that score a share, or an item
-
-// The second launch: its first `merges` workgroups put pieces together as tree_merge does, the others score the keys of a share each.
+// The second launch: its first `merges` workgroups put pieces together as tree_merge does, the others score the keys of a share (or of an
+// item), `parts` of them each.
 template <int D, int R, int TK, bool BF16>
-__global__ __launch_bounds__(256) void paged_join(PagedParams p, int merges, int rows, int by_share)
+__global__ __launch_bounds__(256) void paged_join(PagedParams p, int merges, int rows, int by_share, int parts)
 {
     using List = TreeList<R, TK, PagedParams>;
     if ((int)blockIdx.x >= merges) {
-        const int block = ((int)blockIdx.x - merges) / kScoreParts, part = ((int)blockIdx.x - merges) % kScoreParts;
+        const int block = ((int)blockIdx.x - merges) / parts, part = ((int)blockIdx.x - merges) % parts;
         const int lane = threadIdx.x & 63, mine = 4 * part + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         int counter = 0;
         auto item = [&](int b, int len, int kvh, int t0, int t1, int w0, int n) {      // n pieces from share w0 on, or 0: finished already
-            paged_score<TK>(p, b, kvh, len, t0, t1, counter, mine, 4 * kScoreParts, [&](int r0) {
+            paged_score<TK>(p, b, kvh, len, t0, t1, counter, mine, 4 * parts, [&](int r0) {
                 const int row = min(r0 + lane, p.G - 1), rb = row / R;
                 if (n == 0) {
                     const float2 y = p.row_ml[(size_t)b * p.Hq + (size_t)kvh * p.G + row];
@@ -221,9 +220,15 @@ inline void paged_join_launch(const PagedParams &p, hipStream_t st)
     int rows = 1;                                        // as in tree_merge_launch
     while (2 * rows <= 1024 / D && rows < p.part_rows && blocks * ((p.part_rows + rows - 1) / rows) > 3l * p.units) rows *= 2;
     const long merges = p.shares ? blocks * ((p.part_rows + rows - 1) / rows) : 0;
-    const long scores = !p.logits || (p.shares == 0 && p.row_blocks == 1) ? 0 : kScoreParts * (p.shares ? p.shares : (long)p.n_seq * p.Hkv);
+    // One workgroup to a share of few logits, three to others: finding its place takes a workgroup as long as thousands of logits.  us with 1, 2, 3, 4
+    // of them: 16 caches of up to 13711 keys, 24/8 heads of 64 (10 thousand logits a share at most) 65.9, 66.8, 67.6, 70.5; 4 of up to 5028, 32/8 of 128
+    // (3) 22.8, 24.0, 24.1, 25.7; 32 of up to 8192 (33) 134.8, 134.2, 133.4, 135.8; 16 of up to 26333 (53) 250.3, 247.6, 247.1, 247.7; 32 of up to 3679,
+    // 64/1 (118) 42.9, 35.3, 35.1, 35.4
+    const long scored = p.shares ? p.shares : (long)p.n_seq * p.Hkv;
+    const int parts = (double)p.n_seq * p.Hq * p.logit_keys < 24576.0 * (double)scored ? 1 : 3;
+    const long scores = !p.logits || (p.shares == 0 && p.row_blocks == 1) ? 0 : parts * scored;
     if (merges + scores)
-        hipLaunchKernelGGL((paged_join<D, R, TK, BF16>), dim3((unsigned)(merges + scores)), dim3(256), 0, st, p, (int)merges, rows, (int)by_share);
+        hipLaunchKernelGGL((paged_join<D, R, TK, BF16>), dim3((unsigned)(merges + scores)), dim3(256), 0, st, p, (int)merges, rows, (int)by_share, parts);
 }
 
 // Keys that the longest sequence may go through, in whole tiles of 32, and the list for blocks of R rows and tiles of TK keys (list_plan).
