@@ -47,6 +47,14 @@ __device__ __forceinline__ float2 score_row(float m, float l)
     return make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.0f / l);
 }
 
+// A row's reference (log2 units) and sum with another piece's.
+__device__ __forceinline__ void add_piece(float &m, float &l, float m1, float l1)
+{
+    const float top = fmaxf(m, m1), ref = top == -INFINITY ? 0.f : top;
+    l = l * __builtin_amdgcn_exp2f(m - ref) + l1 * __builtin_amdgcn_exp2f(m1 - ref);
+    m = top;
+}
+
 constexpr int kScoreChunk = 256;             // virtual keys that a wave scores at once, four to a lane
 
 // The score of an item's virtual tiles [t0, t1) and of its part of the keys between the two runs, by waves that share out the
@@ -113,27 +121,27 @@ __global__ __launch_bounds__(256) void paged_join(PagedParams p, int merges, int
         int counter = 0;
         auto item = [&](int b, int len, int kvh, int t0, int t1, int w0, int n) {      // n pieces from share w0 on, or 0: finished already
             paged_score<TK>(p, b, kvh, len, t0, t1, counter, mine, 4 * parts, [&](int r0) {
-                const int row = min(r0 + lane, p.G - 1), rb = row / R;
+                // the lanes divide the rows' pieces (one lane to a row: 7 heads, 32 pieces 28.9 us the call, so 24.0; 64 pieces in fp32 81.6, 75.2)
+                int width = 1;
+                while (width < min(64, p.G - r0)) width *= 2;
+                const int row = min(r0 + (lane & (width - 1)), p.G - 1), rb = row / R, mine0 = lane / width, step = 64 / width;
                 if (n == 0) {
                     const float2 y = p.row_ml[(size_t)b * p.Hq + (size_t)kvh * p.G + row];
                     return score_row(y.x, y.y);
                 }
                 float m = -INFINITY, l = 0.f;
-                for (int x = 0; x < n; x += 4) {         // pieces past the last repeat it, without weight
+                for (int x = mine0; x < n; x += 4 * step) {                      // pieces past the last repeat it, without weight
                     float2 y[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int piece = min(x + i, n - 1);
+                        const int piece = min(x + i * step, n - 1);
                         y[i] = p.part_ml[tree_slot(p, w0 + piece, piece, rb) * p.part_rows + row - rb * R];
-                        if (x + i >= n) y[i] = make_float2(-INFINITY, 0.f);
+                        if (x + i * step >= n) y[i] = make_float2(-INFINITY, 0.f);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float top = fmaxf(m, y[i].x), ref = top == -INFINITY ? 0.f : top;
-                        l = l * __builtin_amdgcn_exp2f(m - ref) + y[i].y * __builtin_amdgcn_exp2f(y[i].x - ref);
-                        m = top;
-                    }
+                    for (int i = 0; i < 4; ++i) add_piece(m, l, y[i].x, y[i].y);
                 }
+                for (int o = width; o < 64; o *= 2) add_piece(m, l, __shfl_xor(m, o), __shfl_xor(l, o));
                 return score_row(m, l);
             });
         };
@@ -220,10 +228,10 @@ inline void paged_join_launch(const PagedParams &p, hipStream_t st)
     int rows = 1;                                        // as in tree_merge_launch
     while (2 * rows <= 1024 / D && rows < p.part_rows && blocks * ((p.part_rows + rows - 1) / rows) > 3l * p.units) rows *= 2;
     const long merges = p.shares ? blocks * ((p.part_rows + rows - 1) / rows) : 0;
-    // One workgroup to a share of few logits, three to others: finding its place takes a workgroup as long as thousands of logits.  us with 1, 2, 3, 4
-    // of them: 16 caches of up to 13711 keys, 24/8 heads of 64 (10 thousand logits a share at most) 65.9, 66.8, 67.6, 70.5; 4 of up to 5028, 32/8 of 128
-    // (3) 22.8, 24.0, 24.1, 25.7; 32 of up to 8192 (33) 134.8, 134.2, 133.4, 135.8; 16 of up to 26333 (53) 250.3, 247.6, 247.1, 247.7; 32 of up to 3679,
-    // 64/1 (118) 42.9, 35.3, 35.1, 35.4
+    // One workgroup to a share of few logits, three to others: finding its place takes a workgroup as long as thousands of logits.  us with 1, 2, 3
+    // of them: 16 caches of up to 13711 keys, 24/8 heads of 64 (10 thousand logits a share at most) 66.0, 67.7, 67.8; 4 of up to 5028, 32/8 of 128
+    // (3) 22.6, 23.7, 23.8; 32 of up to 8192 (33) 135.9, 135.2, 134.3; 16 of up to 26333 (53) 250.0, 247.6, 247.4 (four: 247.7); 32 of up to 3679,
+    // 64/1 (118) 43.2, 35.4, 35.3
     const long scored = p.shares ? p.shares : (long)p.n_seq * p.Hkv;
     const int parts = (double)p.n_seq * p.Hq * p.logit_keys < 24576.0 * (double)scored ? 1 : 3;
     const long scores = !p.logits || (p.shares == 0 && p.row_blocks == 1) ? 0 : parts * scored;
