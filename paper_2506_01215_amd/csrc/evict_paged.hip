@@ -1,18 +1,18 @@
 // Caches in pages go back to their budget (see reform_paged_evict in reform.h).
 //
 //   paged_select   a workgroup has one sequence's KV head: finds the budget-th score between the first and the last keys
-//                  that are always kept, and lists the kept keys
+//                  that are always kept, and lists the kept keys; others set rows aside for the moves (stage_segments)
 //   paged_move     row r becomes row kept[r]: a workgroup has one head's rows, of K or of V and of those a slice of
 //                  128 bytes each, and goes through them in ascending order
 //
 // In place without flags: rank r comes from row kept[r] >= r, so what a chunk of ranks [r0, r1) overwrites is read by
 // ranks below r1 only.  A workgroup that has loaded all of a chunk may store it, and the next chunk's rows can be on their way
 // meanwhile.  Slices do not touch each other's bytes.  Few items of many rows are cut into segments of ranks that move at once; the rows
-// that a segment needs of the next one's are set aside first (paged_stage, a launch between the two).
+// that a segment may need of the next one's are set aside first, while the keys are selected.
 //
 // Bound: reading and writing the rows that move.  Cold caches, all rows moving: 112 heads from 4352 to 4096 rows of 128 elements bf16
-// 440 MB in 102 us, 4.3 TB/s (a large copy: 4.9), and 8 for the selection; 8 heads from 33024 to 32768 266 MB in 66 us, 16 for the selection, which
-// has one compute unit for each head.  Rows pass the caches' usual order of replacement (114 -> 103 us).  Chunks of 1024 threads x 4 x 16 bytes
+// 440 MB in 102 us, 4.3 TB/s (a large copy: 4.9), and 8 for the selection; 8 heads from 33024 to 32768 266 MB in 63 us, 18 for the selection, which
+// has one compute unit for each head, and the setting aside on the others.  Rows pass the caches' usual order of replacement (114 -> 103 us).  Chunks of 1024 threads x 4 x 16 bytes
 // against 512 x 8: 95 against 103; twice as deep 150; with the next chunk's loads before this one's stores 109; 64 bytes of a row to a
 // workgroup 142, 256 more than twice as slow for few items.
 #include "common.h"
@@ -25,7 +25,6 @@ namespace {
 
 constexpr int kSelBins = 2048, kSelGroup = 4;
 constexpr int kMoveThreads = 1024, kMoveLanes = 8, kMoveDeep = 4;        // a chunk: 512 rows of 128 bytes, 64 bytes a thread
-constexpr int kStageThreads = 512;
 
 __device__ __forceinline__ int clamped_len(const PagedEvictParams &p, int b) { return min(max(p.cache_len[b], 0), p.max_len); }
 
@@ -48,6 +47,31 @@ __device__ __forceinline__ int waves_before(const int *counts, int lane, int wav
     return __builtin_amdgcn_readlane(row_incl_scan(lane < wave ? counts[lane] : 0), 15);
 }
 
+// An item's segments, one where more keys go than a segment's staged rows can hold.
+__device__ __forceinline__ int segments(const PagedEvictParams &p, int n) { return n - p.budget <= p.stage_rows ? p.segs : 1; }
+
+__device__ __forceinline__ char *stage_of(const PagedEvictParams &p, int item, int what, int seg)
+{
+    return p.stage + (((size_t)item * 2 + what) * (p.segs - 1) + seg) * p.stage_rows * p.row_bytes;
+}
+
+// Before segments move at once: the rows that a segment's last ranks may need and the next segment overwrites, 16 bytes a thread.  These are
+// the first n - budget behind the segment's end, whichever of them stay, so this need not wait for the selection.
+template <int NT>
+__device__ __forceinline__ void stage_segments(const PagedEvictParams &p, int block, int groups)
+{
+    const int bounds = p.segs - 1, item = block / (2 * bounds * groups), rest = block - item * 2 * bounds * groups;
+    const int what = rest / (bounds * groups), seg = (rest - what * bounds * groups) / groups, group = rest % groups;
+    const int b = item / p.Hkv, g = item - b * p.Hkv, n = clamped_len(p, b);
+    if (n <= p.budget || segments(p, n) == 1) return;
+    const int pieces = p.row_bytes / 16, i = group * NT + threadIdx.x;
+    const int x = i / pieces, c = (i - x * pieces) * 16;
+    if (x >= n - p.budget) return;
+    const long off = pool_row(p.pool, p.pool.table + (size_t)b * p.pool.table_stride, (seg + 1) * p.seg_rows + x);
+    const char *base = (const char *)(what ? p.v : p.k) + (size_t)g * p.pool.head_stride * p.elt;
+    if (off >= 0) *(v4u *)(stage_of(p, item, what, seg) + (size_t)x * p.row_bytes + c) = __builtin_nontemporal_load((const v4u *)(base + off * p.elt + c));
+}
+
 // The scores are compared as ordered integers (ordered_key).  Each pass counts the candidates inside [lo, hi] in 2048 bins of equal
 // width and goes on with the bin that holds the need-th largest, so three passes decide 32 bits, two where the scores spread
 // over less than 22.
@@ -60,8 +84,12 @@ __device__ __forceinline__ int waves_before(const int *counts, int lane, int wav
 // 131328 148 -> 83 (groups of kSelGroup keys: 1 21.0, 9.2; 2 19.4, 8.6; 4 18.9, 8.4; 8 18.9, 9.5).  The rest are the first reads, 4 us, and
 // barriers.
 template <int NT, int K>
-__global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
+__global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p, int groups)
 {
+    if ((int)blockIdx.x >= p.n_seq * p.Hkv) {
+        stage_segments<NT>(p, (int)blockIdx.x - p.n_seq * p.Hkv, groups);
+        return;
+    }
     constexpr int NW = NT / 64, PER = kSelBins / NT;     // waves; bins of a thread
     __shared__ int bins[kSelBins];
     __shared__ int sh_a[NW], sh_b[NW];
@@ -238,7 +266,7 @@ __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p)
 
 // Ranks [r0, r1) of one segment's rows, LANES threads of 16 bytes to a row.  Three things of a row follow from each other: which key it
 // comes from, where that key's row is, and what is in it.  They are fetched two chunks, one chunk and no chunk ahead.  Rows from
-// key `bound` on are the next segment's to overwrite: they come from `stage`, where rank bound - 1 - x has row x.
+// key `bound` on are the next segment's to overwrite: they come from `stage`, where key bound + x is row x.
 __device__ __forceinline__ void move_rows(const PagedEvictParams &p, const int32_t *kept, int r0, int r1, int bound, char *base, const char *stage,
                                           const int32_t *table, int col)
 {
@@ -263,7 +291,7 @@ __device__ __forceinline__ void move_rows(const PagedEvictParams &p, const int32
 #pragma unroll
         for (int i = 0; i < kMoveDeep; ++i) {
             from[i] = nullptr;
-            if (key[i] >= bound) from[i] = pool_row(p.pool, table, key[i]) >= 0 ? staged + (size_t)(bound - 1 - (r + i * ROWS + tr)) * p.row_bytes : nullptr;
+            if (key[i] >= bound) from[i] = pool_row(p.pool, table, key[i]) >= 0 ? staged + (size_t)(key[i] - bound) * p.row_bytes : nullptr;
             else if (key[i] >= 0) from[i] = place(key[i]);
         }
     };
@@ -312,31 +340,6 @@ __device__ __forceinline__ void move_words(const PagedEvictParams &p, const int3
     }
 }
 
-// An item's segments, one where more keys go than a segment's staged rows can hold.
-__device__ __forceinline__ int segments(const PagedEvictParams &p, int n) { return n - p.budget <= p.stage_rows ? p.segs : 1; }
-
-__device__ __forceinline__ char *stage_of(const PagedEvictParams &p, int item, int what, int seg)
-{
-    return p.stage + (((size_t)item * 2 + what) * (p.segs - 1) + seg) * p.stage_rows * p.row_bytes;
-}
-
-// Before segments move at once: rows that a segment's last ranks need and the next segment overwrites, 16 bytes a thread.
-__global__ __launch_bounds__(kStageThreads) void paged_stage(PagedEvictParams p, int groups)
-{
-    const int bounds = p.segs - 1, item = blockIdx.x / (2 * bounds * groups), rest = blockIdx.x - item * 2 * bounds * groups;
-    const int what = rest / (bounds * groups), seg = (rest - what * bounds * groups) / groups, group = rest % groups;
-    const int b = item / p.Hkv, g = item - b * p.Hkv, n = clamped_len(p, b);
-    if (n <= p.budget || segments(p, n) == 1) return;
-    const int pieces = p.row_bytes / 16, i = group * kStageThreads + threadIdx.x;
-    const int bound = (seg + 1) * p.seg_rows, x = i / pieces, c = (i - x * pieces) * 16, r = bound - 1 - x;
-    if (x >= min(p.stage_rows, n - p.budget) || r >= p.budget) return;   // no more rows than go come from behind the bound
-    const int j = p.kept[(size_t)item * p.budget + r];
-    if (j < bound) return;
-    const long off = pool_row(p.pool, p.pool.table + (size_t)b * p.pool.table_stride, j);
-    const char *base = (const char *)(what ? p.v : p.k) + (size_t)g * p.pool.head_stride * p.elt;
-    if (off >= 0) *(v4u *)(stage_of(p, item, what, seg) + (size_t)x * p.row_bytes + c) = __builtin_nontemporal_load((const v4u *)(base + off * p.elt + c));
-}
-
 // XCDs take workgroups in turn: those of one item are eight apart, so that a row's slices meet in one L2.
 __device__ __forceinline__ int item_of(int block, int items, int parts, int &part)
 {
@@ -369,10 +372,11 @@ __global__ __launch_bounds__(kMoveThreads) void paged_move(PagedEvictParams p, i
 
 }  // namespace
 
-// How many segments an item's rows are moved in: as many as there are compute units for.  A segment's chunks follow each other, some
-// 4 us each whatever else runs, so one workgroup for few items of many rows leaves the chip idle: 8 heads of 32768 rows, 128 wide,
-// whole 323 us, in 8 segments 66, in 16 69 (and 5 to 10 for the staging); 112 heads of 4096 rows, of which two would make the best of
-// the chip, 102 whole and 106 in two.  Segments of 1024 rows at least, and where it is known how many keys may go, so large
+// How many segments an item's rows are moved in: as makes 1.75 workgroups for each compute unit.  A segment's chunks follow each other, some
+// 4 us each whatever else runs, so few workgroups leave the chip idle.  The call, us, cold caches of heads 128 wide, all rows moving, at 1, 1.25, 1.5,
+// 1.75, 2 and 3 workgroups: 8 heads of 32768 rows 96, 106, 97, 93, 100, 98 (whole 350); 16 of them 195, 172, 156, 149, 158, 158; 64 of 8192 (rounded
+// to two segments from 1.5 on) 179, 178, 134, 134, 135, 152; over 74 batches 12, 9, 2.4, 0.8, 1.1 and 4.6 % above the best of them.  112 heads of 4096,
+// which move in one: 102, in two 106.  Segments of 1024 rows at least, and where it is known how many keys may go, so large
 // that a quarter of their rows has room for that many; an item that more keys leave moves in one.
 void paged_evict_plan(PagedEvictParams &p)
 {
@@ -380,7 +384,7 @@ void paged_evict_plan(PagedEvictParams &p)
     const int slices = (p.row_bytes + kMoveLanes * 16 - 1) / (kMoveLanes * 16), most_gone = p.max_len - p.budget;
     p.segs = 1;
     if (most_gone > 0) {
-        const double want = p.units / (items * 2.0 * slices), fit = p.budget / (4.0 * most_gone);
+        const double want = 1.75 * p.units / (items * 2.0 * slices) + 0.5, fit = p.budget / (4.0 * most_gone);
         int segs = want < 32.0 ? (int)want : 32;
         if (fit >= 2.0 && segs > fit) segs = (int)fit;
         if (segs > p.budget / 1024) segs = p.budget / 1024;
@@ -398,15 +402,15 @@ size_t paged_evict_stage_bytes(const PagedEvictParams &p)
 hipError_t paged_evict_launch(const PagedEvictParams &p, hipStream_t st)
 {
     const int items = p.n_seq * p.Hkv, most = p.max_len - p.n_sink - p.n_recent;
-    if (most <= 2048) hipLaunchKernelGGL((paged_select<256, 8>), dim3(items), dim3(256), 0, st, p);
-    else if (most <= 8192) hipLaunchKernelGGL((paged_select<1024, 8>), dim3(items), dim3(1024), 0, st, p);
-    else hipLaunchKernelGGL((paged_select<1024, 32>), dim3(items), dim3(1024), 0, st, p);
+    auto select = [&](auto kernel, int threads) {
+        const int groups = p.segs > 1 ? (p.stage_rows * (p.row_bytes / 16) + threads - 1) / threads : 0;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)items * (1 + 2 * (p.segs - 1) * groups)), dim3(threads), 0, st, p, groups);
+    };
+    if (most <= 2048) select(paged_select<256, 8>, 256);
+    else if (most <= 8192) select(paged_select<1024, 8>, 1024);
+    else select(paged_select<1024, 32>, 1024);
     if (p.max_len <= p.budget) return hipGetLastError();
     const int slices = (p.row_bytes + kMoveLanes * 16 - 1) / (kMoveLanes * 16), parts = 2 * slices * p.segs + (p.pos ? 2 : 1);
-    if (p.segs > 1) {
-        const int groups = (p.stage_rows * (p.row_bytes / 16) + kStageThreads - 1) / kStageThreads;
-        hipLaunchKernelGGL(paged_stage, dim3(items * 2 * (p.segs - 1) * groups), dim3(kStageThreads), 0, st, p, groups);
-    }
     hipLaunchKernelGGL(paged_move, dim3((unsigned)items * parts), dim3(kMoveThreads), 0, st, p, slices, parts);
     return hipGetLastError();
 }
