@@ -2,7 +2,7 @@
 // attend_seq_f32.hip: 16 heads of a KV group to a workgroup, whose eight waves take every eighth 16-key tile; both products' operands
 // come straight from memory, 16 bytes a lane.  Lane l % 16 looks up the row of that key of the tile, a tile ahead of its use.
 //
-// Bound: reading K and V once.
+// Bound: reading K and V once: 1073 MB of one cache of 131072 keys, 8 KV heads of 128, in 175 us (the call): 6.1 TB/s.
 #include "paged_list.h"
 
 namespace reform {
@@ -18,8 +18,9 @@ struct PagedSumsF32 {
     float2 row[kRows];
 };
 
-// As paged_segment of the bf16 form; D <= DP elements a row.
-template <int DP>
+// As paged_segment of the bf16 form; D <= DP elements a row.  STREAM: V goes past the caches' order of replacement; pieces of K's lines are read
+// by different loads, so K does not (us without, V, both: 655 MB 129.0, 121.4, 122.9; 131 MB in heads of 64 33.4, 30.3; 65 MB of 256 27.9, 29.6).
+template <int DP, bool STREAM>
 __device__ __forceinline__ void paged_segment_f32(const PagedParams &p, int b, int kvh, int len, int row0, int t0, int t1, float *po, float2 *pml,
                                                   PagedSumsF32<DP> &sh)
 {
@@ -79,7 +80,10 @@ __device__ __forceinline__ void paged_segment_f32(const PagedParams &p, int b, i
 #pragma unroll
             for (int a = 0; a < NV; ++a) {
                 v[e][a] = (quadlet)(0.f);
-                if (at >= 0 && VEC * (16 * a + ln) < D) v[e][a] = *(const quadlet *)(V + at + VEC * (16 * a + ln));
+                if (at >= 0 && VEC * (16 * a + ln) < D) {
+                    const quadlet *from = (const quadlet *)(V + at + VEC * (16 * a + ln));
+                    v[e][a] = STREAM ? __builtin_nontemporal_load(from) : *from;
+                }
             }
         };
         if (AHEAD) {
@@ -182,12 +186,12 @@ __device__ __forceinline__ void paged_segment_f32(const PagedParams &p, int b, i
     }
 }
 
-template <int DP>
+template <int DP, bool STREAM>
 __global__ __launch_bounds__(kWaves * 64, 2) void paged_attend_f32(PagedParams p)
 {
     __shared__ PagedSumsF32<DP> sh;
     list_walk<kRows, kKeys>(p, [&](int b, const TreeSeq &seq, int kvh, int rb, int t0, int t1, long slot) {
-        paged_segment_f32<DP>(p, b, kvh, seq.len, rb * kRows, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * DP,
+        paged_segment_f32<DP, STREAM>(p, b, kvh, seq.len, rb * kRows, t0, t1, slot < 0 ? nullptr : p.part_o + (size_t)slot * p.part_rows * DP,
                               slot < 0 ? nullptr : p.part_ml + (size_t)slot * p.part_rows, sh);
     });
 }
@@ -196,7 +200,8 @@ template <int DP>
 hipError_t launch(const PagedParams &p, hipStream_t st)
 {
     const unsigned grid = (unsigned)(p.shares ? p.shares : p.n_seq * p.Hkv) * p.row_blocks;
-    hipLaunchKernelGGL((paged_attend_f32<DP>), dim3(grid), dim3(kWaves * 64), 0, st, p);
+    if (p.stream) hipLaunchKernelGGL((paged_attend_f32<DP, true>), dim3(grid), dim3(kWaves * 64), 0, st, p);
+    else hipLaunchKernelGGL((paged_attend_f32<DP, false>), dim3(grid), dim3(kWaves * 64), 0, st, p);
     paged_join_launch<DP, kRows, kKeys, false>(p, st);
     return hipGetLastError();
 }
@@ -204,11 +209,15 @@ hipError_t launch(const PagedParams &p, hipStream_t st)
 }  // namespace
 
 // Keys that a workgroup takes whole: fitted to 22 batches of 1 to 48 caches of up to 3000 keys, with scores and without, in heads of 64 and
-// 128, each whole and shared out: 1.01 times the better of the two in the mean, at worst 1.08.  Wider and narrower heads in proportion.
+// 128, each whole and shared out: 1.01 times the better of the two in the mean, at worst 1.08.  Narrower heads in proportion, wider ones by two batches
+// of 109 and 149 keys (whole 16.2 and 18.5 us, shared out 19.4 and 22.6).
+//
+// Shares: as many as run at once, two a compute unit in up to 127 registers and one beyond (heads of 128, two / one, us: 2 caches of 4000 keys, 8 KV
+// heads, 31.6 / 22.0, 4 of 20000 128.6 / 122.7; of 256: 8 of 4000, 2 KV heads, 60.1 / 43.3; of 64: 8 of 4000, 8 KV heads, 33.4 / 34.4; of 32: 36.1 / 43.3).
 void paged_plan_f32(PagedParams &p)
 {
-    const int whole = p.D <= 32 ? 900 : p.D <= 64 ? 450 : p.D <= 128 ? 250 : 125;
-    paged_plan(p, kRows, kKeys, whole, kWaves, 2 * p.units);
+    const int whole = p.D <= 32 ? 900 : p.D <= 64 ? 450 : p.D <= 128 ? 250 : 175;
+    paged_plan(p, kRows, kKeys, whole, kWaves, p.D <= 64 ? 2 * p.units : p.units);
 }
 
 hipError_t paged_attend_f32_launch(const PagedParams &p, hipStream_t st)
