@@ -294,12 +294,12 @@ hipError_t launch(const PagedParams &p, hipStream_t st)
 }  // namespace
 
 // Keys that a workgroup takes whole: fitted to 88 batches of 1 to 48 caches of 150 to 6000 keys, half of them with scores, each whole and
-// shared out: 1.004 times the better of the two in the mean, at worst 1.10 (2000 and 1600 keys 1.02, 1.34).  Shares as for one
-// drafted token (tree_plan_bf16).
+// shared out: 1.004 times the better of the two in the mean, at worst 1.10 (2000 and 1600 keys 1.02, 1.34).  As many
+// shares as run at once, of 128 keys at least (heads of 64, 256 / 128, us: 1 cache of 1258 keys, 28/4 heads, 10.8 / 10.0; 4 of 1221, 16/2, 11.2 / 10.1; 4 with
+// windows of 5761, 16/2, 12.7 / 13.4; heads of 128: 2 with windows of 2204, 16/4, 13.4 / 12.2).
 void paged_plan_bf16(PagedParams &p)
 {
-    const bool narrow = p.D == 64;
-    paged_plan(p, 16, 32, 1000, (narrow ? 256 : 128) / 32, (narrow ? 2 : 1) * p.units);
+    paged_plan(p, 16, 32, 1000, 128 / 32, (p.D == 64 ? 2 : 1) * p.units);
 }
 
 namespace {
