@@ -233,8 +233,10 @@ struct PagedEvictParams {
     int units;               // compute units
     long score_ss, score_hs;
     int32_t *first;          // [n_seq][Hkv]: first row that moves
-    int segs, seg_rows, stage_rows;          // segments that an item's rows are moved in, ranks of one, staged rows of one at most
-    char *stage;             // [n_seq][Hkv][k, v][segs - 1][stage_rows] rows
+    int segs, enough;        // segments that an item's rows are moved in, at most; that give every compute unit one
+    int stage_rows;          // rows of K, or V, of an item that can be set aside
+    int move_threads;        // of a workgroup that moves rows
+    char *stage;             // [n_seq][Hkv][k, v][stage_rows] rows
 };
 
 struct EmbedParams {

@@ -24,7 +24,8 @@ namespace reform {
 namespace {
 
 constexpr int kSelBins = 2048, kSelGroup = 4;
-constexpr int kMoveThreads = 1024, kMoveLanes = 8, kMoveDeep = 4;        // a chunk: 512 rows of 128 bytes, 64 bytes a thread
+constexpr int kLeastSegment = 128, kSmallSegment = 256;
+constexpr int kMoveLanes = 8, kMoveDeep = 4;             // a chunk: 512 rows of 128 bytes with 1024 threads, 64 bytes a thread
 
 __device__ __forceinline__ int clamped_len(const PagedEvictParams &p, int b) { return min(max(p.cache_len[b], 0), p.max_len); }
 
@@ -47,29 +48,47 @@ __device__ __forceinline__ int waves_before(const int *counts, int lane, int wav
     return __builtin_amdgcn_readlane(row_incl_scan(lane < wave ? counts[lane] : 0), 15);
 }
 
-// An item's segments, one where more keys go than a segment's staged rows can hold.
-__device__ __forceinline__ int segments(const PagedEvictParams &p, int n) { return n - p.budget <= p.stage_rows ? p.segs : 1; }
-
-__device__ __forceinline__ char *stage_of(const PagedEvictParams &p, int item, int what, int seg)
+// Ranks of a segment of an item that loses `gone` keys.
+__host__ __device__ __forceinline__ int segment_rows(const PagedEvictParams &p, int gone)
 {
-    return p.stage + (((size_t)item * 2 + what) * (p.segs - 1) + seg) * p.stage_rows * p.row_bytes;
+    const int fit = (int)((unsigned)p.budget / (unsigned)gone), quarter = fit / 4, half = fit / 2 < p.enough ? fit / 2 : p.enough;
+    int count = quarter > half ? quarter : half;
+    count = count < 1 ? 1 : count < p.segs ? count : p.segs;
+    return (p.budget + count - 1) / count;
+}
+
+// The segments that an item of n keys is moved in: the fewer the more keys go, since the rows that are set aside for each are that many.
+// (count - 1) * gone is no more than half the budget and (p.segs - 1) * (most keys that go): paged_evict_plan's room.
+struct Segments {
+    int count, rows, gone;   // ranks of a segment; keys that go, rows that are set aside behind its end
+    __device__ __forceinline__ Segments(const PagedEvictParams &p, int n)
+    {
+        gone = n - p.budget;
+        rows = segment_rows(p, gone);
+        count = (p.budget - 1) / rows + 1;
+    }
+};
+
+__device__ __forceinline__ char *stage_of(const PagedEvictParams &p, int item, int what)
+{
+    return p.stage + ((size_t)item * 2 + what) * p.stage_rows * p.row_bytes;
 }
 
 // Before segments move at once: the rows that a segment's last ranks may need and the next segment overwrites, 16 bytes a thread.  These are
-// the first n - budget behind the segment's end, whichever of them stay, so this need not wait for the selection.
+// the first ones behind the segment's end, whichever of them stay, so this need not wait for the selection.
 template <int NT>
 __device__ __forceinline__ void stage_segments(const PagedEvictParams &p, int block, int groups)
 {
-    const int bounds = p.segs - 1, item = block / (2 * bounds * groups), rest = block - item * 2 * bounds * groups;
-    const int what = rest / (bounds * groups), seg = (rest - what * bounds * groups) / groups, group = rest % groups;
+    const int item = block / (2 * groups), rest = block - item * 2 * groups, what = rest / groups, group = rest - what * groups;
     const int b = item / p.Hkv, g = item - b * p.Hkv, n = clamped_len(p, b);
-    if (n <= p.budget || segments(p, n) == 1) return;
+    if (n <= p.budget) return;
+    const Segments s(p, n);
     const int pieces = p.row_bytes / 16, i = group * NT + threadIdx.x;
-    const int x = i / pieces, c = (i - x * pieces) * 16;
-    if (x >= n - p.budget) return;
-    const long off = pool_row(p.pool, p.pool.table + (size_t)b * p.pool.table_stride, (seg + 1) * p.seg_rows + x);
+    const int row = i / pieces, c = (i - row * pieces) * 16, seg = row / s.gone;
+    if (seg >= s.count - 1) return;
+    const long off = pool_row(p.pool, p.pool.table + (size_t)b * p.pool.table_stride, (seg + 1) * s.rows + row - seg * s.gone);
     const char *base = (const char *)(what ? p.v : p.k) + (size_t)g * p.pool.head_stride * p.elt;
-    if (off >= 0) *(v4u *)(stage_of(p, item, what, seg) + (size_t)x * p.row_bytes + c) = __builtin_nontemporal_load((const v4u *)(base + off * p.elt + c));
+    if (off >= 0) *(v4u *)(stage_of(p, item, what) + (size_t)row * p.row_bytes + c) = __builtin_nontemporal_load((const v4u *)(base + off * p.elt + c));
 }
 
 // The scores are compared as ordered integers (ordered_key).  Each pass counts the candidates inside [lo, hi] in 2048 bins of equal
@@ -267,10 +286,11 @@ __global__ __launch_bounds__(NT) void paged_select(PagedEvictParams p, int group
 // Ranks [r0, r1) of one segment's rows, LANES threads of 16 bytes to a row.  Three things of a row follow from each other: which key it
 // comes from, where that key's row is, and what is in it.  They are fetched two chunks, one chunk and no chunk ahead.  Rows from
 // key `bound` on are the next segment's to overwrite: they come from `stage`, where key bound + x is row x.
+template <int NT>
 __device__ __forceinline__ void move_rows(const PagedEvictParams &p, const int32_t *kept, int r0, int r1, int bound, char *base, const char *stage,
                                           const int32_t *table, int col)
 {
-    constexpr int ROWS = kMoveThreads / kMoveLanes, CHUNK = kMoveDeep * ROWS;
+    constexpr int ROWS = NT / kMoveLanes, CHUNK = kMoveDeep * ROWS;
     const int tr = threadIdx.x / kMoveLanes, tc = threadIdx.x % kMoveLanes;
     char *const at = base + col + tc * 16;
     const char *const staged = stage + col + tc * 16;
@@ -321,20 +341,21 @@ __device__ __forceinline__ void move_rows(const PagedEvictParams &p, const int32
 }
 
 // The same for four bytes a row in one piece of memory (score, pos).
+template <int NT>
 __device__ __forceinline__ void move_words(const PagedEvictParams &p, const int32_t *kept, int first, int n, uint32_t *base)
 {
     uint32_t data[kMoveDeep];
-    for (int r0 = first; r0 < p.budget; r0 += kMoveDeep * kMoveThreads) {
+    for (int r0 = first; r0 < p.budget; r0 += kMoveDeep * NT) {
 #pragma unroll
         for (int i = 0; i < kMoveDeep; ++i) {
-            const int r = r0 + i * kMoveThreads + threadIdx.x;
+            const int r = r0 + i * NT + threadIdx.x;
             if (r < p.budget) data[i] = base[min(kept[r], n - 1)];
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kMoveDeep; ++i) {
-            const int r = r0 + i * kMoveThreads + threadIdx.x;
+            const int r = r0 + i * NT + threadIdx.x;
             if (r < p.budget) base[r] = data[i];
         }
     }
@@ -349,7 +370,8 @@ __device__ __forceinline__ int item_of(int block, int items, int parts, int &par
     return block < even ? (block & 7) * each + i : 8 * each + i;
 }
 
-__global__ __launch_bounds__(kMoveThreads) void paged_move(PagedEvictParams p, int slices, int parts)
+template <int NT>
+__global__ __launch_bounds__(NT) void paged_move(PagedEvictParams p, int slices, int parts)
 {
     int part;
     const int item = item_of(blockIdx.x, p.n_seq * p.Hkv, parts, part);
@@ -359,59 +381,70 @@ __global__ __launch_bounds__(kMoveThreads) void paged_move(PagedEvictParams p, i
     const int32_t *kept = p.kept + (size_t)item * p.budget;
     if (part >= 2 * slices * p.segs) {
         const size_t at = (size_t)b * p.score_ss + (size_t)g * p.score_hs;
-        move_words(p, kept, first, n, part == 2 * slices * p.segs ? (uint32_t *)p.score + at : (uint32_t *)p.pos + at);
+        move_words<NT>(p, kept, first, n, part == 2 * slices * p.segs ? (uint32_t *)p.score + at : (uint32_t *)p.pos + at);
         return;
     }
-    const int seg = part / (2 * slices), rest = part - seg * 2 * slices, what = rest / slices, segs = segments(p, n);
-    const bool last = segs == 1 || seg == segs - 1;
-    const int r0 = max(first, seg * p.seg_rows), r1 = last ? p.budget : (seg + 1) * p.seg_rows;
-    if (seg >= segs || r0 >= r1) return;
-    move_rows(p, kept, r0, r1, last ? INT_MAX : r1, (char *)(what ? p.v : p.k) + (size_t)g * p.pool.head_stride * p.elt,
-              last ? nullptr : stage_of(p, item, what, seg), p.pool.table + (size_t)b * p.pool.table_stride, rest % slices * kMoveLanes * 16);
+    const Segments s(p, n);
+    const int seg = part / (2 * slices), rest = part - seg * 2 * slices, what = rest / slices;
+    const bool last = seg == s.count - 1;
+    const int r0 = max(first, seg * s.rows), r1 = last ? p.budget : (seg + 1) * s.rows;
+    if (seg >= s.count || r0 >= r1) return;
+    move_rows<NT>(p, kept, r0, r1, last ? INT_MAX : r1, (char *)(what ? p.v : p.k) + (size_t)g * p.pool.head_stride * p.elt,
+                  last ? nullptr : stage_of(p, item, what) + (size_t)seg * s.gone * p.row_bytes, p.pool.table + (size_t)b * p.pool.table_stride,
+                  rest % slices * kMoveLanes * 16);
 }
 
 }  // namespace
 
-// How many segments an item's rows are moved in: as makes 1.75 workgroups for each compute unit.  A segment's chunks follow each other, some
+// How many segments an item's rows are moved in, at most: as makes 1.75 workgroups for each compute unit.  A segment's chunks follow each other, some
 // 4 us each whatever else runs, so few workgroups leave the chip idle.  The call, us, cold caches of heads 128 wide, all rows moving, at 1, 1.25, 1.5,
 // 1.75, 2 and 3 workgroups: 8 heads of 32768 rows 96, 106, 97, 93, 100, 98 (whole 350); 16 of them 195, 172, 156, 149, 158, 158; 64 of 8192 (rounded
 // to two segments from 1.5 on) 179, 178, 134, 134, 135, 152; over 74 batches 12, 9, 2.4, 0.8, 1.1 and 4.6 % above the best of them.  112 heads of 4096,
-// which move in one: 102, in two 106.  Segments of 1024 rows at least, and where it is known how many keys may go, so large
-// that a quarter of their rows has room for that many; an item that more keys leave moves in one.
+// which move in one: 102, in two 106.
+//
+// Segments of 128 rows at least (of 1024, 512, 256, 128: 8 heads of 1827 rows 27.5, 19.3, 18.6, 18.2; 4 of 444 14.2, 14.0, 13.8, 12.2), and of four times the
+// rows that are set aside for one, or twice if that leaves compute units idle (twice / four times: 8 heads of 64 in fp32 that lose 671 of 7517 rows 35.8 / 49.2,
+// 8 of 128 that lose 441 of 4891 32.5 / 39.2; with a workgroup to each compute unit at four times, 8 heads that lose 512
+// of 16896 63 / 55, 8 of 64 in fp32 that lose 256 of 8448 38 / 32).
+// Short segments in workgroups of 512 threads, since their chunks would be half empty (152 heads back to 114 rows 18.6 -> 15.8; 12 back to 372 13.7 -> 14.8).
 void paged_evict_plan(PagedEvictParams &p)
 {
     const double items = (double)p.n_seq * p.Hkv;
     const int slices = (p.row_bytes + kMoveLanes * 16 - 1) / (kMoveLanes * 16), most_gone = p.max_len - p.budget;
     p.segs = 1;
-    if (most_gone > 0) {
-        const double want = 1.75 * p.units / (items * 2.0 * slices) + 0.5, fit = p.budget / (4.0 * most_gone);
-        int segs = want < 32.0 ? (int)want : 32;
-        if (fit >= 2.0 && segs > fit) segs = (int)fit;
-        if (segs > p.budget / 1024) segs = p.budget / 1024;
-        if (segs > 1 && items * p.budget * p.row_bytes / 32.0 < 2147483648.0) p.segs = segs;      // threads of the staging
-    }
-    p.seg_rows = (p.budget + p.segs - 1) / p.segs;
-    p.stage_rows = p.segs == 1 ? 0 : most_gone < p.seg_rows / 4 ? most_gone : p.seg_rows / 4;
+    p.move_threads = p.budget <= kSmallSegment ? 512 : 1024;
+    p.stage_rows = 0;
+    if (most_gone <= 0) return;
+    const double one = p.units / (items * 2.0 * slices), want = 1.75 * one + 0.5;            // segments for a workgroup to each compute unit
+    int segs = want < 32.0 ? (int)want : 32;
+    p.enough = (int)one;
+    if (segs > p.budget / kLeastSegment) segs = p.budget / kLeastSegment;
+    if (segs <= 1 || items * p.budget * p.row_bytes / 16.0 >= 2147483648.0) return;        // threads of stage_segments
+    p.segs = segs;
+    // workgroups of segments that there are not would cost some us, unless it is not known how few keys may go
+    const int fit = p.budget / most_gone, rows = segment_rows(p, most_gone);
+    if (fit >= 4) p.segs = (p.budget - 1) / rows + 1;
+    if (rows <= kSmallSegment) p.move_threads = 512;
+    const int64_t all = (int64_t)(p.segs - 1) * most_gone;
+    p.stage_rows = all < p.budget / 2 ? (int)all : p.budget / 2;
 }
 
-size_t paged_evict_stage_bytes(const PagedEvictParams &p)
-{
-    return (size_t)p.n_seq * p.Hkv * 2 * (p.segs - 1) * p.stage_rows * p.row_bytes;
-}
+size_t paged_evict_stage_bytes(const PagedEvictParams &p) { return (size_t)p.n_seq * p.Hkv * 2 * p.stage_rows * p.row_bytes; }
 
 hipError_t paged_evict_launch(const PagedEvictParams &p, hipStream_t st)
 {
     const int items = p.n_seq * p.Hkv, most = p.max_len - p.n_sink - p.n_recent;
     auto select = [&](auto kernel, int threads) {
-        const int groups = p.segs > 1 ? (p.stage_rows * (p.row_bytes / 16) + threads - 1) / threads : 0;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)items * (1 + 2 * (p.segs - 1) * groups)), dim3(threads), 0, st, p, groups);
+        const int groups = (p.stage_rows * (p.row_bytes / 16) + threads - 1) / threads;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)items * (1 + 2 * groups)), dim3(threads), 0, st, p, groups);
     };
     if (most <= 2048) select(paged_select<256, 8>, 256);
     else if (most <= 8192) select(paged_select<1024, 8>, 1024);
     else select(paged_select<1024, 32>, 1024);
     if (p.max_len <= p.budget) return hipGetLastError();
     const int slices = (p.row_bytes + kMoveLanes * 16 - 1) / (kMoveLanes * 16), parts = 2 * slices * p.segs + (p.pos ? 2 : 1);
-    hipLaunchKernelGGL(paged_move, dim3((unsigned)items * parts), dim3(kMoveThreads), 0, st, p, slices, parts);
+    if (p.move_threads == 512) hipLaunchKernelGGL(paged_move<512>, dim3((unsigned)items * parts), dim3(512), 0, st, p, slices, parts);
+    else hipLaunchKernelGGL(paged_move<1024>, dim3((unsigned)items * parts), dim3(1024), 0, st, p, slices, parts);
     return hipGetLastError();
 }
 

@@ -242,3 +242,11 @@ def test_long_rows_of_other_scores(kind):
     """Rows that are read anew in every pass: runs of candidates that end inside 512 and inside 64."""
     for n, budget in ((32900 + 14, 32000), (33800, 33700), (50001, 25000)):
         run_case(1, 64, [n], 64, budget, 4, 10, BF, seed=n, kind=kind)
+
+
+@pytest.mark.parametrize("columns", [None, 640])
+@pytest.mark.parametrize("budget,gone", [(2048, (1, 73, 128, 300)), (2050, (500, 1024, 1025, 1026)), (777, (1, 97, 388, 389)), (4097, (64, 2048, 2049, 4500)), (256, (3, 64, 129))])
+def test_segments_by_the_keys_that_go(budget, gone, columns):
+    """An item's segments follow from how many of its keys go, whatever its neighbours' do and the table has room for."""
+    for kind in ("spread", "ties"):
+        run_case(1, 64, [budget + n for n in gone], 16, budget, 4, 10, BF, seed=budget, kind=kind, columns=columns)
