@@ -6,7 +6,7 @@
 // same k; C[m][n]: n = l % 16, m = 4 (l / 16) + e.  The contraction over the head takes its elements in the order
 // 16 a + 4 (l / 16) + b, so a lane reads 16 bytes of a row at once; a lane then owns one query and the keys
 // 4 (l / 16) + e, which is the B operand of O^T = V^T P^T for the contraction over those four keys, and V's
-// operand is element l % 16 of row 4 (l / 16) + e: both straight from global memory, no LDS.
+// operand is an element of row 4 (l / 16) + e for each l % 16: both straight from global memory, no LDS.
 #pragma once
 #include "attend_seq.h"
 
@@ -26,7 +26,11 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const KEYS &s, int
                                             float2 *pml, F32Sums<DP> &sh)
 {
     constexpr bool WINDOW = std::is_same<KEYS, WindowKeys>::value;
-    constexpr int NA = DP / 16;
+    // V^T's operand of a product is element l % 16 of a row of 16; which 16 of the head's elements these are is free.  A lane takes VEC
+    // adjacent ones for as many products, with one load (element by element / so, us: prompts of 864 rows, 24/8 heads of 64, 35.7 / 32.6, 8/2 of 256
+    // 51.8 / 46.7; 8 nodes over three caches, 32/8 of 128, 36.9 / 33.2; 512 rows with a window, 16/2 of 128, 28.3 / 25.3).
+    constexpr int NA = DP / 16, VEC = NA < 4 ? NA : 4, NV = NA / VEC;
+    typedef float quadlet __attribute__((ext_vector_type(VEC)));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int ln = lane & 15, lg = lane >> 4;
     unsigned long long line = 0ull;
@@ -74,14 +78,14 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const KEYS &s, int
     for (; t < t1; t += kF32Waves) {
         const int j0 = key_start<kF32Keys>(s, t);
         if (!AHEAD) load_keys(t);
-        float v[4][NA];
+        quadlet v[4][NV];
         auto load_values = [&](int e) {
-            const float *vr = (const float *)s.v + (size_t)min(key_of(s, t * kF32Keys + 4 * lg + e), s.n - 1) * s.v_rs + ln;
+            const float *vr = (const float *)s.v + (size_t)min(key_of(s, t * kF32Keys + 4 * lg + e), s.n - 1) * s.v_rs;
 #pragma unroll
-            for (int a = 0; a < NA; ++a) {
-                const bool in = 16 * a + ln < D;
-                const float x = vr[in ? 16 * a : -ln];
-                v[e][a] = in ? x : 0.f;
+            for (int a = 0; a < NV; ++a) {
+                const int from = VEC * (16 * a + ln);
+                const quadlet x = *(const quadlet *)(vr + (from < D ? from : 0));
+                v[e][a] = from < D ? x : (quadlet)(0.f);
             }
         };
         if (AHEAD) {
@@ -120,7 +124,7 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const KEYS &s, int
         for (int e = 0; e < 4; ++e) {
             if (!AHEAD) load_values(e);
 #pragma unroll
-            for (int a = 0; a < NA; ++a) o[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][a], p[e], o[a], 0, 0, 0);
+            for (int a = 0; a < NA; ++a) o[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][a / VEC][a % VEC], p[e], o[a], 0, 0, 0);
         }
     }
     // the waves' sums, as in seq_segment
@@ -133,15 +137,23 @@ __device__ __forceinline__ void f32_segment(const SeqRows &r, const KEYS &s, int
     for (int w = 0; w < kF32Waves; ++w) m_all = fmaxf(m_all, sh.m[w][ln]);
     const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_all) * c);
 #pragma unroll
-    for (int a = 0; a < NA; ++a) {
-        o[a] *= f;
-        if (wave >= kF32Waves / 2) *(f32x4 *)&sh.o[wave - kF32Waves / 2][ln][16 * a + 4 * lg] = o[a];
-    }
-    __syncthreads();
-    if (wave < kF32Waves / 2) {
+    for (int a = 0; a < NA; ++a) o[a] *= f;
+    // element e of product a is element VEC (16 (a / VEC) + 4 lg + e) + a % VEC of the head
+    auto meet = [&](float *row, bool add) {
 #pragma unroll
-        for (int a = 0; a < NA; ++a) *(f32x4 *)&sh.o[wave][ln][16 * a + 4 * lg] += o[a];
-    }
+        for (int a = 0; a < NV; ++a)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                quadlet *const to = (quadlet *)(row + VEC * (16 * a + 4 * lg + e));
+                quadlet y = add ? *to : (quadlet)(0.f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) y[i] += o[a * VEC + i][e];
+                *to = y;
+            }
+    };
+    if (wave >= kF32Waves / 2) meet(sh.o[wave - kF32Waves / 2][ln], false);
+    __syncthreads();
+    if (wave < kF32Waves / 2) meet(sh.o[wave][ln], true);
     __syncthreads();
     const int rows_here = min(kF32Rows, r.rows - r.row0);
     for (int i = threadIdx.x; i < rows_here * (DP / 4); i += kF32Waves * 64) {
