@@ -365,13 +365,13 @@ __device__ __forceinline__ void rows_segment(const SeqRows &r, KEYS k, bool by_h
         asm volatile("" ::: "memory");
         auto after = [](int slot, int by, int slots) { const int x = slot + by; return x >= slots ? x - slots : x; };
         const int next = (t + 1) * KG + kg;
-        const int j1 = key_start<BN>(k, next);
-        const bool more = next < ntiles, whole = j1 + BN <= k.n && !key_split<BN>(k, next);
+        const bool more = next < ntiles, whole = WINDOW ? key_start<BN>(k, next) + BN <= k.n && !key_split<BN>(k, next) : (next + 1) * BN <= k.n;
         u16 *const nk = wk + (kslot ^ 1) * TILE, *const nv = wv + after(vslot, 1, S::VSLOTS) * TILE;
         if (more && !whole) load_end(t + 1, nk, nv);
+        const size_t j1 = WINDOW ? (size_t)key_start<BN>(k, next) : (size_t)next * BN;
         const int vread = STEP == kRowsLag || STEP == kRowsLast ? after(vslot, S::VSLOTS - 1, S::VSLOTS) : vslot;
         rows_tile<D, NW, KG, STEP, NB>(w, ldsK + kslot * TILE, ldsV + vread * TILE, nk, nv,
-                                      (const char *)((const u16 *)k.k + (size_t)j1 * k.k_rs) + koff, (const char *)((const u16 *)k.v + (size_t)j1 * k.v_rs) + voff,
+                                      (const char *)((const u16 *)k.k + j1 * k.k_rs) + koff, (const char *)((const u16 *)k.v + j1 * k.v_rs) + voff,
                                       step_k, step_v, more && whole, c, mask_tile);
         kslot ^= 1;
         vslot = after(vslot, 1, S::VSLOTS);

@@ -3,7 +3,7 @@
 //
 // Blocks of rows as attend_seq_f32.h takes them.
 //
-// Bound: the fp32 matrix pipe (0.15 PFLOP/s, of which it reaches 0.32 to 0.48: 2048 rows, 32/8 heads of 128, 534 us; 4096, 32/8 of 64, 926; 8 x 1000, 32/8 of 128, 1341) and,
+// Bound: the fp32 matrix pipe (0.15 PFLOP/s, of which it reaches 0.35 to 0.57: 2048 rows, 32/8 heads of 128, 495 us; 4096, 32/8 of 64, 776; 8 x 1000, 32/8 of 128, 1232) and,
 // at the sizes of checks, latency (three prompts of up to 301 rows, 4 heads of 64: 11 us).  32 rows to a workgroup, so that K and V are read half
 // as often: the same time for large batches, twice as long for small ones (60 batches, 1.27).
 #include "attend_seq_f32.h"
