@@ -85,14 +85,17 @@ __device__ __forceinline__ void paged_score(const PagedParams &p, int b, int kvh
             if (p.G > 64) y = rows(r0);
             const float *x = logits + (size_t)r0 * p.logit_keys + v;
             const int n = min(64, p.G - r0);
-            for (int r = 0; r < n; r += 4) {             // four rows' logits on their way at once; rows behind the last weigh nothing
+            // four rows' logits on their way at once; behind the last row it is taken again, against its own reference (another row's
+            // may lie further below than a float reaches), with a weight of 0
+            for (int r = 0; r < n; r += 4) {
                 f32x4 l[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) l[i] = *(const f32x4 *)(x + (size_t)min(r + i, n - 1) * p.logit_keys);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float ref = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y.x), r + i));
-                    const float inv = r + i < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y.y), r + i)) : 0.f;
+                    const int row = min(r + i, n - 1);
+                    const float ref = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y.x), row));
+                    const float inv = r + i < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y.y), row)) : 0.f;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(fmaf(l[i][e], c, -ref)) * inv;
                 }
