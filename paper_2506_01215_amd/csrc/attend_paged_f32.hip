@@ -212,7 +212,7 @@ hipError_t launch(const PagedParams &p, hipStream_t st)
 // 128, each whole and shared out: 1.01 times the better of the two in the mean, at worst 1.08.  Narrower heads in proportion, wider ones by two batches
 // of 109 and 149 keys (whole 16.2 and 18.5 us, shared out 19.4 and 22.6).
 //
-// Shares: as many as run at once, two a compute unit in up to 127 registers and one beyond (heads of 128, two / one, us: 2 caches of 4000 keys, 8 KV
+// Shares: as many as run at once, two a compute unit in up to 128 registers and one beyond (heads of 128, two / one, us: 2 caches of 4000 keys, 8 KV
 // heads, 31.6 / 22.0, 4 of 20000 128.6 / 122.7; of 256: 8 of 4000, 2 KV heads, 60.1 / 43.3; of 64: 8 of 4000, 8 KV heads, 33.4 / 34.4; of 32: 36.1 / 43.3).
 void paged_plan_f32(PagedParams &p)
 {

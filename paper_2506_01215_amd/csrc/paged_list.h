@@ -101,6 +101,18 @@ __device__ __forceinline__ void paged_score(const PagedParams &p, int b, int kvh
                 }
             }
         }
+        // Beside a row whose sum is no number the weight of a key that is not seen has to stay 0: its logits are -inf in every row.
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!((sum[0] + sum[1]) + (sum[2] + sum[3]) < INFINITY)) != 0ull, 0)) {
+            f32x4 most = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+            for (int r = 0; r < p.G; ++r) {
+                const f32x4 l = *(const f32x4 *)(logits + (size_t)r * p.logit_keys + v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most[e] = l[e] == -INFINITY ? most[e] : 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] = most[e] == 0.f ? sum[e] : 0.f;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (e < here) score[j + e] = (j + e == len - 1 ? 0.f : before[e]) + sum[e];          // the new token has no score yet
