@@ -565,12 +565,13 @@ reform_status reform_tree_accept(const reform_accept_desc *desc, const int32_t *
  * As reform_prompt_attend, with fewer keys seen: row i of a sequence of nq query and nk key rows stands at
  * key t = nk - nq + i and sees
  *     j in [0, t] with j > t - window or j < n_sink
- * A window of nk keys or more is reform_prompt_attend.  A row that sees no key (t < 0) gets out = 0 and lse = -inf.
+ * A window of nk keys or more gives reform_prompt_attend's results, up to rounding.  A row that sees no key (t < 0) gets out = 0 and lse = -inf.
  *     q, out, k, v, cu_q, cu_k, lse   as in reform_prompt_attend: layouts, lengths read on the device, boundaries that are out of
  *              place, rows of no sequence, arithmetic.  Keys and values that are not finite stay within their sequence; there, rows
  *              whose block goes through their tile of 64 keys may become NaN as well as those that see them
  * Supported: as reform_prompt_attend; window >= 1, n_sink >= 0.
- * The workspace is that of reform_prompt_attend: without it, or with less than the query asks for, REFORM_ERR_WORKSPACE.
+ * No workspace is needed: the query gives 0, and what is passed is not looked at.  Few rows behind a wide window are not shared out over
+ * workgroups, as reform_prompt_attend does it, which is the faster call there where the window covers all keys.
  */
 typedef struct {
     uint32_t struct_size;

@@ -55,3 +55,24 @@ def test_only_rows_of_sequences_are_written(hq, hkv, d, cu_q, cu_k, dtype):
     assert bool((out.cpu()[:, ~written] == KEPT).all()) and bool((lse.cpu()[:, ~written] == KEPT).all())
     room[1:-1, margin:-margin] = KEPT
     assert bool((room == KEPT).all()) and bool((lse_room[:margin] == KEPT).all()) and bool((lse_room[-margin:] == KEPT).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (8, 2, 128)])
+def test_no_workspace_is_needed(hq, hkv, d, dtype):
+    """Few rows behind many keys, whose keys reform_prompt_attend shares out and wants room for: the query gives 0, what is passed is not
+    looked at, and a window of all keys gives that call's results up to rounding."""
+    nq, nk = 3, 3000
+    g = torch.Generator().manual_seed(d)
+    q, k, v = (sref.randn(g, h, n, d, dtype=dtype) for h, n in ((hq, nq), (hkv, nk), (hkv, nk)))
+    dev = [x.to(DEV) for x in (q, k, v)]
+    cu_q, cu_k = i32([0, nq]), i32([0, nk])
+    desc = binding.window_desc(*dev, torch.empty_like(dev[0]), cu_q, d ** -0.5, nk)
+    prompt = binding.prompt_desc(*dev, torch.empty_like(dev[0]), cu_q, d ** -0.5)
+    assert binding.window_workspace_bytes(desc) == 0 and binding.prompt_workspace_bytes(prompt) > 0
+    want, want_lse, a, err = ref.window_attend(q, k, v, [nq], [nk], d ** -0.5, nk, 0)
+    for ws in (None, torch.empty(1, dtype=torch.uint8, device=DEV)):
+        out, lse = binding.reform_window_attend(*dev, cu_q, d ** -0.5, nk, cu_k=cu_k, workspace=ws)
+        check_attention(out, lse, want, want_lse, a, err, nk, dtype)
+    out, lse = binding.reform_prompt_attend(*dev, cu_q, d ** -0.5, cu_k=cu_k)
+    check_attention(out, lse, want, want_lse, a, err, nk, dtype)
