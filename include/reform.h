@@ -569,7 +569,8 @@ reform_status reform_tree_accept(const reform_accept_desc *desc, const int32_t *
  *     q, out, k, v, cu_q, cu_k, lse   as in reform_prompt_attend: layouts, lengths read on the device, boundaries that are out of
  *              place, rows of no sequence, arithmetic.  Keys and values that are not finite stay within their sequence; there, rows
  *              whose block goes through their tile of 64 keys may become NaN as well as those that see them
- * Supported: as reform_prompt_attend; window >= 1, n_sink >= 0.
+ * Supported: as reform_prompt_attend; window >= 1, n_sink >= 0; out and lse without a byte in common with the inputs or each other
+ * (REFORM_ERR_INVALID_ARG).
  * No workspace is needed: the query gives 0, and what is passed is not looked at.  Few rows behind a wide window are not shared out over
  * workgroups, as reform_prompt_attend does it, which is the faster call there where the window covers all keys.
  */
@@ -612,7 +613,7 @@ reform_status reform_window_attend(const reform_window_desc *desc, const void *q
  *     cache_len   [n_seq] int32 in device memory; values outside [0, max_len] are moved into it
  *     score       [n_seq][n_kv_heads][>= max_len] fp32 by strides, entries contiguous; may be NULL
  *     lse         [n_seq][n_q_heads] fp32, may be NULL
- * out, lse and score lie apart from the inputs and one another.
+ * out, lse and score have no byte in common with the inputs or one another (REFORM_ERR_INVALID_ARG; they may lie between one another's rows).
  * Arithmetic: products and sums in fp32; for bf16 the probabilities of the P.V product are taken in two bf16 parts (16 bits), the score sums the
  * unrounded fp32 ones.  Bitwise reproducible for the same arguments; results depend on the batch and on max_len by rounding only.
  * Keys and values that are not finite matter where they are seen only, and there stay within their sequence and KV head (an infinite
@@ -660,7 +661,8 @@ reform_status reform_paged_attend(const reform_paged_desc *desc, const void *q, 
  *     pos      like score, with its strides, int32 that travel with the rows, in/out; may be NULL
  *     kept_idx [n_seq][n_kv_heads][budget] int32 out, contiguous, the first new_len entries of a head; may be NULL
  *     new_len  [n_seq] int32 out, may be NULL
- * k, v, score, pos, kept_idx and new_len lie apart from one another (k and v may be parts of one pool) and from the inputs.
+ * k, v, score, pos, kept_idx and new_len have no byte in common with one another or the inputs (REFORM_ERR_INVALID_ARG; k and v may be
+ * parts of one pool).
  * The workspace takes the kept keys, and rows that are set aside where few heads have many; the query gives 0 where max_len is within
  * the budget.  Without it, or with less than the query asks for, the call returns REFORM_ERR_WORKSPACE.
  * Supported: head_dim * sizeof(element) a multiple of 16 up to 4096; strides of k and v multiples of 16 bytes; page_len, n_pages,

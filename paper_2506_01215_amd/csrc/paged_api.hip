@@ -26,7 +26,7 @@ namespace {
 constexpr int64_t kMaxPagedKeys = (1ll << 31) - 65536;   // keys are counted in 32-bit signed integers, some tiles or chunks past the last one
 inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
-// An output that is another output or an input, where it is given at all.
+// An output that is another output or an input, where it is given at all.  (The workspace is asked for before the whole tensors are compared.)
 bool shared(std::initializer_list<const void *> outs, std::initializer_list<const void *> ins)
 {
     for (const void *const *x = outs.begin(); x != outs.end(); ++x) {
@@ -111,6 +111,22 @@ PagedPool pool_of(const DESC *d, const int32_t *page_table)
     const uint64_t one = 1ull << (32 + p.shift);
     p.magic = (unsigned)((one + (uint64_t)d->page_len - 1) / (uint64_t)d->page_len - (1ull << 32));
     return p;
+}
+
+template <class DESC>
+Area pool_area(const DESC *d, const void *x)
+{
+    return area_of(x, elt_size(d->dtype), d->head_dim, {{d->n_pages, d->kv_page_stride}, {d->n_kv_heads, d->kv_head_stride}, {d->page_len, d->kv_row_stride}});
+}
+
+template <class DESC>
+Area table_area(const DESC *d, const int32_t *x) { return area_of(x, 4, d->max_pages, {{d->n_seq, d->table_stride}}); }
+
+// Of score, or of what has its strides.
+template <class DESC>
+Area score_area(const DESC *d, const void *x)
+{
+    return area_of(x, 4, d->max_len, {{d->n_seq, d->score_seq_stride}, {d->n_kv_heads, d->score_head_stride}});
 }
 
 reform_status check_paged(const reform_paged_desc *d)
@@ -233,6 +249,11 @@ reform_status reform_window_attend(const reform_window_desc *d, const void *q, c
     if (shared({out, lse}, {q, k, v, cu_q, cu_k})) return REFORM_ERR_INVALID_ARG;
     WindowParams p = window_sizes(d);
     p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse; p.cu_q = cu_q; p.cu_k = cu_k;
+    const int64_t es = elt_size(d->dtype), dim = d->head_dim;
+    if (mixed({area_of(out, es, dim, {{p.Hq, p.o_hs}, {p.n_q, p.o_rs}}), area_of(lse, 4, (int64_t)p.Hq * p.n_q, {})},
+              {area_of(q, es, dim, {{p.Hq, p.q_hs}, {p.n_q, p.q_rs}}), area_of(k, es, dim, {{p.Hkv, p.k_hs}, {p.n_k, p.k_rs}}),
+               area_of(v, es, dim, {{p.Hkv, p.v_hs}, {p.n_k, p.v_rs}}), area_of(cu_q, 4, p.n_seq + 1, {}), area_of(cu_k, 4, p.n_seq + 1, {})}))
+        return REFORM_ERR_INVALID_ARG;
     return window_attend_launch(p, d->dtype == REFORM_BF16, (hipStream_t)hip_stream) == hipSuccess ? REFORM_OK : REFORM_ERR_RUNTIME;
 }
 
@@ -265,6 +286,11 @@ reform_status reform_paged_attend(const reform_paged_desc *d, const void *q, con
         p.logits = room.logits ? (float *)(at + room.part_o + room.part_ml) : nullptr;
         p.row_ml = room.row_ml ? (float2 *)(at + room.part_o + room.part_ml + room.logits) : nullptr;
     }
+    const int64_t es = elt_size(d->dtype);
+    if (mixed({area_of(out, es, p.D, {{p.n_seq, p.o_ss}, {p.Hq, p.o_hs}}), area_of(lse, 4, (int64_t)p.n_seq * p.Hq, {}), score_area(d, score)},
+              {area_of(q, es, p.D, {{p.n_seq, p.q_ss}, {p.Hq, p.q_hs}}), pool_area(d, k), pool_area(d, v), table_area(d, page_table),
+               area_of(cache_len, 4, p.n_seq, {})}))
+        return REFORM_ERR_INVALID_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     const hipError_t e = d->dtype == REFORM_BF16 ? paged_attend_bf16(p, st) : paged_attend_f32_launch(p, st);
     return e == hipSuccess ? REFORM_OK : REFORM_ERR_RUNTIME;
@@ -297,6 +323,11 @@ reform_status reform_paged_evict(const reform_paged_evict_desc *d, void *k, void
         p.first = (int32_t *)(at + room.list);
         p.stage = at + room.list + room.first;
     }
+    const int64_t items = (int64_t)p.n_seq * p.Hkv;
+    if (mixed({pool_area(d, k), pool_area(d, v), score_area(d, score), score_area(d, pos), area_of(kept_idx, 4, items * p.budget, {}),
+               area_of(new_len, 4, p.n_seq, {})},
+              {table_area(d, page_table), area_of(cache_len, 4, p.n_seq, {})}))
+        return REFORM_ERR_INVALID_ARG;
     return paged_evict_launch(p, (hipStream_t)hip_stream) == hipSuccess ? REFORM_OK : REFORM_ERR_RUNTIME;
 }
 

@@ -2,20 +2,15 @@
 #pragma once
 #include "../../include/reform.h"
 #include "common.h"
+#include "overlap.h"
 
-#include <algorithm>
 #include <cmath>
-#include <initializer_list>
 
 namespace reform {
 
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 inline int64_t elt_size(int dtype) { return dtype == REFORM_BF16 ? 2 : 4; }
 inline bool known_dtype(int dtype) { return dtype == REFORM_F32 || dtype == REFORM_BF16; }
-
-struct Walk {
-    int64_t n, step;
-};
 
 // Strides of something that is written: its pieces of `extent` elements, at every combination of the walks' steps, must not
 // overlap.  Sorted by their steps, each walk's step has to pass over all that the ones before it cover.
@@ -32,6 +27,18 @@ inline bool bad_out_strides(int64_t extent, std::initializer_list<Walk> walks)
     for (int i = 0; i < n; ++i) {
         if ((double)w[i].step < covered) return true;
         covered += (double)(w[i].n - 1) * (double)w[i].step;
+    }
+    return false;
+}
+
+// Whether an output has a byte in common with another output or an input.
+inline bool mixed(std::initializer_list<Area> outs, std::initializer_list<Area> ins)
+{
+    for (const Area *x = outs.begin(); x != outs.end(); ++x) {
+        for (const Area *y = x + 1; y != outs.end(); ++y)
+            if (areas_meet(*x, *y)) return true;
+        for (const Area &y : ins)
+            if (areas_meet(*x, y)) return true;
     }
     return false;
 }
