@@ -617,13 +617,17 @@ reform_status reform_window_attend(const reform_window_desc *desc, const void *q
  * Arithmetic: products and sums in fp32; for bf16 the probabilities of the P.V product are taken in two bf16 parts (16 bits), the score sums the
  * unrounded fp32 ones.  Bitwise reproducible for the same arguments; results depend on the batch and on max_len by rounding only.
  * Keys and values that are not finite matter where they are seen only, and there stay within their sequence and KV head (an infinite
- * value may give NaN).  Rows behind L are never looked at.
+ * value may give NaN), in the score within the keys that are seen.  Rows behind L are never looked at.
  * Supported: types and head_dim as reform_prompt_attend; any page_len >= 1; n_pages * page_len below 2^31; max_len at most
  * max_pages * page_len and 2^31 - 65536; row stride of k and v below 2^24; n_seq * n_q_heads at most 2^22; with B = ceil(n_q_heads /
  * n_kv_heads / 16), n_seq * n_kv_heads * B * (max_len / 16 + 64) below 2^31.  n_seq = 0 does nothing.
  * The workspace takes partial results of caches that are shared out over workgroups, and the logits of all keys if the score is asked
  * for (4 bytes a key that can be seen and query head); the query wants to know whether it is: want_score.  Without it, or with less than the
- * query asks for, the call returns REFORM_ERR_WORKSPACE.
+ * query asks for, the call returns REFORM_ERR_WORKSPACE.  The host knows max_len and not the lengths: that decides the workspace's size, how
+ * the keys are shared out, and whether K and V go past the caches' order of replacement (64 MB and more of them), so a bound that fits the batch
+ * is the faster one.
+ * The score is that of generated tokens: the calls on prompts add nothing to it, and the first eviction after a prompt ranks its keys by what the
+ * tokens since then gave them.  A program that wants more in it before writes that into score.
  */
 typedef struct {
     uint32_t struct_size;

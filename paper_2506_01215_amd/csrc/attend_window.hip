@@ -4,6 +4,10 @@
 // the first key that its first row's window shows to the last that its last row sees, in tiles cut from both counted through (WindowKeys).  Only tiles at the
 // ends of the runs are masked.
 //
+// The probabilities of P.V are rounded to bf16 once, as the packed prompts' are: outputs are off by 0.0020 to 0.0023 of their norm, where their
+// own rounding alone makes 0.0016 to 0.0017.  What the rounding leaves would take a second product, half as much again of what bounds long prompts; the
+// matrix pipe of single tokens waits for memory, and they take it.
+//
 //   window_attend<D,NW,KG>         blocks of 32 NW rows, all waves through the same tiles, KG groups of them (attend_rows.h)
 //   window_attend_short<D,NB,NW>   blocks of 16 NB rows whose NW waves divide the tiles (attend_seq.h)
 //   window_attend_f32<DP>          blocks of 16 rows, fp32 (attend_seq_f32.h)

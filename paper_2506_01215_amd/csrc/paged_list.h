@@ -264,7 +264,8 @@ inline void paged_plan(PagedParams &p, int R, int TK, int whole, int least, int 
     if (keys < 32) keys = 32;
     p.logit_keys = (int)keys;
     list_plan(p, p.G, (double)keys, R, TK, whole, least, p.units, workgroups);
-    // K and V that are read once, and too large to be there still when they are read next.  8 sequences, pages of 16, us with / without
+    // K and V that are read once, and too large to be there still when they are read next, as far as the host can tell: by the longest that the caches
+    // may be, so short ones in a wide table take the hint as well, and the times of the small sizes.  8 sequences, pages of 16, us with / without
     // the hint, a program that goes round 3 such caches | 24 of them: 31 MB 15.6 / 13.0 | 15.8 / 17.4, 63 MB 19.8 / 19.9 | 20.3 /
     // 22.1, 127 MB 28.9 / 31.5 | 29.6 / 32.9, 399 MB 68.1 / 77.7; several row blocks (64/1 heads, 67 MB) 32.3 / 26.5 | 32.9 / 31.2
     // fp32: from twice as many bytes on (8 caches, 98 MB 33.0 / 34.0, 65 MB 31.8 / 31.6)
